@@ -30,7 +30,7 @@
  *
  * Pointers.  Unless a field says "host", every pointer is a DEVICE pointer owned by the
  * caller and borrowed until the work enqueued by the call has completed on the stream.  The
- * library writes only `out`, `span_mass`, `workspace` and `status`.  Calls enqueue work on the
+ * attention calls write only `out`, `span_mass`, `workspace` and `status`.  Calls enqueue work on the
  * caller's stream, never synchronise, and never allocate device memory.  Return codes are
  * synchronous and cover argument validation and launch errors; faults the device detects
  * (a block-table entry outside [0, num_blocks), a sequence longer than its table, more rows
@@ -63,7 +63,8 @@ enum {
     HOOK_ATTN_ERR_WORKSPACE = -3,   /* workspace missing or smaller than hook_attn_workspace_bytes */
     HOOK_ATTN_ERR_CUDA = -4,        /* a CUDA runtime/driver call failed (launch, attribute) */
     HOOK_ATTN_ERR_TIMEOUT = -5,     /* device status: a bounded wait inside a kernel ran out */
-    HOOK_ATTN_ERR_BOUNDS = -6       /* device status: block id / length outside its range */
+    HOOK_ATTN_ERR_BOUNDS = -6,      /* device status: block id / length outside its range */
+    HOOK_ATTN_ERR_NO_PAGES = -7     /* device status: hook_cache_extend ran out of free pages */
 };
 
 /* Which query rows of a prefill call are probed: the config's "hookq_mode" (Section 2). */
@@ -227,6 +228,148 @@ int hook_capture_qk(hook_attn_handle* handle, const hook_attn_params* p, int is_
  * word `waited_ns`, and returns normally: no trap, no hang, the context stays usable. */
 int hook_attn_selftest_wait_limit(hook_attn_handle* handle, int32_t* status, uint64_t limit_ns, uint64_t* waited_ns,
                                   void* cuda_stream);
+
+/* ---- what a decode step needs around the attention -------------------------------------------------------
+ * (The paper leaves all of it to the engine it plugs into: Section 2.1, execute_model runs the model's forward
+ * pass over the engine's cache.)  The conventions above hold: device pointers unless a field says host, the
+ * caller's stream, no synchronisation, no allocation, HOOK_ATTN_ERR_INVALID_ARG unless the handle's device is
+ * current, an optional status word for what only the device can see. */
+
+enum { HOOK_DTYPE_BF16 = 0, HOOK_DTYPE_F16 = 1, HOOK_DTYPE_F32 = 2 };
+
+/* Which axis turns which pair of a head: the pairs of axis 0, then those of axis 1, ... (BLOCKED), or dealt
+ * out in turn, one to each axis that still has some left (CYCLIC). */
+enum { HOOK_ROPE_AXES_BLOCKED = 0, HOOK_ROPE_AXES_CYCLIC = 1 };
+/* Which elements of a head form pair p: p and p + rotary_dim / 2, or 2 p and 2 p + 1. */
+enum { HOOK_ROPE_PAIR_HALVES = 0, HOOK_ROPE_PAIR_ADJACENT = 1 };
+#define HOOK_ROPE_MAX_AXES 4
+
+typedef struct {
+    /* ---- shapes ---- */
+    int32_t num_seqs, total_q, num_q_heads, num_kv_heads, head_dim, page_size, num_blocks, max_blocks_per_seq;
+    int32_t dtype;               /* HOOK_DTYPE_* of q, k and v; what is written is bf16 */
+    int32_t rotary_dim;          /* R, even, 0 .. head_dim: the first R elements of a head are rotated */
+    int32_t num_axes;            /* 1 .. HOOK_ROPE_MAX_AXES (time, height, width, ...) */
+    int32_t axis_pairs[HOOK_ROPE_MAX_AXES]; /* pairs of each axis; they add up to R / 2 */
+    int32_t axis_order;          /* HOOK_ROPE_AXES_* */
+    int32_t pairing;             /* HOOK_ROPE_PAIR_* */
+    float   factor;              /* multiplies cosines and sines (long-context scalings); finite */
+
+    /* ---- device tensors ---- */
+    const void*    q;            /* [total_q][Hq][D], strides in elements; the last one is 1 */
+    const void*    k;            /* [total_q][Hkv][D] */
+    const void*    v;            /* [total_q][Hkv][D] */
+    int64_t        q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+    const float*   inv_freq;     /* fp32 [R / 2]; NULL when R = 0 */
+    const int32_t* positions;    /* [num_axes][total_q], axes position_axis_stride apart; NULL: every axis has the
+                                    row's position in its sequence */
+    int64_t        position_axis_stride;
+    void*          q_out;        /* bf16 [total_q][Hq][D], contiguous; may be q itself (bf16 and contiguous), and
+                                    overlaps none of the inputs otherwise */
+    void*          k_cache;      /* as in hook_attn_params, written here */
+    void*          v_cache;
+    int64_t        kv_block_stride, kv_token_stride, kv_head_stride;
+    const int32_t* block_table;
+    const int32_t* seq_lens;     /* L_s INCLUDING this call's rows */
+    const int32_t* cu_q_lens;    /* [num_seqs + 1]; NULL: decode, one row per sequence, total_q == num_seqs */
+    int32_t*       status;
+} hook_rope_params;
+
+/* Rotary positions with several axes, appended to the cache: what the rows of a call need before
+ * hook_attn_prefill / hook_attn_decode.  Pair p of a q or k head turns by positions[axis(p)][row] * inv_freq[p]:
+ *   (a, b) -> factor * (a cos - b sin, b cos + a sin)
+ * with the angle reduced in 64 bits, the rest in 32, and one rounding to bf16.  k and v of row i of sequence s go
+ * to position L_s - n_s + i of its pages; the pages that are written belong to one sequence alone
+ * (hook_cache_extend sees to it).  Rows behind cu_q_lens[num_seqs] are left as they were.  A row whose sequence
+ * or page is out of range (L_s beyond its table, n_s > L_s, a block id outside the pool) sets status, its q_out
+ * row is zeroed and nothing is appended for it. */
+int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* cuda_stream);
+
+typedef struct {
+    int32_t num_rows, vocab_size, max_tokens, num_bias, num_masks;
+    int32_t dtype, out_dtype;    /* HOOK_DTYPE_* of logits; of out: the same, or HOOK_DTYPE_F32 */
+    const void*     logits;      /* [num_rows][vocab_size], rows logits_row_stride elements apart */
+    void*           out;         /* may be logits itself (same type and stride), and overlaps nothing otherwise */
+    int64_t         logits_row_stride, out_row_stride;
+    const int32_t*  tokens;      /* [num_rows][max_tokens]: a row's prompt, then what was generated; ids outside
+                                    [0, vocab_size) (placeholders) are passed over.  NULL: no penalties */
+    int64_t         tokens_row_stride;
+    const int32_t*  prompt_lens; /* [num_rows] tokens of the prompt */
+    const int32_t*  total_lens;  /* [num_rows] tokens of prompt and generation, prompt_lens <= total_lens <= max_tokens */
+    const float*    repetition;  /* [num_rows], > 0; NULL: 1 */
+    const float*    presence;    /* [num_rows]; NULL: 0 */
+    const float*    frequency;   /* [num_rows]; NULL: 0 */
+    const int32_t*  bias_offsets;/* [num_rows + 1] prefix sums of the rows' bias entries; NULL: no biases */
+    const int32_t*  bias_tokens; /* [num_bias]; of a token named twice in a row the last entry counts */
+    const float*    bias_values; /* [num_bias] */
+    const uint32_t* mask;        /* [num_masks][ceil(vocab_size / 32)], bit v % 32 of word v / 32: token v is
+                                    allowed.  NULL: no grammar */
+    int64_t         mask_row_stride; /* in words */
+    const int32_t*  mask_rows;   /* [num_rows] row of mask, negative: the row has no grammar.  NULL: row r has mask r */
+    int32_t*        status;
+} hook_logits_params;
+
+/* Edits of the logits before a token is chosen, in 32 bits with one rounding to out's type.  With c the number of
+ * times token v was generated in the row, and `seen` whether it is in its prompt or generated:
+ *   x = seen ? (x > 0 ? x / repetition : x * repetition) : x;   x -= frequency * c + presence * (c > 0);
+ *   x += bias[v];   x = -inf if the grammar forbids v (whatever x is; a mask may forbid all).
+ * A row whose lengths, bias offsets or mask row are out of range sets status and its part of out is not written; a
+ * bias for a token outside the vocabulary sets status and is passed over.  vocab_size <= 2^20. */
+int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, void* cuda_stream);
+
+/* The pool that the sequences of a cache share.  All its arrays are written by the calls below. */
+typedef struct {
+    int32_t  num_seqs, max_blocks_per_seq, num_blocks, page_size;   /* num_seqs <= 16384 */
+    int32_t* block_table;        /* [num_seqs][max_blocks_per_seq] */
+    int32_t* seq_lens;           /* [num_seqs] tokens; 0: the row is empty */
+    int32_t* page_refs;          /* [num_blocks] sequences that hold the page; 0: free */
+    int32_t* status;
+} hook_cache_pool;
+
+/* children[i] becomes a copy of sequence parents[i] that shares its pages (no data moves).  An entry is passed
+ * over, with status HOOK_ATTN_ERR_BOUNDS, when one of its rows does not exist, its child is not empty, is named by
+ * an earlier entry or is a parent in this call, or the parent's length or pages are out of range. */
+int hook_cache_fork(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* parents, const int32_t* children,
+                    int32_t num_forks, void* cuda_stream);
+
+/* Room for new_rows[s] >= 0 more tokens in every sequence: the missing pages are taken from the pool, lowest ids
+ * first and in the order of the sequences, and seq_lens grows.  A sequence that would write into a partly filled
+ * page that it shares gets a page of its own instead, and pairs[s] = (old page, new page) for
+ * hook_cache_copy_pages; else pairs[s] = (-1, -1).  Sequences that the pool cannot serve in their turn stay as
+ * they are and set status HOOK_ATTN_ERR_NO_PAGES; those whose length, table or last page is out of range stay as
+ * they are and set HOOK_ATTN_ERR_BOUNDS.  pairs: int32 [num_seqs][2]. */
+int hook_cache_extend(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* new_rows, int32_t* pairs,
+                      void* cuda_stream);
+
+/* Cuts sequence seqs[i] to its first keep_lens[i] tokens (NULL: 0, the whole sequence goes; more than it has:
+ * nothing happens): the pages behind them are given back, or to the others that share them, and their table
+ * entries become -1.  Of a sequence that is named twice the first entry counts.  A row that does not exist, a
+ * negative or too long length and a page that nobody holds set status. */
+int hook_cache_free(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* seqs, const int32_t* keep_lens,
+                    int32_t num_entries, void* cuda_stream);
+
+/* Plans how the U pages in use move together at the low end of the pool: the k-th used page at U or above goes to
+ * the k-th free page below U.  The pool itself is only read, so that the old tables stay valid until the pairs are
+ * copied.  Outputs: block_table_out (like block_table; may be block_table itself; -1 behind a sequence's pages),
+ * page_refs_out (like page_refs, not page_refs itself), page_map int32 [num_blocks] (where each page is afterwards,
+ * -1: free), pairs int32 [num_blocks / 2][2] (source, destination; -1 behind the last), num_pairs int32 [1]. */
+int hook_cache_compact(hook_attn_handle* handle, const hook_cache_pool* pool, int32_t* block_table_out, int32_t* page_refs_out,
+                       int32_t* page_map, int32_t* pairs, int32_t* num_pairs, void* cuda_stream);
+
+typedef struct {
+    int32_t num_layers, num_blocks, page_size, num_kv_heads, head_dim, max_pairs;
+    int64_t kv_block_stride, kv_token_stride, kv_head_stride;   /* of every layer's caches, in elements */
+    void* const*   k_caches;     /* HOST array [num_layers] of device pointers */
+    void* const*   v_caches;     /* HOST array [num_layers] */
+    const int32_t* pairs;        /* [max_pairs][2] source and destination page; a negative one: passed over */
+    const int32_t* num_pairs;    /* device int32 [1], how many of them count; NULL: max_pairs */
+    int32_t*       status;
+} hook_cache_copy_params;
+
+/* Copies pages in the caches of all layers.  A source may have many destinations.  The pairs are independent of one
+ * another: one whose destination is also another pair's destination or source, or whose source is another pair's
+ * destination, is not carried out and sets status, like one outside the pool. */
+int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params* p, void* cuda_stream);
 
 /* Human-readable name of a return / status code. */
 const char* hook_attn_strerror(int code);

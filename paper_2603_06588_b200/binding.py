@@ -22,16 +22,23 @@ HOOK_ATTN_ERR_WORKSPACE = -3
 HOOK_ATTN_ERR_CUDA = -4
 HOOK_ATTN_ERR_TIMEOUT = -5
 HOOK_ATTN_ERR_BOUNDS = -6
+HOOK_ATTN_ERR_NO_PAGES = -7
 HOOK_PROBE_ROWS_ALL = 0
 HOOK_PROBE_ROWS_LAST = 1
 
 EXPORTS = ("hook_attn_create", "hook_attn_destroy", "hook_attn_workspace_bytes",
            "hook_attn_prefill", "hook_attn_decode", "hook_attn_mixed", "hook_attn_decode_static_scratch",
-           "hook_attn_score", "hook_steer_residual", "hook_capture_qk", "hook_attn_selftest_wait_limit",
-           "hook_attn_strerror")
+           "hook_attn_score", "hook_steer_residual", "hook_capture_qk", "hook_rope_append", "hook_adjust_logits",
+           "hook_cache_fork", "hook_cache_extend", "hook_cache_free", "hook_cache_compact", "hook_cache_copy_pages",
+           "hook_attn_selftest_wait_limit", "hook_attn_strerror")
 HOOK_SCORE_MEAN = 0
 HOOK_SCORE_SUM_NORMALIZE = 1
 STATIC_SCRATCH_BYTES = 16 << 20   # HOOK_ATTN_STATIC_SCRATCH_BYTES
+HOOK_DTYPE_BF16, HOOK_DTYPE_F16, HOOK_DTYPE_F32 = 0, 1, 2
+HOOK_ROPE_AXES_BLOCKED, HOOK_ROPE_AXES_CYCLIC = 0, 1
+HOOK_ROPE_PAIR_HALVES, HOOK_ROPE_PAIR_ADJACENT = 0, 1
+HOOK_ROPE_MAX_AXES = 4
+_DTYPES = {torch.bfloat16: HOOK_DTYPE_BF16, torch.float16: HOOK_DTYPE_F16, torch.float32: HOOK_DTYPE_F32}
 
 
 class HookAttnParams(ctypes.Structure):
@@ -53,6 +60,48 @@ class HookAttnParams(ctypes.Structure):
         ("workspace_bytes", ctypes.c_size_t), ("status", ctypes.c_void_p),
         ("head_mask", ctypes.c_void_p), ("alpha", ctypes.c_void_p),
     ]
+
+
+def _fields(text: str, ctype) -> list:
+    return [(name, ctype) for name in text.split()]
+
+
+class HookRopeParams(ctypes.Structure):
+    """Mirror of ``hook_rope_params``."""
+    _fields_ = (
+        _fields("num_seqs total_q num_q_heads num_kv_heads head_dim page_size num_blocks max_blocks_per_seq dtype rotary_dim num_axes",
+                ctypes.c_int32)
+        + [("axis_pairs", ctypes.c_int32 * HOOK_ROPE_MAX_AXES), ("axis_order", ctypes.c_int32), ("pairing", ctypes.c_int32),
+           ("factor", ctypes.c_float)]
+        + _fields("q k v", ctypes.c_void_p)
+        + _fields("q_row_stride q_head_stride k_row_stride k_head_stride v_row_stride v_head_stride", ctypes.c_int64)
+        + _fields("inv_freq positions", ctypes.c_void_p) + [("position_axis_stride", ctypes.c_int64)]
+        + _fields("q_out k_cache v_cache", ctypes.c_void_p)
+        + _fields("kv_block_stride kv_token_stride kv_head_stride", ctypes.c_int64)
+        + _fields("block_table seq_lens cu_q_lens status", ctypes.c_void_p))
+
+
+class HookLogitsParams(ctypes.Structure):
+    """Mirror of ``hook_logits_params``."""
+    _fields_ = (
+        _fields("num_rows vocab_size max_tokens num_bias num_masks dtype out_dtype", ctypes.c_int32)
+        + _fields("logits out", ctypes.c_void_p) + _fields("logits_row_stride out_row_stride", ctypes.c_int64)
+        + [("tokens", ctypes.c_void_p), ("tokens_row_stride", ctypes.c_int64)]
+        + _fields("prompt_lens total_lens repetition presence frequency bias_offsets bias_tokens bias_values mask", ctypes.c_void_p)
+        + [("mask_row_stride", ctypes.c_int64)] + _fields("mask_rows status", ctypes.c_void_p))
+
+
+class HookCachePool(ctypes.Structure):
+    """Mirror of ``hook_cache_pool``."""
+    _fields_ = (_fields("num_seqs max_blocks_per_seq num_blocks page_size", ctypes.c_int32)
+                + _fields("block_table seq_lens page_refs status", ctypes.c_void_p))
+
+
+class HookCacheCopyParams(ctypes.Structure):
+    """Mirror of ``hook_cache_copy_params``."""
+    _fields_ = (_fields("num_layers num_blocks page_size num_kv_heads head_dim max_pairs", ctypes.c_int32)
+                + _fields("kv_block_stride kv_token_stride kv_head_stride", ctypes.c_int64)
+                + _fields("k_caches v_caches pairs num_pairs status", ctypes.c_void_p))
 
 
 class HookAttnError(RuntimeError):
@@ -95,6 +144,17 @@ def load_library() -> ctypes.CDLL:
         lib.hook_capture_qk.restype = ctypes.c_int
         lib.hook_capture_qk.argtypes = [ctypes.c_void_p, ctypes.POINTER(HookAttnParams), ctypes.c_int, ctypes.c_void_p,
                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+        void_p, i32 = ctypes.c_void_p, ctypes.c_int32
+        for name, args in (("hook_rope_append", [ctypes.POINTER(HookRopeParams)]),
+                           ("hook_adjust_logits", [ctypes.POINTER(HookLogitsParams)]),
+                           ("hook_cache_fork", [ctypes.POINTER(HookCachePool), void_p, void_p, i32]),
+                           ("hook_cache_extend", [ctypes.POINTER(HookCachePool), void_p, void_p]),
+                           ("hook_cache_free", [ctypes.POINTER(HookCachePool), void_p, void_p, i32]),
+                           ("hook_cache_compact", [ctypes.POINTER(HookCachePool)] + [void_p] * 5),
+                           ("hook_cache_copy_pages", [ctypes.POINTER(HookCacheCopyParams)])):
+            fn = getattr(lib, name)
+            fn.restype = ctypes.c_int
+            fn.argtypes = [void_p] + args + [void_p]
         lib.hook_attn_selftest_wait_limit.restype = ctypes.c_int
         lib.hook_attn_selftest_wait_limit.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p,
                                                       ctypes.c_void_p]
@@ -159,7 +219,7 @@ def make_params(*, q, k_cache, v_cache, block_table, seq_lens, cu_q_lens=None, s
 
 
 class HookAttn:
-    """Per-device handle plus the two entry points, taking torch CUDA tensors."""
+    """Per-device handle plus the entry points, taking torch CUDA tensors."""
 
     def __init__(self, device: int = 0):
         lib = load_library()
@@ -267,6 +327,163 @@ class HookAttn:
         if rc != HOOK_ATTN_OK:
             raise HookAttnError(rc, "hook_capture_qk")
         return q_out, k_out, cu_k
+
+    # -- what a decode step needs around the attention --------------------------------------
+    def _checked(self, name: str, *args, stream=None) -> None:
+        rc = int(getattr(self._lib, name)(self._h, *args, self._stream(stream)))
+        if rc != HOOK_ATTN_OK:
+            raise HookAttnError(rc, name)
+
+    def hook_rope_append(self, *, q, k, v, k_cache, v_cache, block_table, seq_lens, inv_freq, cu_q_lens=None, positions=None,
+                         axis_pairs=None, axis_order: int = HOOK_ROPE_AXES_BLOCKED, pairing: int = HOOK_ROPE_PAIR_HALVES,
+                         factor: float = 1.0, q_out=None, status=None, stream=None) -> torch.Tensor:
+        """Rotates ``q [T, Hq, D]`` and ``k [T, Hkv, D]`` and appends k and ``v`` to the pages of the rows' sequences.
+        ``inv_freq`` fp32 ``[R / 2]`` gives the frequencies of the pairs and R; ``axis_pairs`` how many pairs each axis has (default:
+        one axis); ``positions`` int32 ``[axes, T]`` (default: the rows' places in their sequences).  bf16, fp16 or fp32 in, the
+        rotated queries out as bf16, contiguous, like the attention reads them."""
+        total_q, hq, d = q.shape
+        nb, page, hkv, d2 = k_cache.shape
+        assert d2 == d and v_cache.shape == k_cache.shape and v_cache.stride() == k_cache.stride() and k_cache.stride(3) == 1
+        assert k_cache.dtype == v_cache.dtype == torch.bfloat16
+        assert k.shape == v.shape == (total_q, hkv, d) and q.dtype == k.dtype == v.dtype
+        assert (q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1) or total_q == 0
+        assert block_table.dtype == seq_lens.dtype == torch.int32 and block_table.is_contiguous() and seq_lens.is_contiguous()
+        assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+        if q_out is None:
+            q_out = torch.empty((total_q, hq, d), dtype=torch.bfloat16, device=q.device)
+        assert q_out.dtype == torch.bfloat16 and q_out.shape == q.shape and q_out.is_contiguous()
+        pairs = inv_freq.shape[0]
+        axis_pairs = (pairs,) if axis_pairs is None else tuple(axis_pairs)
+        p = HookRopeParams()
+        p.num_seqs, p.total_q, p.num_q_heads, p.num_kv_heads, p.head_dim, p.page_size = seq_lens.shape[0], total_q, hq, hkv, d, page
+        p.num_blocks, p.max_blocks_per_seq = nb, block_table.shape[1]
+        assert block_table.shape[0] == p.num_seqs
+        p.dtype, p.rotary_dim, p.num_axes = _DTYPES[q.dtype], 2 * pairs, len(axis_pairs)
+        p.axis_pairs[:min(len(axis_pairs), HOOK_ROPE_MAX_AXES)] = axis_pairs[:HOOK_ROPE_MAX_AXES]
+        p.axis_order, p.pairing, p.factor = int(axis_order), int(pairing), float(factor)
+        p.q, p.k, p.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
+        p.q_row_stride, p.q_head_stride, _ = q.stride()
+        p.k_row_stride, p.k_head_stride, _ = k.stride()
+        p.v_row_stride, p.v_head_stride, _ = v.stride()
+        p.inv_freq = inv_freq.data_ptr()
+        if positions is not None:
+            assert positions.dtype == torch.int32 and positions.shape == (len(axis_pairs), total_q)
+            assert positions.stride(1) == 1 or total_q <= 1
+            p.positions, p.position_axis_stride = positions.data_ptr(), positions.stride(0)
+        p.q_out, p.k_cache, p.v_cache = q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr()
+        p.kv_block_stride, p.kv_token_stride, p.kv_head_stride, _ = k_cache.stride()
+        p.block_table, p.seq_lens = block_table.data_ptr(), seq_lens.data_ptr()
+        if cu_q_lens is not None:
+            assert cu_q_lens.dtype == torch.int32 and cu_q_lens.is_contiguous() and cu_q_lens.shape[0] == p.num_seqs + 1
+            p.cu_q_lens = cu_q_lens.data_ptr()
+        p.status = _dptr(status)
+        self._checked("hook_rope_append", ctypes.byref(p), stream=stream)
+        return q_out
+
+    def hook_adjust_logits(self, logits, *, out=None, tokens=None, prompt_lens=None, total_lens=None, repetition=None, presence=None,
+                           frequency=None, bias_offsets=None, bias_tokens=None, bias_values=None, mask=None, mask_rows=None,
+                           status=None, stream=None) -> torch.Tensor:
+        """Penalties, biases and grammar masks on ``logits [rows, vocab]`` (bf16, fp16 or fp32; rows may be strided), in place or into
+        ``out`` (the same type, or fp32).  ``tokens`` int32 ``[rows, max_tokens]`` holds each row's prompt and what was generated;
+        the biases are lists in rows (``bias_offsets [rows + 1]``); ``mask`` int32 ``[masks, ceil(vocab / 32)]`` has a bit for each allowed
+        token and ``mask_rows`` says which of them a row has (negative: none)."""
+        out = logits if out is None else out
+        rows, vocab = logits.shape
+        assert out.shape == logits.shape and (vocab == 1 or (logits.stride(1) == 1 and out.stride(1) == 1))
+        p = HookLogitsParams()
+        p.num_rows, p.vocab_size, p.dtype, p.out_dtype = rows, vocab, _DTYPES[logits.dtype], _DTYPES[out.dtype]
+        p.logits, p.out = logits.data_ptr(), out.data_ptr()
+        p.logits_row_stride, p.out_row_stride = max(logits.stride(0), vocab), max(out.stride(0), vocab)
+        if tokens is not None:
+            assert tokens.dtype == torch.int32 and tokens.shape[0] == rows and (tokens.stride(1) == 1 or tokens.shape[1] <= 1)
+            for t in (prompt_lens, total_lens):
+                assert t.dtype == torch.int32 and t.shape == (rows,) and t.is_contiguous()
+            p.max_tokens, p.tokens_row_stride = tokens.shape[1], max(tokens.stride(0), tokens.shape[1])
+            p.tokens, p.prompt_lens, p.total_lens = tokens.data_ptr(), prompt_lens.data_ptr(), total_lens.data_ptr()
+        for name, t in (("repetition", repetition), ("presence", presence), ("frequency", frequency)):
+            if t is not None:
+                assert t.dtype == torch.float32 and t.shape == (rows,) and t.is_contiguous()
+                setattr(p, name, t.data_ptr())
+        if bias_offsets is not None:
+            assert bias_offsets.dtype == bias_tokens.dtype == torch.int32 and bias_values.dtype == torch.float32
+            assert bias_offsets.shape == (rows + 1,) and bias_tokens.shape == bias_values.shape
+            assert bias_offsets.is_contiguous() and bias_tokens.is_contiguous() and bias_values.is_contiguous()
+            p.num_bias = bias_tokens.shape[0]
+            p.bias_offsets, p.bias_tokens, p.bias_values = bias_offsets.data_ptr(), bias_tokens.data_ptr(), bias_values.data_ptr()
+        if mask is not None:
+            assert mask.dtype in (torch.int32, torch.uint32) and mask.shape[1] >= (vocab + 31) // 32
+            assert mask.stride(1) == 1 or mask.shape[1] == 1
+            p.num_masks, p.mask, p.mask_row_stride = mask.shape[0], mask.data_ptr(), max(mask.stride(0), mask.shape[1])
+            if mask_rows is not None:
+                assert mask_rows.dtype == torch.int32 and mask_rows.shape == (rows,) and mask_rows.is_contiguous()
+                p.mask_rows = mask_rows.data_ptr()
+        p.status = _dptr(status)
+        self._checked("hook_adjust_logits", ctypes.byref(p), stream=stream)
+        return out
+
+    @staticmethod
+    def _pool(block_table, seq_lens, page_refs, status) -> HookCachePool:
+        for t in (block_table, seq_lens, page_refs):
+            assert t.dtype == torch.int32 and t.is_contiguous()
+        seqs, width = block_table.shape
+        assert seq_lens.shape[0] == seqs
+        return HookCachePool(seqs, width, page_refs.shape[0], 16, block_table.data_ptr(), seq_lens.data_ptr(), page_refs.data_ptr(), _dptr(status))
+
+    def hook_cache_fork(self, block_table, seq_lens, page_refs, parents, children, status=None, stream=None) -> None:
+        """Sequence ``children[i]`` (empty) becomes a copy of ``parents[i]`` that shares its pages."""
+        assert parents.dtype == children.dtype == torch.int32 and parents.shape == children.shape
+        assert parents.is_contiguous() and children.is_contiguous()
+        pool = self._pool(block_table, seq_lens, page_refs, status)
+        self._checked("hook_cache_fork", ctypes.byref(pool), parents.data_ptr(), children.data_ptr(), parents.shape[0], stream=stream)
+
+    def hook_cache_extend(self, block_table, seq_lens, page_refs, new_rows, pairs=None, status=None, stream=None) -> torch.Tensor:
+        """Room for ``new_rows[s]`` more tokens in every sequence; returns ``pairs`` int32 ``[seqs, 2]``, the pages to copy before
+        anything is appended (-1: none)."""
+        assert new_rows.dtype == torch.int32 and new_rows.shape == seq_lens.shape and new_rows.is_contiguous()
+        if pairs is None:
+            pairs = torch.empty((seq_lens.shape[0], 2), dtype=torch.int32, device=seq_lens.device)
+        assert pairs.dtype == torch.int32 and pairs.shape == (seq_lens.shape[0], 2) and pairs.is_contiguous()
+        pool = self._pool(block_table, seq_lens, page_refs, status)
+        self._checked("hook_cache_extend", ctypes.byref(pool), new_rows.data_ptr(), pairs.data_ptr(), stream=stream)
+        return pairs
+
+    def hook_cache_free(self, block_table, seq_lens, page_refs, seqs, keep_lens=None, status=None, stream=None) -> None:
+        """Cuts the sequences ``seqs`` to their first ``keep_lens`` tokens (default: to nothing)."""
+        assert seqs.dtype == torch.int32 and seqs.is_contiguous()
+        assert keep_lens is None or (keep_lens.dtype == torch.int32 and keep_lens.shape == seqs.shape and keep_lens.is_contiguous())
+        pool = self._pool(block_table, seq_lens, page_refs, status)
+        self._checked("hook_cache_free", ctypes.byref(pool), seqs.data_ptr(), _dptr(keep_lens), seqs.shape[0], stream=stream)
+
+    def hook_cache_compact(self, block_table, seq_lens, page_refs, status=None, stream=None):
+        """Plans how the used pages move together at the low end of the pool.  Returns ``(block_table, page_refs, page_map, pairs,
+        num_pairs)`` as they are once the pairs are copied; the old ones stay as they are."""
+        pool = self._pool(block_table, seq_lens, page_refs, status)
+        nb = page_refs.shape[0]
+        table_out, refs_out, page_map = torch.empty_like(block_table), torch.empty_like(page_refs), torch.empty_like(page_refs)
+        pairs = torch.empty((nb // 2, 2), dtype=torch.int32, device=page_refs.device)
+        num_pairs = torch.empty(1, dtype=torch.int32, device=page_refs.device)
+        self._checked("hook_cache_compact", ctypes.byref(pool), table_out.data_ptr(), refs_out.data_ptr(), page_map.data_ptr(),
+                      pairs.data_ptr(), num_pairs.data_ptr(), stream=stream)
+        return table_out, refs_out, page_map, pairs, num_pairs
+
+    def hook_cache_copy_pages(self, caches, pairs, num_pairs=None, status=None, stream=None) -> None:
+        """Copies pages ``pairs[i] = (source, destination)`` in the ``caches``, a list of ``(k_cache, v_cache)`` of the layers (one
+        shape, one set of strides).  ``num_pairs``: int32 ``[1]`` on the device, how many of the pairs count."""
+        assert pairs.dtype == torch.int32 and pairs.dim() == 2 and pairs.shape[1] == 2 and pairs.is_contiguous()
+        assert num_pairs is None or (num_pairs.dtype == torch.int32 and num_pairs.numel() == 1)
+        n = len(caches)
+        if n == 0:
+            return
+        first = caches[0][0]
+        shape, stride = first.shape, first.stride()
+        assert first.dtype == torch.bfloat16 and stride[3] == 1
+        ks, vs = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)()
+        for i, (kc, vc) in enumerate(caches):
+            assert kc.shape == vc.shape == shape and kc.stride() == vc.stride() == stride and kc.dtype == vc.dtype == first.dtype
+            ks[i], vs[i] = kc.data_ptr(), vc.data_ptr()
+        p = HookCacheCopyParams(n, shape[0], shape[1], shape[2], shape[3], pairs.shape[0], stride[0], stride[1], stride[2],
+                                ctypes.addressof(ks), ctypes.addressof(vs), pairs.data_ptr(), _dptr(num_pairs), _dptr(status))
+        self._checked("hook_cache_copy_pages", ctypes.byref(p), stream=stream)
 
     # -- convenience ---------------------------------------------------------------------
     def plan(self, is_decode: bool, *, q, k_cache, v_cache, block_table, seq_lens, cu_q_lens=None,

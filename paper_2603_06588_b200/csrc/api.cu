@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "ops.cuh"
 
 namespace hook_attn {
 // decode.cu
@@ -35,6 +36,19 @@ cudaError_t launch_steer_residual(__nv_bfloat16* hidden, const float* vec, float
                                   int64_t row_stride, int num_sms, cudaStream_t st);
 cudaError_t launch_capture(const KernelArgs& a, const HeadCfg& hc, int head_dim, bool decode, __nv_bfloat16* q_out,
                            __nv_bfloat16* k_out, const int32_t* cu_k, cudaStream_t st);
+// rope.cu
+cudaError_t launch_rope_append(const RopeArgs& a, int dtype, cudaStream_t st);
+// logits.cu
+cudaError_t configure_logits();
+cudaError_t launch_adjust_logits(const LogitsArgs& a, int dtype, int out_dtype, cudaStream_t st);
+// cache_pages.cu
+cudaError_t configure_cache_pages();
+cudaError_t launch_fork(const PoolArgs& p, const int32_t* parents, const int32_t* children, int n, cudaStream_t st);
+cudaError_t launch_free(const PoolArgs& p, const int32_t* seqs, const int32_t* keep_lens, int n, cudaStream_t st);
+cudaError_t launch_extend(const PoolArgs& p, const int32_t* new_rows, int32_t* pairs, cudaStream_t st);
+cudaError_t launch_compact(const PoolArgs& p, int32_t* table_out, int32_t* refs_out, int32_t* page_map, int32_t* pairs,
+                           int32_t* num_pairs, cudaStream_t st);
+cudaError_t launch_copy_pages(const CopyArgs& a, cudaStream_t st);
 }  // namespace hook_attn
 
 using namespace hook_attn;
@@ -87,6 +101,21 @@ int check_handle(const hook_attn_handle* handle)
     int current = -1;
     if (cudaGetDevice(&current) != cudaSuccess) { (void)cudaGetLastError(); return HOOK_ATTN_ERR_CUDA; }
     return current == handle->device ? HOOK_ATTN_OK : HOOK_ATTN_ERR_INVALID_ARG;
+}
+
+bool dtype_ok(int dtype) { return dtype == HOOK_DTYPE_BF16 || dtype == HOOK_DTYPE_F16 || dtype == HOOK_DTYPE_F32; }
+
+int64_t min64(int64_t x, int64_t y) { return x < y ? x : y; }
+
+int prepare_pool(const hook_cache_pool* p, PoolArgs& a)
+{
+    if (!p || p->num_seqs < 0 || p->max_blocks_per_seq < 0 || p->num_blocks < 0 || p->page_size <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->page_size != kPage || p->num_seqs > kMaxPoolSeqs) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->num_seqs > 0 && (!p->seq_lens || (p->max_blocks_per_seq > 0 && !p->block_table))) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->num_blocks > 0 && !p->page_refs) return HOOK_ATTN_ERR_INVALID_ARG;
+    a.block_table = p->block_table; a.seq_lens = p->seq_lens; a.page_refs = p->page_refs; a.status = p->status;
+    a.num_seqs = p->num_seqs; a.max_blocks = p->max_blocks_per_seq; a.num_blocks = p->num_blocks;
+    return HOOK_ATTN_OK;
 }
 
 // Fills the kernel arguments; returns a HOOK_ATTN_* code.
@@ -163,6 +192,8 @@ int hook_attn_create(hook_attn_handle** handle, int device)
     if (e == cudaSuccess) e = configure_prefill_mma();
     if (e == cudaSuccess) e = configure_prefill_tc();
     if (e == cudaSuccess) e = configure_mixed();
+    if (e == cudaSuccess) e = configure_logits();
+    if (e == cudaSuccess) e = configure_cache_pages();
     cudaSetDevice(prev);
     if (e != cudaSuccess) return HOOK_ATTN_ERR_CUDA;
     hook_attn_handle* h = new hook_attn_handle;
@@ -372,6 +403,194 @@ int hook_capture_qk(hook_attn_handle* handle, const hook_attn_params* p, int is_
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
 }
 
+int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* cuda_stream)
+{
+    if (!p || p->num_seqs < 0 || p->total_q < 0 || p->num_q_heads <= 0 || p->num_kv_heads <= 0 || p->head_dim <= 0 ||
+        p->page_size <= 0 || p->num_blocks < 0 || p->max_blocks_per_seq < 0)
+        return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->num_q_heads % p->num_kv_heads != 0 || !dtype_ok(p->dtype) || !isfinite(p->factor)) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->axis_order != HOOK_ROPE_AXES_BLOCKED && p->axis_order != HOOK_ROPE_AXES_CYCLIC) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->pairing != HOOK_ROPE_PAIR_HALVES && p->pairing != HOOK_ROPE_PAIR_ADJACENT) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->rotary_dim < 0 || p->rotary_dim > p->head_dim || (p->rotary_dim & 1)) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->num_axes < 1 || p->num_axes > HOOK_ROPE_MAX_AXES) return HOOK_ATTN_ERR_INVALID_ARG;
+    const int pairs = p->rotary_dim / 2;
+    int left[HOOK_ROPE_MAX_AXES], sum = 0;
+    for (int i = 0; i < p->num_axes; ++i) {
+        left[i] = p->axis_pairs[i];
+        if (left[i] < 0 || left[i] > pairs) return HOOK_ATTN_ERR_INVALID_ARG;
+        sum += left[i];
+    }
+    if (sum != pairs) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (!p->cu_q_lens && p->total_q != p->num_seqs) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->head_dim != 64 && p->head_dim != 128) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->page_size != kPage || p->num_q_heads > kMaxHeads || p->num_seqs > 65535) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->num_seqs > 0 && p->total_q > 0) {
+        if (!p->q || !p->k || !p->v || !p->q_out || !p->k_cache || !p->v_cache || !p->block_table || !p->seq_lens)
+            return HOOK_ATTN_ERR_INVALID_ARG;
+        if (pairs > 0 && !p->inv_freq) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->kv_block_stride <= 0 || p->kv_token_stride <= 0 || p->kv_head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
+        if ((p->kv_block_stride | p->kv_token_stride | p->kv_head_stride) & 7) return HOOK_ATTN_ERR_UNSUPPORTED;
+        if (!aligned16(p->q_out) || !aligned16(p->k_cache) || !aligned16(p->v_cache)) return HOOK_ATTN_ERR_UNSUPPORTED;
+        const uintptr_t size = p->dtype == HOOK_DTYPE_F32 ? 4 : 2;
+        if ((reinterpret_cast<uintptr_t>(p->q) | reinterpret_cast<uintptr_t>(p->k) | reinterpret_cast<uintptr_t>(p->v)) & (size - 1))
+            return HOOK_ATTN_ERR_UNSUPPORTED;
+        const int64_t D = p->head_dim;
+        if (p->q == p->q_out && (p->dtype != HOOK_DTYPE_BF16 || p->q_head_stride != D || p->q_row_stride != D * p->num_q_heads))
+            return HOOK_ATTN_ERR_INVALID_ARG;       // in place only where every element stays where it is
+    }
+    int rc = check_handle(handle);
+    if (rc != HOOK_ATTN_OK || p->num_seqs == 0 || p->total_q == 0) return rc;
+
+    RopeArgs a;
+    memset(&a, 0, sizeof a);
+    a.q = p->q; a.k = p->k; a.v = p->v;
+    a.q_row = p->q_row_stride; a.q_head = p->q_head_stride;
+    a.k_row = p->k_row_stride; a.k_head = p->k_head_stride;
+    a.v_row = p->v_row_stride; a.v_head = p->v_head_stride;
+    a.q_out = static_cast<__nv_bfloat16*>(p->q_out);
+    a.k_cache = static_cast<__nv_bfloat16*>(p->k_cache);
+    a.v_cache = static_cast<__nv_bfloat16*>(p->v_cache);
+    a.bs = p->kv_block_stride; a.ts = p->kv_token_stride; a.hs = p->kv_head_stride;
+    a.block_table = p->block_table; a.seq_lens = p->seq_lens; a.cu_q_lens = p->cu_q_lens;
+    a.positions = p->positions; a.axis_stride = p->position_axis_stride;
+    a.inv_freq = p->inv_freq;
+    a.status = p->status;
+    a.num_seqs = p->num_seqs; a.total_q = p->total_q; a.Hq = p->num_q_heads; a.Hkv = p->num_kv_heads;
+    a.head_dim = p->head_dim; a.pairs = pairs; a.num_blocks = p->num_blocks; a.max_blocks = p->max_blocks_per_seq;
+    a.max_keys = (int32_t)min64((int64_t)p->max_blocks_per_seq * kPage, INT32_MAX);
+    a.factor = p->factor;
+    a.halves = p->pairing == HOOK_ROPE_PAIR_HALVES;
+    for (int pair = 0, axis = 0; pair < pairs; ++pair) {
+        while (left[axis] == 0) axis = (axis + 1) % p->num_axes;
+        a.axis_of_pair[pair] = (uint8_t)axis;
+        --left[axis];
+        if (p->axis_order == HOOK_ROPE_AXES_CYCLIC) axis = (axis + 1) % p->num_axes;
+    }
+    cudaError_t e = launch_rope_append(a, p->dtype, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, void* cuda_stream)
+{
+    if (!p || p->num_rows < 0 || p->vocab_size <= 0 || p->max_tokens < 0 || p->num_bias < 0 || p->num_masks < 0)
+        return HOOK_ATTN_ERR_INVALID_ARG;
+    if (!dtype_ok(p->dtype) || !dtype_ok(p->out_dtype)) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->out_dtype != p->dtype && p->out_dtype != HOOK_DTYPE_F32) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->vocab_size > kMaxVocab || p->num_rows > 65535) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->num_rows > 0) {
+        if (!p->logits || !p->out || p->logits_row_stride < p->vocab_size || p->out_row_stride < p->vocab_size)
+            return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->tokens && (!p->prompt_lens || !p->total_lens || p->tokens_row_stride < p->max_tokens)) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->bias_offsets && p->num_bias > 0 && (!p->bias_tokens || !p->bias_values)) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->mask && p->mask_row_stride < (p->vocab_size + 31) / 32) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->mask && !p->mask_rows && p->num_masks < p->num_rows) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->logits == p->out && (p->dtype != p->out_dtype || p->logits_row_stride != p->out_row_stride))
+            return HOOK_ATTN_ERR_INVALID_ARG;
+        const uintptr_t in = p->dtype == HOOK_DTYPE_F32 ? 3 : 1, out = p->out_dtype == HOOK_DTYPE_F32 ? 3 : 1;
+        if ((reinterpret_cast<uintptr_t>(p->logits) & in) || (reinterpret_cast<uintptr_t>(p->out) & out)) return HOOK_ATTN_ERR_UNSUPPORTED;
+    }
+    int rc = check_handle(handle);
+    if (rc != HOOK_ATTN_OK || p->num_rows == 0) return rc;
+
+    LogitsArgs a;
+    memset(&a, 0, sizeof a);
+    a.logits = p->logits; a.out = p->out;
+    a.in_row = p->logits_row_stride; a.out_row = p->out_row_stride;
+    a.tokens = p->tokens; a.token_row = p->tokens_row_stride;
+    a.prompt_lens = p->prompt_lens; a.total_lens = p->total_lens;
+    a.repetition = p->repetition; a.presence = p->presence; a.frequency = p->frequency;
+    a.bias_offsets = p->num_bias > 0 ? p->bias_offsets : nullptr;
+    a.bias_tokens = p->bias_tokens; a.bias_values = p->bias_values;
+    a.mask = p->mask; a.mask_row = p->mask_row_stride; a.mask_rows = p->mask_rows;
+    a.status = p->status;
+    a.rows = p->num_rows; a.vocab = p->vocab_size; a.max_tokens = p->max_tokens; a.num_bias = p->num_bias; a.num_masks = p->num_masks;
+    cudaError_t e = launch_adjust_logits(a, p->dtype, p->out_dtype, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_cache_fork(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* parents, const int32_t* children,
+                    int32_t num_forks, void* cuda_stream)
+{
+    PoolArgs a;
+    int rc = prepare_pool(pool, a);
+    if (rc != HOOK_ATTN_OK) return rc;
+    if (num_forks < 0 || (num_forks > 0 && (!parents || !children))) return HOOK_ATTN_ERR_INVALID_ARG;
+    if ((rc = check_handle(handle)) != HOOK_ATTN_OK || num_forks == 0) return rc;
+    cudaError_t e = launch_fork(a, parents, children, num_forks, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_cache_extend(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* new_rows, int32_t* pairs, void* cuda_stream)
+{
+    PoolArgs a;
+    int rc = prepare_pool(pool, a);
+    if (rc != HOOK_ATTN_OK) return rc;
+    if (a.num_seqs > 0 && (!new_rows || !pairs)) return HOOK_ATTN_ERR_INVALID_ARG;
+    if ((rc = check_handle(handle)) != HOOK_ATTN_OK || a.num_seqs == 0) return rc;
+    cudaError_t e = launch_extend(a, new_rows, pairs, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_cache_free(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* seqs, const int32_t* keep_lens,
+                    int32_t num_entries, void* cuda_stream)
+{
+    PoolArgs a;
+    int rc = prepare_pool(pool, a);
+    if (rc != HOOK_ATTN_OK) return rc;
+    if (num_entries < 0 || (num_entries > 0 && !seqs)) return HOOK_ATTN_ERR_INVALID_ARG;
+    if ((rc = check_handle(handle)) != HOOK_ATTN_OK || num_entries == 0) return rc;
+    cudaError_t e = launch_free(a, seqs, keep_lens, num_entries, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_cache_compact(hook_attn_handle* handle, const hook_cache_pool* pool, int32_t* block_table_out, int32_t* page_refs_out,
+                       int32_t* page_map, int32_t* pairs, int32_t* num_pairs, void* cuda_stream)
+{
+    PoolArgs a;
+    int rc = prepare_pool(pool, a);
+    if (rc != HOOK_ATTN_OK) return rc;
+    if ((a.num_seqs > 0 && a.max_blocks > 0 && !block_table_out) || (a.num_blocks > 0 && (!page_refs_out || !page_map)) ||
+        (a.num_blocks > 1 && !pairs) || !num_pairs || (a.num_blocks > 0 && page_refs_out == pool->page_refs))
+        return HOOK_ATTN_ERR_INVALID_ARG;
+    if ((rc = check_handle(handle)) != HOOK_ATTN_OK) return rc;
+    cudaError_t e = launch_compact(a, block_table_out, page_refs_out, page_map, pairs, num_pairs, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params* p, void* cuda_stream)
+{
+    if (!p || p->num_layers < 0 || p->num_blocks < 0 || p->page_size <= 0 || p->num_kv_heads <= 0 || p->head_dim <= 0 || p->max_pairs < 0)
+        return HOOK_ATTN_ERR_INVALID_ARG;
+    if ((p->head_dim != 64 && p->head_dim != 128) || p->page_size != kPage || p->num_kv_heads > kMaxHeads) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->num_layers > 0 && p->max_pairs > 0) {
+        if (!p->k_caches || !p->v_caches || !p->pairs) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->kv_block_stride <= 0 || p->kv_token_stride <= 0 || p->kv_head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
+        if ((p->kv_block_stride | p->kv_token_stride | p->kv_head_stride) & 7) return HOOK_ATTN_ERR_UNSUPPORTED;
+        for (int l = 0; l < p->num_layers; ++l) {
+            if (!p->k_caches[l] || !p->v_caches[l]) return HOOK_ATTN_ERR_INVALID_ARG;
+            if (!aligned16(p->k_caches[l]) || !aligned16(p->v_caches[l])) return HOOK_ATTN_ERR_UNSUPPORTED;
+        }
+    }
+    int rc = check_handle(handle);
+    if (rc != HOOK_ATTN_OK) return rc;
+    if (p->num_layers == 0 || p->max_pairs == 0) return HOOK_ATTN_OK;
+    CopyArgs a;
+    memset(&a, 0, sizeof a);
+    a.bs = p->kv_block_stride; a.ts = p->kv_token_stride; a.hs = p->kv_head_stride;
+    a.pairs = p->pairs; a.num_pairs = p->num_pairs;
+    a.status = p->status;
+    a.num_blocks = p->num_blocks; a.Hkv = p->num_kv_heads; a.head_dim = p->head_dim; a.max_pairs = p->max_pairs;
+    for (int l0 = 0; l0 < p->num_layers; l0 += kCopyLayers) {
+        a.layers = p->num_layers - l0 < kCopyLayers ? p->num_layers - l0 : kCopyLayers;
+        for (int l = 0; l < a.layers; ++l) {
+            a.k[l] = static_cast<__nv_bfloat16*>(p->k_caches[l0 + l]);
+            a.v[l] = static_cast<__nv_bfloat16*>(p->v_caches[l0 + l]);
+        }
+        if (launch_copy_pages(a, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return HOOK_ATTN_ERR_CUDA;
+    }
+    return HOOK_ATTN_OK;
+}
+
 int hook_attn_selftest_wait_limit(hook_attn_handle* handle, int32_t* status, uint64_t limit_ns, uint64_t* waited_ns,
                                   void* cuda_stream)
 {
@@ -392,6 +611,7 @@ const char* hook_attn_strerror(int code)
         case HOOK_ATTN_ERR_CUDA: return "CUDA call failed";
         case HOOK_ATTN_ERR_TIMEOUT: return "bounded wait ran out on the device";
         case HOOK_ATTN_ERR_BOUNDS: return "block id or sequence length out of range";
+        case HOOK_ATTN_ERR_NO_PAGES: return "no free page left in the pool";
         default: return "unknown code";
     }
 }

@@ -1,0 +1,230 @@
+"""Penalties, biases and grammar masks on logits: oracle pins, refusals (CPU) and GPU parity."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops
+from paper_2603_06588_b200 import binding
+
+from ._ops import FAKE_HANDLE, no_device, struct_fields
+
+# Relative to the sum of the magnitudes of a value's terms: the division, the product with the count, the two subtractions and the
+# addition of the bias are each rounded to 24 bits: 5 x 2^-24 < 2^-21.
+ARITHMETIC = 2.0 ** -21
+SMALLEST = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25, torch.float32: 0.0}    # half a step of the numbers next to zero
+
+
+# --------------------------------------------------------------------------------------------------- CPU
+def test_struct_mirror():
+    assert struct_fields("hook_logits_params") == [f[0] for f in binding.HookLogitsParams._fields_]
+
+
+def test_oracle_closed_forms():
+    x = np.array([[2.0, -2.0, 1.0, 0.5, 3.0]])
+    out, _ = ops.adjust_logits(x, tokens=[[0, 1, 4, 4, -1, 7]], prompt_lens=[1], total_lens=[6], repetition=[2.0], presence=[0.25], frequency=[0.5],
+                               bias=[[(3, 1.0), (3, 2.0), (9, 5.0)]], mask=np.array([[1, 1, 0, 1, 1]], dtype=bool))
+    assert out[0].tolist() == [1.0, -4.0 - 0.75, -np.inf, 2.5, 1.5 - 1.25]
+    same, _ = ops.adjust_logits(x, mask=np.zeros((1, 5), dtype=bool), mask_rows=[-1])
+    assert np.array_equal(same, x)
+
+
+def _params(**over):
+    p = binding.HookLogitsParams()
+    p.num_rows, p.vocab_size, p.max_tokens, p.num_bias, p.num_masks = 2, 1000, 64, 4, 2
+    p.logits, p.out, p.logits_row_stride, p.out_row_stride = 0x10000, 0x20000, 1000, 1000
+    p.tokens = p.prompt_lens = p.total_lens = p.bias_offsets = p.bias_tokens = p.bias_values = p.mask = 0x30000
+    p.tokens_row_stride, p.mask_row_stride = 64, 32
+    for k, v in over.items():
+        setattr(p, k, v)
+    return p
+
+
+@no_device
+@pytest.mark.parametrize("over,code", [
+    (dict(), binding.HOOK_ATTN_ERR_CUDA),
+    (dict(out=0x10000), binding.HOOK_ATTN_ERR_CUDA),
+    (dict(tokens=None, prompt_lens=None, total_lens=None), binding.HOOK_ATTN_ERR_CUDA),
+    (dict(num_rows=-1), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(vocab_size=0), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(dtype=7), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(logits=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(out_row_stride=999), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(prompt_lens=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(tokens_row_stride=63), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(bias_values=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(mask_row_stride=31), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(num_masks=1), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(out=0x10000, out_dtype=binding.HOOK_DTYPE_F32), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(out=0x10000, out_row_stride=1008), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(out_dtype=binding.HOOK_DTYPE_F16), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(vocab_size=(1 << 20) + 1, logits_row_stride=1 << 21, out_row_stride=1 << 21, mask_row_stride=1 << 16), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(num_rows=65536), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(logits=0x10001), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(out=0x20002, dtype=binding.HOOK_DTYPE_F32, out_dtype=binding.HOOK_DTYPE_F32), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+])
+def test_refusals(over, code):
+    assert binding.load_library().hook_adjust_logits(FAKE_HANDLE, ctypes.byref(_params(**over)), None) == code
+
+
+# --------------------------------------------------------------------------------------------------- GPU
+@pytest.fixture(scope="module")
+def eng():
+    return binding.HookAttn(0)
+
+
+def _bits(mask):
+    """Boolean ``[masks, vocab]`` as int32 words, lowest bit first."""
+    words = -(-mask.shape[1] // 32)
+    padded = np.zeros((mask.shape[0], words * 32), dtype=np.uint8)
+    padded[:, :mask.shape[1]] = mask
+    return torch.from_numpy(np.packbits(padded, axis=1, bitorder="little").view(np.int32).copy())
+
+
+def _check(eng, x, out_dtype=None, tokens=None, prompt=None, total=None, rep=None, pres=None, freq=None, bias=None, mask=None, mask_rows=None,
+           in_place=False, pad=0, out_pad=0, expect_status=0, untouched=()):
+    rows, vocab = x.shape
+    out_dtype = out_dtype or x.dtype
+    i32 = lambda a: None if a is None else torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+    f32 = lambda a: None if a is None else torch.tensor(a, dtype=torch.float32, device="cuda")
+    wide = torch.full((rows, vocab + pad), 3.0, dtype=x.dtype, device="cuda")
+    wide[:, :vocab] = x.cuda()
+    logits = wide[:, :vocab]
+    out_wide = wide if in_place else torch.full((rows, vocab + out_pad), 3.0, dtype=out_dtype, device="cuda")
+    out = out_wide[:, :vocab]
+    kw = {}
+    if bias is not None:
+        kw = dict(bias_offsets=i32(np.cumsum([0] + [len(b) for b in bias])), bias_tokens=i32([t for b in bias for t, _ in b] or np.zeros(0)),
+                  bias_values=f32([v for b in bias for _, v in b]))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = eng.hook_adjust_logits(logits, out=None if in_place else out, tokens=i32(tokens), prompt_lens=i32(prompt), total_lens=i32(total),
+                                 repetition=f32(rep), presence=f32(pres), frequency=f32(freq), mask=None if mask is None else _bits(mask).cuda(),
+                                 mask_rows=i32(mask_rows), status=status, **kw)
+    torch.cuda.synchronize()
+    assert int(status.item()) == expect_status and got.data_ptr() == out.data_ptr()
+    r32 = lambda a: None if a is None else np.asarray(a, dtype=np.float32).astype(np.float64)
+    live = [r for r in range(rows) if r not in untouched]
+    pick = lambda a: None if a is None else [a[r] for r in live]
+    bias32 = None if bias is None else [[(t, float(np.float32(v))) for t, v in bias[r]] for r in live]
+    if mask is not None and mask_rows is None:
+        mask_rows = list(range(rows))
+    want, scale = ops.adjust_logits(x.double().numpy()[live], tokens=pick(tokens), prompt_lens=pick(prompt), total_lens=pick(total),
+                                    repetition=pick(r32(rep)), presence=pick(r32(pres)), frequency=pick(r32(freq)), bias=bias32, mask=mask,
+                                    mask_rows=pick(mask_rows))
+    top = torch.finfo(out_dtype)
+    want[np.abs(want) >= top.max * (1 + top.eps / 4)] *= np.inf          # rounded to out's type, these are infinite
+    res = out.double().cpu().numpy()
+    for r in untouched:
+        assert np.array_equal(res[r], np.full(vocab, 3.0) if not in_place else x[r].double().numpy())
+    res = res[live]
+    fine = np.isfinite(want)
+    assert np.array_equal(res[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]) and np.array_equal(np.isnan(res), np.isnan(want))
+    tol = np.abs(want) * (torch.finfo(out_dtype).eps / 2) + scale * ARITHMETIC + SMALLEST[out_dtype]
+    assert np.all(np.abs(res[fine] - want[fine]) <= tol[fine])
+    if out_wide.shape[1] > vocab:
+        assert (out_wide[:, vocab:] == 3.0).all()
+    return got
+
+
+def _random(rows, vocab, dtype, hist, seed, bias=0):
+    g = np.random.default_rng(seed)
+    x = torch.from_numpy(g.normal(size=(rows, vocab)) * 3).to(dtype)
+    tokens = (g.random((rows, max(1, hist))) ** 3 * vocab).astype(np.int64)
+    total = g.integers(0, hist + 1, rows)
+    prompt = (total * g.random(rows)).astype(np.int64)
+    b = [[(int(t), float(v)) for t, v in zip(g.integers(0, vocab, g.integers(0, bias + 1)), g.normal(size=bias) * 4)] for _ in range(rows)] if bias else None
+    return g, x, dict(tokens=tokens, prompt=prompt, total=total, rep=1 + g.random(rows), pres=g.random(rows), freq=g.random(rows), bias=b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [(torch.bfloat16, None), (torch.bfloat16, torch.float32), (torch.float16, None), (torch.float16, torch.float32),
+                                       (torch.float32, None)])
+@pytest.mark.parametrize("vocab", [1, 31, 33, 1000, 8192, 20011])
+def test_everything_on(eng, dtype, out, vocab):
+    """Odd vocabularies make every row start at another alignment; history with repeats; biases with tokens named twice."""
+    g, x, kw = _random(5, vocab, dtype, 300, vocab, bias=40)
+    mask = g.random((3, vocab)) < 0.7
+    _check(eng, x, out, mask=mask, mask_rows=[2, -1, 0, 2, 1], **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hist", [1, 255, 4097, 50000])
+def test_long_histories(eng, hist):
+    _, x, kw = _random(3, 50021, torch.bfloat16, hist, hist)
+    kw["total"][0], kw["prompt"][0] = hist, 0
+    _check(eng, x, torch.float32, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 2, 150, 600])
+def test_many_rows(eng, rows):
+    g, x, kw = _random(rows, 3001, torch.float32, 64, rows, bias=3)
+    _check(eng, x, mask=g.random((rows, 3001)) < 0.5, **kw)
+
+
+@pytest.mark.gpu
+def test_large_vocabulary(eng):
+    g, x, kw = _random(2, (1 << 20) - 3, torch.bfloat16, 2000, 5, bias=500)
+    _check(eng, x, torch.float32, mask=g.random((2, x.shape[1])) < 0.5, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pad,out_pad", [(0, 0), (24, 0), (5, 3), (1, 0), (0, 8)])
+@pytest.mark.parametrize("dtype,out", [(torch.bfloat16, torch.float32), (torch.float32, None), (torch.float16, None)])
+def test_strided_rows(eng, pad, out_pad, dtype, out):
+    g, x, kw = _random(4, 1021, dtype, 100, 11, bias=5)
+    _check(eng, x, out, mask=g.random((4, 1021)) < 0.5, pad=pad, out_pad=out_pad, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_in_place(eng, dtype):
+    g, x, kw = _random(4, 9001, dtype, 100, 12, bias=5)
+    _check(eng, x, mask=g.random((4, 9001)) < 0.5, in_place=True, pad=7, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("only", ["rep", "pres", "freq", "bias", "mask", "nothing", "tokens"])
+def test_one_edit_at_a_time(eng, only):
+    g, x, kw = _random(3, 777, torch.float32, 100, 13, bias=9)
+    history = {k: kw[k] for k in ("tokens", "prompt", "total")}
+    args = {"bias": dict(bias=kw["bias"]), "mask": dict(mask=g.random((3, 777)) < 0.5), "nothing": {}, "tokens": history}
+    _check(eng, x, **args.get(only) or dict(history, **({only: kw[only]} if only in kw else {})))
+
+
+@pytest.mark.gpu
+def test_masks_that_leave_nothing_infinities_and_nan(eng):
+    x = torch.zeros(3, 40)
+    x[0, :4] = torch.tensor([float("inf"), float("-inf"), float("nan"), torch.finfo(torch.float32).min])
+    x[1] = x[0]
+    x[2] = float("nan")
+    mask = np.ones((2, 40), dtype=bool)
+    mask[1] = False
+    tokens = [[0, 1, 3, 3]] * 3
+    _check(eng, x, tokens=tokens, prompt=[1] * 3, total=[4] * 3, freq=[0.5] * 3, rep=[1.25] * 3, mask=mask, mask_rows=[0, 1, 1])
+
+
+@pytest.mark.gpu
+def test_tokens_and_biases_outside_the_vocabulary(eng):
+    x = torch.randn(2, 50, generator=torch.Generator().manual_seed(1))
+    tokens = [[-1, 50, 2 ** 31 - 1, -2 ** 31, 7], [50, 51, 52, 53, 54]]
+    _check(eng, x, tokens=tokens, prompt=[0, 2], total=[5, 5], freq=[0.5, 0.5], rep=[2.0, 2.0])
+    _check(eng, x, bias=[[(3, 1.0), (-1, 9.0)], [(50, 2.0), (49, 1.0)]], expect_status=binding.HOOK_ATTN_ERR_BOUNDS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("over", [dict(total=[5, 9]), dict(total=[5, -1]), dict(prompt=[0, 6]), dict(prompt=[0, -1]), dict(mask_rows=[0, 2])])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_broken_rows_are_left_alone(eng, over, in_place):
+    x = torch.randn(2, 50, generator=torch.Generator().manual_seed(1))
+    kw = dict(tokens=[[1, 2, 3, 4, 5, 6, 7, 8]] * 2, prompt=[0, 0], total=[5, 5], freq=[0.5, 0.5], mask=np.arange(100).reshape(2, 50) % 3 > 0, mask_rows=[1, 0])
+    _check(eng, x, expect_status=binding.HOOK_ATTN_ERR_BOUNDS, untouched=(1,), in_place=in_place, **dict(kw, **over))
+
+
+@pytest.mark.gpu
+def test_same_bits_every_time(eng):
+    g, x, kw = _random(7, 20011, torch.bfloat16, 3000, 21, bias=60)
+    first = _check(eng, x, torch.float32, **kw).clone()
+    for _ in range(3):
+        assert torch.equal(_check(eng, x, torch.float32, **kw), first)

@@ -1,0 +1,332 @@
+"""Pages of the cache: fork, extend, free, compact, copy.  Oracle pins, refusals (CPU) and GPU parity, to the last integer."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops
+from paper_2603_06588_b200 import binding
+
+from ._ops import FAKE_HANDLE, no_device, struct_fields
+
+
+# --------------------------------------------------------------------------------------------------- CPU
+@pytest.mark.parametrize("name,cls", [("hook_cache_pool", binding.HookCachePool), ("hook_cache_copy_params", binding.HookCacheCopyParams)])
+def test_struct_mirror(name, cls):
+    assert struct_fields(name) == [f[0] for f in cls._fields_]
+
+
+def _consistent(pool):
+    """Every page counts the table entries that name it."""
+    refs = [0] * len(pool.refs)
+    for row, L in zip(pool.table, pool.lens):
+        held = row[:-(-L // 16)]
+        assert all(p >= 0 for p in held) and all(p == -1 for p in row[len(held):])
+        for p in held:
+            refs[p] += 1
+    assert refs == pool.refs
+
+
+def test_oracle_life_cycle():
+    pool = ops.Pool(4, 6, 12)
+    assert pool.extend([20, 0, 0, 0]) == [(-1, -1)] * 4
+    assert pool.table[0][:2] == [0, 1] and pool.refs[:3] == [1, 1, 0]
+    pool.fork([0, 0], [1, 2])
+    assert pool.refs[:2] == [3, 3] and pool.lens == [20, 20, 20, 0]
+    pairs = pool.extend([0, 1, 13, 0])                           # both leave the shared page; the second needs another one too
+    assert pairs == [(-1, -1), (1, 2), (1, 3), (-1, -1)]
+    assert pool.table[1][:2] == [0, 2] and pool.table[2][:3] == [0, 3, 4] and pool.refs[:5] == [3, 1, 1, 1, 1]
+    _consistent(pool)
+    pool.free([0, 0, 2], [16, 0, 0])
+    assert pool.lens == [16, 21, 0, 0] and pool.refs[:5] == [2, 0, 1, 0, 0]
+    _consistent(pool)
+    table, refs, page_map, moves = pool.compact()
+    assert moves == [(2, 1)] and refs[:3] == [2, 1, 0] and table[1][:2] == [0, 1] and page_map[:3] == [0, -1, 1]
+    assert not pool.faults
+
+
+def test_oracle_copy():
+    cache = np.arange(6)
+    out, refused = ops.copy_pages(cache, [(0, 3), (0, 4), (-1, 2), (5, 5)])
+    assert out.tolist() == [0, 1, 2, 0, 0, 5] and not refused
+    assert ops.copy_pages(cache, [(0, 1), (1, 2)])[1] and ops.copy_pages(cache, [(0, 1), (2, 1)])[0].tolist() == cache.tolist()
+
+
+def _pool_params(**over):
+    p = binding.HookCachePool(4, 8, 64, 16, 0x10000, 0x20000, 0x30000, None)
+    for k, v in over.items():
+        setattr(p, k, v)
+    return p
+
+
+@no_device
+@pytest.mark.parametrize("over,code", [
+    (dict(), binding.HOOK_ATTN_ERR_CUDA), (dict(num_seqs=-1), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(block_table=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(seq_lens=None), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(page_refs=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(page_size=32), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(num_seqs=16385), binding.HOOK_ATTN_ERR_UNSUPPORTED)])
+def test_pool_refusals(over, code):
+    lib, p = binding.load_library(), ctypes.byref(_pool_params(**over))
+    assert lib.hook_cache_fork(FAKE_HANDLE, p, 0x1000, 0x1000, 1, None) == code
+    assert lib.hook_cache_extend(FAKE_HANDLE, p, 0x1000, 0x1000, None) == code
+    assert lib.hook_cache_free(FAKE_HANDLE, p, 0x1000, None, 1, None) == code
+    assert lib.hook_cache_compact(FAKE_HANDLE, p, 0x1000, 0x2000, 0x3000, 0x4000, 0x5000, None) == code
+
+
+@no_device
+def test_list_refusals():
+    lib, p, bad = binding.load_library(), ctypes.byref(_pool_params()), binding.HOOK_ATTN_ERR_INVALID_ARG
+    assert lib.hook_cache_fork(FAKE_HANDLE, p, None, 0x1000, 1, None) == bad
+    assert lib.hook_cache_fork(FAKE_HANDLE, p, 0x1000, 0x1000, -1, None) == bad
+    assert lib.hook_cache_extend(FAKE_HANDLE, p, 0x1000, None, None) == bad
+    assert lib.hook_cache_free(FAKE_HANDLE, p, None, None, 1, None) == bad
+    assert lib.hook_cache_compact(FAKE_HANDLE, p, 0x1000, 0x30000, 0x3000, 0x4000, 0x5000, None) == bad      # the counts in place
+    assert lib.hook_cache_compact(FAKE_HANDLE, p, 0x1000, 0x2000, 0x3000, 0x4000, None, None) == bad
+    assert lib.hook_cache_fork(FAKE_HANDLE, None, 0x1000, 0x1000, 1, None) == bad
+    assert lib.hook_cache_fork(None, p, 0x1000, 0x1000, 1, None) == bad
+
+
+@no_device
+@pytest.mark.parametrize("over,code", [
+    (dict(), binding.HOOK_ATTN_ERR_CUDA), (dict(num_layers=-1), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(pairs=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(k_caches=None), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(kv_block_stride=0), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(head_dim=80), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(page_size=8), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(kv_head_stride=132), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(address=0x10008), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(address=0), binding.HOOK_ATTN_ERR_INVALID_ARG)])
+def test_copy_refusals(over, code):
+    at = over.pop("address", 0x10000) if "address" in over else 0x10000
+    ptrs = (ctypes.c_void_p * 2)(0x10000, at)
+    p = binding.HookCacheCopyParams(2, 64, 16, 8, 128, 4, 16 * 1024, 1024, 128, ctypes.addressof(ptrs), ctypes.addressof(ptrs), 0x20000, None, None)
+    for k, v in over.items():
+        setattr(p, k, v)
+    assert binding.load_library().hook_cache_copy_pages(FAKE_HANDLE, ctypes.byref(p), None) == code
+
+
+# --------------------------------------------------------------------------------------------------- GPU
+@pytest.fixture(scope="module")
+def eng():
+    return binding.HookAttn(0)
+
+
+class Both:
+    """The same pool on the device and as the oracle's lists."""
+
+    def __init__(self, eng, num_seqs, max_blocks, num_blocks):
+        self.eng, self.want = eng, ops.Pool(num_seqs, max_blocks, num_blocks)
+        self.load()
+
+    def load(self):
+        t = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+        w = self.want
+        self.dev = dict(block_table=t(w.table).reshape(len(w.lens), w.max_blocks), seq_lens=t(w.lens), page_refs=t(w.refs),
+                        status=torch.zeros(1, dtype=torch.int32, device="cuda"))
+
+    def _i32(self, a):
+        return None if a is None else torch.tensor(a, dtype=torch.int32, device="cuda")
+
+    def compare(self):
+        torch.cuda.synchronize()
+        assert self.dev["seq_lens"].tolist() == self.want.lens
+        assert self.dev["page_refs"].tolist() == self.want.refs
+        assert self.dev["block_table"].tolist() == self.want.table
+        codes = {"bounds": binding.HOOK_ATTN_ERR_BOUNDS, "no pages": binding.HOOK_ATTN_ERR_NO_PAGES}
+        assert int(self.dev["status"].item()) == min([codes[f] for f in self.want.faults], default=0)
+        self.dev["status"].zero_()
+        self.want.faults = []
+
+    def fork(self, parents, children):
+        self.eng.hook_cache_fork(**self.dev, parents=self._i32(parents), children=self._i32(children))
+        self.want.fork(parents, children)
+        self.compare()
+
+    def extend(self, new_rows):
+        pairs = self.eng.hook_cache_extend(**self.dev, new_rows=self._i32(new_rows))
+        want = self.want.extend(new_rows)
+        self.compare()
+        assert [tuple(p) for p in pairs.tolist()] == want
+        return want
+
+    def free(self, seqs, keep=None):
+        self.eng.hook_cache_free(**self.dev, seqs=self._i32(seqs), keep_lens=self._i32(keep))
+        self.want.free(seqs, keep)
+        self.compare()
+
+    def compact(self, adopt=True):
+        table, refs, page_map, pairs, count = self.eng.hook_cache_compact(**self.dev)
+        want_table, want_refs, want_map, moves = self.want.compact()
+        self.compare()                                            # the pool itself has not changed
+        assert table.tolist() == want_table and refs.tolist() == want_refs and page_map.tolist() == want_map
+        assert count.tolist() == [len(moves)]
+        assert [tuple(p) for p in pairs.tolist()] == moves + [(-1, -1)] * (len(refs) // 2 - len(moves))
+        if adopt:
+            self.want.table, self.want.refs = want_table, want_refs
+            self.load()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(6))
+@pytest.mark.parametrize("num_seqs,max_blocks,num_blocks", [(1, 1, 1), (3, 4, 7), (40, 9, 150), (300, 40, 3000), (1100, 5, 2500)])
+def test_random_life(eng, seed, num_seqs, max_blocks, num_blocks):
+    g = np.random.default_rng(seed)
+    both = Both(eng, num_seqs, max_blocks, num_blocks)
+    for _ in range(8):
+        new = (g.integers(0, 40, num_seqs) * (g.random(num_seqs) < 0.6)).tolist()
+        both.extend(new)
+        n = int(g.integers(1, num_seqs + 1))
+        both.fork(g.integers(0, num_seqs, n).tolist(), g.integers(0, num_seqs, n).tolist())
+        both.extend((g.random(num_seqs) < 0.5).astype(int).tolist())
+        both.free(g.integers(0, num_seqs, n // 2).tolist(), g.integers(0, 60, n // 2).tolist() if g.random() < 0.5 else None)
+        if g.random() < 0.5:
+            both.compact()
+        _consistent(both.want)
+
+
+@pytest.mark.gpu
+def test_sharers_that_leave_a_page_together_give_it_back(eng):
+    both = Both(eng, 3, 4, 10)
+    both.extend([20, 0, 0])
+    both.fork([0, 0], [1, 2])
+    assert both.extend([1, 1, 1]) == [(1, 2), (1, 3), (1, 4)]
+    assert both.want.refs[1] == 0
+    assert both.extend([0, 0, 60 - 21]) == [(-1, -1)] * 3         # and it is taken again
+    assert 1 in both.want.table[2]
+
+
+@pytest.mark.gpu
+def test_pool_runs_out(eng):
+    both = Both(eng, 5, 8, 6)
+    both.extend([30, 40, 3, 17, 0])                               # 2 + 3 pages, then one, then none for the fourth
+    assert both.want.lens == [30, 40, 3, 0, 0]
+    both.extend([2, 8, 5, 1, 0])                                  # room in the pages that are there
+    both.extend([1, 0, 0, 0, 0])
+    assert both.want.lens == [32, 48, 8, 0, 0]
+
+
+@pytest.mark.gpu
+def test_exact_fit_and_full_rows(eng):
+    both = Both(eng, 2, 3, 6)
+    both.extend([48, 48])
+    both.extend([1, 0])                                           # beyond the table's row
+    both.free([1], [17])
+    both.extend([0, 31])
+    assert both.want.lens == [48, 48]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("break_it", ["length", "negative length", "table", "refs"])
+def test_broken_pools_are_reported(eng, break_it):
+    both = Both(eng, 4, 4, 20)
+    both.extend([20, 20, 20, 0])
+    if break_it == "length":
+        both.want.lens[1] = 65
+    elif break_it == "negative length":
+        both.want.lens[1] = -3
+    elif break_it == "table":
+        both.want.table[1][1] = 20
+    else:
+        both.want.refs[both.want.table[1][1]] = 0
+    both.load()
+    if break_it != "refs":
+        both.fork([1], [3])
+    both.extend([1, 1, 0, 0])
+    both.free([1, 7, -1])
+
+
+@pytest.mark.gpu
+def test_refused_forks(eng):
+    both = Both(eng, 6, 4, 30)
+    both.extend([20, 33, 0, 0, 0, 5])
+    both.fork([0, 1, 0, 2, 0, 9, 1], [2, 2, 5, 3, 0, 4, -1])      # named twice, not empty, a child as a parent, itself, rows that are not there
+    assert both.want.lens == [20, 33, 0, 0, 0, 5]                 # row 2 is a parent here: refused too
+    both.fork([0, 1], [2, 2])
+    assert both.want.lens[2] == 20
+    both.fork([4], [3])                                           # an empty parent
+    assert both.want.lens[3] == 0
+
+
+@pytest.mark.gpu
+def test_in_place_table_of_compact(eng):
+    both = Both(eng, 3, 4, 20)
+    both.extend([20, 40, 60])
+    both.free([1])
+    pool = ctypes.byref(binding.HookAttn._pool(**both.dev))
+    out = torch.empty(20 * 4, dtype=torch.int32, device="cuda")
+    refs, page_map, pairs, count = out[:20], out[20:40], out[40:60], out[60:61]
+    rc = eng._lib.hook_cache_compact(eng._h, pool, both.dev["block_table"].data_ptr(), refs.data_ptr(), page_map.data_ptr(), pairs.data_ptr(),
+                                     count.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    want_table, want_refs, _, _ = both.want.compact()
+    assert rc == 0 and both.dev["block_table"].tolist() == want_table and refs.tolist() == want_refs
+
+
+def _cache(layout, pages, hkv, d, layers, seed):
+    g = torch.Generator().manual_seed(seed)
+    shape = {"contiguous": (layers, 2, pages, 16, hkv, d), "interleaved": (layers, pages, 2, 16, hkv, d), "heads first": (layers, 2, pages, hkv, 16, d),
+             "padded": (layers, 2, pages, 16, hkv, d + 8)}[layout]
+    return torch.randint(-2 ** 15, 2 ** 15, shape, generator=g, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+
+
+def _layers(cache, layout, d):
+    out = []
+    for c in cache:
+        k, v = (c[:, 0], c[:, 1]) if layout == "interleaved" else (c[0], c[1])
+        if layout == "heads first":
+            k, v = k.transpose(1, 2), v.transpose(1, 2)
+        out.append((k[..., :d], v[..., :d]))
+    return out
+
+
+def _check_copy(eng, pairs, layout="contiguous", pages=40, hkv=3, d=64, layers=2, count=None, expect_status=0):
+    host = _cache(layout, pages, hkv, d, layers, 3)
+    dev, want = host.cuda(), host.clone()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    eng.hook_cache_copy_pages(_layers(dev, layout, d), torch.tensor(pairs, dtype=torch.int32, device="cuda").reshape(-1, 2),
+                              num_pairs=None if count is None else torch.tensor([count], dtype=torch.int32, device="cuda"), status=status)
+    torch.cuda.synchronize()
+    live = pairs if count is None else pairs[:max(0, count)]
+    for k, v in _layers(want, layout, d):
+        for t in (k, v):
+            t.copy_(torch.from_numpy(ops.copy_pages(t.contiguous().view(torch.int16).numpy(), live)[0]).view(torch.bfloat16))
+    assert torch.equal(dev.cpu().view(torch.int16), want.view(torch.int16))
+    assert int(status.item()) == expect_status
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["contiguous", "interleaved", "heads first", "padded"])
+@pytest.mark.parametrize("hkv,d,layers", [(1, 64, 1), (3, 64, 2), (8, 128, 3), (1, 128, 70)])
+def test_copy(eng, layout, hkv, d, layers):
+    _check_copy(eng, [(0, 20), (0, 21), (7, 39), (-1, -1), (5, -1), (-3, 6), (4, 4), (19, 22)], layout, hkv=hkv, d=d, layers=layers)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [0, 1, 3, 9, -2])
+def test_copy_counts_on_the_device(eng, count):
+    _check_copy(eng, [(0, 20), (1, 21), (2, 22), (3, 23)], count=count)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pairs", [[(0, 1), (2, 1)], [(0, 1), (1, 2)], [(0, 1), (1, 0)], [(0, 1), (0, 1), (3, 4)], [(0, 40)], [(40, 0)], [(5, 5), (0, 5)]])
+def test_dependent_pairs_are_refused(eng, pairs):
+    _check_copy(eng, pairs, expect_status=binding.HOOK_ATTN_ERR_BOUNDS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [300, 2000])
+def test_many_pairs(eng, n):
+    g = np.random.default_rng(n)
+    order = g.permutation(2 * n)
+    pairs = [(int(order[g.integers(0, n)]), int(order[n + i])) for i in range(n)]
+    _check_copy(eng, pairs, pages=2 * n, hkv=1, layers=1)
+    pairs[n // 2] = (pairs[n // 2][0], pairs[3][1])               # one destination twice: neither is carried out
+    _check_copy(eng, pairs, pages=2 * n, hkv=1, layers=1, expect_status=binding.HOOK_ATTN_ERR_BOUNDS)
+
+
+@pytest.mark.gpu
+def test_nothing_to_do(eng):
+    both = Both(eng, 2, 2, 4)
+    both.fork([], [])
+    both.free([])
+    both.extend([0, 0])
+    both.compact()
+    _check_copy(eng, [])
+    eng.hook_cache_copy_pages([], torch.zeros((1, 2), dtype=torch.int32, device="cuda"))

@@ -37,7 +37,7 @@ cudaError_t launch_steer_residual(__nv_bfloat16* hidden, const float* vec, float
 cudaError_t launch_capture(const KernelArgs& a, const HeadCfg& hc, int head_dim, bool decode, __nv_bfloat16* q_out,
                            __nv_bfloat16* k_out, const int32_t* cu_k, cudaStream_t st);
 // rope.cu
-cudaError_t launch_rope_append(const RopeArgs& a, int dtype, cudaStream_t st);
+cudaError_t launch_rope_append(RopeArgs& a, int dtype, int num_sms, cudaStream_t st);
 // logits.cu
 cudaError_t configure_logits();
 cudaError_t launch_adjust_logits(const LogitsArgs& a, int dtype, int out_dtype, cudaStream_t st);
@@ -466,7 +466,7 @@ int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* 
         --left[axis];
         if (p->axis_order == HOOK_ROPE_AXES_CYCLIC) axis = (axis + 1) % p->num_axes;
     }
-    cudaError_t e = launch_rope_append(a, p->dtype, static_cast<cudaStream_t>(cuda_stream));
+    cudaError_t e = launch_rope_append(a, p->dtype, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
 }
 

@@ -20,6 +20,7 @@ struct RopeArgs {
     int64_t axis_stride;
     int32_t* status;
     int32_t num_seqs, total_q, Hq, Hkv, head_dim, pairs, num_blocks, max_blocks, max_keys;
+    int32_t rows_per_cta;
     float factor;
     bool halves;
     uint8_t axis_of_pair[kMaxPairs];

@@ -14,57 +14,51 @@ namespace hook_attn {
 
 namespace {
 
-constexpr int kRopeThreads = 256;
-
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 
-// Where row `row` of the call goes.
-struct RowPlace {
-    int seq;       // num_seqs: the row lies behind the last sequence
-    int pos;       // its position in the sequence
-    int64_t slot;  // element offset of its slot in the cache (token and block part)
-    bool ok;
-};
+constexpr int kRopeThreads = 256;
+constexpr int kRopeRows = 8;       // rows per CTA at most: one warp looks each of them up
 
-// The whole CTA looks one row up: the sequence is the number of sequences that end at or before the row.
+// Where a row of the call goes.
+struct RowPlace {
+    int64_t slot;  // element offset of its slot in the cache (block and token part)
+    int pos;       // its position in the sequence
+    int state;     // kGood; kBroken: zero its queries; kBehind: behind the last sequence, leave it alone
+};
+enum { kGood = 0, kBroken = 1, kBehind = 2 };
+
+// A warp looks a row up: its sequence is the number of sequences that end at or before the row.
 __device__ __forceinline__ RowPlace find_row(const RopeArgs& a, int row)
 {
-    RowPlace r;
-    int lo = row, n = 1;
+    const int lane = threadIdx.x & 31;
+    RowPlace r = {0, 0, kBehind};
+    int seq = row, lo = row, n = 1;
+    if (row >= a.total_q) return r;
     if (a.cu_q_lens) {
-        int before = 0;
-        for (int base = 0; base < a.num_seqs; base += kRopeThreads) {
-            const int s = base + (int)threadIdx.x;
-            before += __syncthreads_count(s < a.num_seqs && a.cu_q_lens[s + 1] <= row);
-        }
-        r.seq = before;
-        if (before < a.num_seqs) {
-            lo = a.cu_q_lens[before];
-            n = a.cu_q_lens[before + 1] - lo;
-        }
-    } else {
-        r.seq = row;
+        seq = 0;
+#pragma unroll 4
+        for (int s = lane; s < a.num_seqs; s += 32) seq += a.cu_q_lens[s + 1] <= row;
+        seq = __reduce_add_sync(0xffffffffu, seq);
+        if (seq >= a.num_seqs) return r;
+        lo = a.cu_q_lens[seq];
+        n = a.cu_q_lens[seq + 1] - lo;
     }
-    r.ok = false;
-    r.pos = 0;
-    r.slot = 0;
-    if (r.seq >= a.num_seqs) return r;
-    const int L = a.seq_lens[r.seq], at = row - lo;
+    r.state = kBroken;
+    const int L = a.seq_lens[seq], at = row - lo;
     if (L <= 0 || L > a.max_keys || at < 0 || at >= n || n > L) return r;
     r.pos = L - n + at;
-    const int page = a.block_table[(int64_t)r.seq * a.max_blocks + r.pos / kPage];
+    const int page = a.block_table[(int64_t)seq * a.max_blocks + r.pos / kPage];
     if (page < 0 || page >= a.num_blocks) return r;
     r.slot = (int64_t)page * a.bs + (int64_t)(r.pos % kPage) * a.ts;
-    r.ok = true;
+    r.state = kGood;
     return r;
 }
 
-// Cosine and sine of one pair of one row, times the factor.
-__device__ __forceinline__ float2 turn_of(const RopeArgs& a, int row, int pos, int pair)
+// Cosine and sine of one pair at one position, times the factor.
+__device__ __forceinline__ float2 turn_of(const RopeArgs& a, int p, int pair)
 {
-    const int p = a.positions ? a.positions[(int64_t)a.axis_of_pair[pair] * a.axis_stride + row] : pos;
     double turns = (double)p * (double)a.inv_freq[pair] * 0.15915494309189535;   // 1 / (2 pi)
     turns -= rint(turns);
     float s, c;
@@ -72,68 +66,138 @@ __device__ __forceinline__ float2 turn_of(const RopeArgs& a, int row, int pos, i
     return make_float2(c * a.factor, s * a.factor);
 }
 
-// One CTA per row, one pair (or one element behind the rotated ones) per thread and step: any strides, any R.
-template <typename T>
-__global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_constant__ RopeArgs a)
+// V values in a row of memory: the widest accesses that V allows, then 32 bits each.
+template <typename T, int V>
+struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Pack {
+    T x[V];
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void load(float (&x)[V], const T* p)
 {
-    __shared__ float2 turn[kMaxPairs];
-    const int row = blockIdx.x, D = a.head_dim, half = a.pairs, items = D - half;
-    const RowPlace at = find_row(a, row);
-    if (at.seq >= a.num_seqs) return;                      // rows behind the last sequence stay as they are
-    __nv_bfloat16* qo = a.q_out + (int64_t)row * a.Hq * D;
-    if (!at.ok) {
-        for (int i = threadIdx.x; i < a.Hq * D; i += kRopeThreads) qo[i] = __float2bfloat16(0.f);
-        if (threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-        return;
+    const Pack<T, V> raw = *reinterpret_cast<const Pack<T, V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = to_f32(raw.x[i]);
+}
+
+template <int V>
+__device__ __forceinline__ void store(__nv_bfloat16* p, const float (&x)[V])
+{
+    Pack<__nv_bfloat16, V> raw;
+#pragma unroll
+    for (int i = 0; i < V; ++i) raw.x[i] = __float2bfloat16(x[i]);
+    *reinterpret_cast<Pack<__nv_bfloat16, V>*>(p) = raw;
+}
+
+// A CTA takes a few rows.  An item is two runs of V elements of one head: V pairs that turn, or 2 V elements that are only
+// moved; the thread that reads them writes them, so the queries may be rotated in place.  Bound by HBM: every element is read
+// once and written once, and a row's cosines and sines (R / 2 of them) are computed once for all its heads.
+template <typename T, int V>
+__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_constant__ RopeArgs a)
+{
+    __shared__ __align__(16) float2 turn[kRopeRows][kMaxPairs];
+    __shared__ RowPlace places[kRopeRows];
+    const int row0 = blockIdx.x * a.rows_per_cta, warp = threadIdx.x >> 5;
+    if (warp < a.rows_per_cta) {
+        const RowPlace r = find_row(a, row0 + warp);
+        if ((threadIdx.x & 31) == 0) {
+            places[warp] = r;
+            if (r.state == kBroken) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        }
     }
-    if ((int)threadIdx.x < half) turn[threadIdx.x] = turn_of(a, row, at.pos, threadIdx.x);
+    if (!a.positions) __syncthreads();             // the angles go by the places
+    for (int i = threadIdx.x; i < a.rows_per_cta * kMaxPairs; i += kRopeThreads) {
+        const int r = i / kMaxPairs, pair = i % kMaxPairs, row = row0 + r;
+        if (pair < a.pairs && row < a.total_q)
+            turn[r][pair] = turn_of(a, a.positions ? a.positions[a.axis_of_pair[pair] * a.axis_stride + row] : places[r].pos, pair);
+    }
     __syncthreads();
-    const int step = a.halves ? half : 1, mul = a.halves ? 1 : 2;
-    const int heads = a.Hq + 2 * a.Hkv;
-    for (int i = threadIdx.x; i < heads * items; i += kRopeThreads) {
-        int h = i / items;
-        const int j = i - h * items;
+
+    const int D = a.head_dim, heads = a.Hq + 2 * a.Hkv, per_head = D / (2 * V), turning = a.pairs / V;
+    const int total = a.rows_per_cta * heads * per_head, shift = 31 - __clz(per_head);   // head_dim is a power of two
+    for (int i = threadIdx.x; i < total; i += kRopeThreads) {
+        const int j = i & (per_head - 1), rh = i >> shift, r = rh / heads;
+        int h = rh - r * heads;
+        const int state = places[r].state;
+        if (state == kBehind || (state == kBroken && h >= a.Hq)) continue;
+        const int64_t row = row0 + r;
         const T* src;
         __nv_bfloat16* dst;
-        bool rotated = j < half;
+        bool turns = j < turning;
         if (h < a.Hq) {
-            src = static_cast<const T*>(a.q) + (int64_t)row * a.q_row + (int64_t)h * a.q_head;
-            dst = qo + h * D;
+            src = static_cast<const T*>(a.q) + row * a.q_row + h * a.q_head;
+            dst = a.q_out + (row * a.Hq + h) * D;
         } else if ((h -= a.Hq) < a.Hkv) {
-            src = static_cast<const T*>(a.k) + (int64_t)row * a.k_row + (int64_t)h * a.k_head;
-            dst = a.k_cache + at.slot + (int64_t)h * a.hs;
+            src = static_cast<const T*>(a.k) + row * a.k_row + h * a.k_head;
+            dst = a.k_cache + places[r].slot + h * a.hs;
         } else {
             h -= a.Hkv;
-            src = static_cast<const T*>(a.v) + (int64_t)row * a.v_row + (int64_t)h * a.v_head;
-            dst = a.v_cache + at.slot + (int64_t)h * a.hs;
-            if (rotated) {
-                const int e = j * mul;
-                dst[e] = __float2bfloat16(to_f32(src[e]));
-                dst[e + step] = __float2bfloat16(to_f32(src[e + step]));
-                continue;
+            src = static_cast<const T*>(a.v) + row * a.v_row + h * a.v_head;
+            dst = a.v_cache + places[r].slot + h * a.hs;
+            turns = false;
+        }
+        int e0 = j * 2 * V, e1 = e0 + V;
+        if (a.halves && j < turning) {             // v takes the same runs as k: which they are is of no account there
+            e0 = j * V;
+            e1 = a.pairs + j * V;
+        }
+        float x[V], y[V];
+        load(x, src + e0);
+        load(y, src + e1);
+        if (turns) {
+#pragma unroll
+            for (int m = 0; m < V; ++m) {
+                const float2 t = turn[r][j * V + m];
+                if (a.halves) {
+                    const float u = x[m], w = y[m];
+                    x[m] = u * t.x - w * t.y;
+                    y[m] = w * t.x + u * t.y;
+                } else if (V == 1) {
+                    const float u = x[0], w = y[0];
+                    x[0] = u * t.x - w * t.y;
+                    y[0] = w * t.x + u * t.y;
+                } else {                           // pair m: elements 2 m and 2 m + 1 of x, then of y
+                    float& u = m < V / 2 ? x[2 * m % V] : y[2 * m % V];
+                    float& w = m < V / 2 ? x[(2 * m + 1) % V] : y[(2 * m + 1) % V];
+                    const float u0 = u, w0 = w;
+                    u = u0 * t.x - w0 * t.y;
+                    w = w0 * t.x + u0 * t.y;
+                }
             }
         }
-        if (rotated) {
-            const int e = j * mul;
-            const float2 t = turn[j];
-            const float x = to_f32(src[e]), y = to_f32(src[e + step]);
-            dst[e] = __float2bfloat16(x * t.x - y * t.y);
-            dst[e + step] = __float2bfloat16(y * t.x + x * t.y);
-        } else {
-            const int e = j + half;
-            dst[e] = __float2bfloat16(to_f32(src[e]));
+        if (state == kBroken) {
+#pragma unroll
+            for (int m = 0; m < V; ++m) x[m] = y[m] = 0.f;
         }
+        store(dst + e0, x);
+        store(dst + e1, y);
     }
+}
+
+template <typename T>
+cudaError_t launch(RopeArgs& a, int num_sms, cudaStream_t st)
+{
+    // Several rows per CTA once every SM has eight CTAs of one row: fewer look-ups wait for memory one after the other.
+    a.rows_per_cta = a.total_q / (num_sms * 8);
+    a.rows_per_cta = a.rows_per_cta < 1 ? 1 : a.rows_per_cta > kRopeRows ? kRopeRows : a.rows_per_cta;
+    const int grid = (a.total_q + a.rows_per_cta - 1) / a.rows_per_cta;
+    // The widest run that divides the rotated half and the strides and on whose multiples the tensors start.
+    const int64_t strides = a.q_row | a.q_head | a.k_row | a.k_head | a.v_row | a.v_head | a.pairs;
+    const uintptr_t at = (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) / sizeof(T);
+    const bool by16 = ((reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & 15) == 0;
+    if (((strides & 7) == 0) && by16) rope_append_kernel<T, 8><<<grid, kRopeThreads, 0, st>>>(a);
+    else if (((strides | at) & 3) == 0) rope_append_kernel<T, 4><<<grid, kRopeThreads, 0, st>>>(a);
+    else rope_append_kernel<T, 1><<<grid, kRopeThreads, 0, st>>>(a);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_rope_append(const RopeArgs& a, int dtype, cudaStream_t st)
+cudaError_t launch_rope_append(RopeArgs& a, int dtype, int num_sms, cudaStream_t st)
 {
-    if (dtype == HOOK_DTYPE_BF16) rope_rows_kernel<__nv_bfloat16><<<a.total_q, kRopeThreads, 0, st>>>(a);
-    else if (dtype == HOOK_DTYPE_F16) rope_rows_kernel<__half><<<a.total_q, kRopeThreads, 0, st>>>(a);
-    else rope_rows_kernel<float><<<a.total_q, kRopeThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    if (dtype == HOOK_DTYPE_BF16) return launch<__nv_bfloat16>(a, num_sms, st);
+    if (dtype == HOOK_DTYPE_F16) return launch<__half>(a, num_sms, st);
+    return launch<float>(a, num_sms, st);
 }
 
 }  // namespace hook_attn

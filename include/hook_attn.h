@@ -299,7 +299,8 @@ typedef struct {
     const float*    repetition;  /* [num_rows], > 0; NULL: 1 */
     const float*    presence;    /* [num_rows]; NULL: 0 */
     const float*    frequency;   /* [num_rows]; NULL: 0 */
-    const int32_t*  bias_offsets;/* [num_rows + 1] prefix sums of the rows' bias entries; NULL: no biases */
+    const int32_t*  bias_offsets;/* [num_rows + 1] prefix sums of the rows' bias entries, at most 2047 a row;
+                                    NULL: no biases */
     const int32_t*  bias_tokens; /* [num_bias]; of a token named twice in a row the last entry counts */
     const float*    bias_values; /* [num_bias] */
     const uint32_t* mask;        /* [num_masks][ceil(vocab_size / 32)], bit v % 32 of word v / 32: token v is
@@ -314,7 +315,7 @@ typedef struct {
  *   x = seen ? (x > 0 ? x / repetition : x * repetition) : x;   x -= frequency * c + presence * (c > 0);
  *   x += bias[v];   x = -inf if the grammar forbids v (whatever x is; a mask may forbid all).
  * A row whose lengths, bias offsets or mask row are out of range sets status and its part of out is not written; a
- * bias for a token outside the vocabulary sets status and is passed over.  vocab_size <= 2^20. */
+ * bias for a token outside the vocabulary sets status and is passed over.  vocab_size <= 2^20, max_tokens < 2^20. */
 int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, void* cuda_stream);
 
 /* The pool that the sequences of a cache share.  All its arrays are written by the calls below. */

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -38,6 +39,11 @@ HOOK_DTYPE_BF16, HOOK_DTYPE_F16, HOOK_DTYPE_F32 = 0, 1, 2
 HOOK_ROPE_AXES_BLOCKED, HOOK_ROPE_AXES_CYCLIC = 0, 1
 HOOK_ROPE_PAIR_HALVES, HOOK_ROPE_PAIR_ADJACENT = 0, 1
 HOOK_ROPE_MAX_AXES = 4
+_NO_PAIRS = (0,) * HOOK_ROPE_MAX_AXES
+HOOK_CACHE_PAGE = 16             # tokens per page of the cache
+# Arguments between the handle and the stream: p an address, i an int32.
+_AROUND = {"hook_rope_append": "p", "hook_adjust_logits": "p", "hook_cache_fork": "pppi", "hook_cache_extend": "ppp",
+           "hook_cache_free": "pppi", "hook_cache_compact": "pppppp", "hook_cache_copy_pages": "p"}
 _DTYPES = {torch.bfloat16: HOOK_DTYPE_BF16, torch.float16: HOOK_DTYPE_F16, torch.float32: HOOK_DTYPE_F32}
 
 
@@ -104,6 +110,18 @@ class HookCacheCopyParams(ctypes.Structure):
                 + _fields("k_caches v_caches pairs num_pairs status", ctypes.c_void_p))
 
 
+def _packer(mirror) -> struct.Struct:
+    """The layout of a mirrored C struct for one ``pack`` of all its fields, arrays element by element."""
+    code = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", ctypes.c_void_p: "P"}
+    out = "@"
+    for _, t in mirror._fields_:
+        out += code[t] if t in code else f"{t._length_}{code[t._type_]}"
+    return struct.Struct(out + "0q")
+
+
+_ROPE, _LOGITS, _POOL, _COPY = (_packer(m) for m in (HookRopeParams, HookLogitsParams, HookCachePool, HookCacheCopyParams))
+
+
 class HookAttnError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -144,17 +162,11 @@ def load_library() -> ctypes.CDLL:
         lib.hook_capture_qk.restype = ctypes.c_int
         lib.hook_capture_qk.argtypes = [ctypes.c_void_p, ctypes.POINTER(HookAttnParams), ctypes.c_int, ctypes.c_void_p,
                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
-        void_p, i32 = ctypes.c_void_p, ctypes.c_int32
-        for name, args in (("hook_rope_append", [ctypes.POINTER(HookRopeParams)]),
-                           ("hook_adjust_logits", [ctypes.POINTER(HookLogitsParams)]),
-                           ("hook_cache_fork", [ctypes.POINTER(HookCachePool), void_p, void_p, i32]),
-                           ("hook_cache_extend", [ctypes.POINTER(HookCachePool), void_p, void_p]),
-                           ("hook_cache_free", [ctypes.POINTER(HookCachePool), void_p, void_p, i32]),
-                           ("hook_cache_compact", [ctypes.POINTER(HookCachePool)] + [void_p] * 5),
-                           ("hook_cache_copy_pages", [ctypes.POINTER(HookCacheCopyParams)])):
+        void_p, i32 = ctypes.c_void_p, ctypes.c_int32              # structs are passed by address, or packed as bytes
+        for name, args in _AROUND.items():
             fn = getattr(lib, name)
             fn.restype = ctypes.c_int
-            fn.argtypes = [void_p] + args + [void_p]
+            fn.argtypes = [void_p] + [i32 if a == "i" else void_p for a in args] + [void_p]
         lib.hook_attn_selftest_wait_limit.restype = ctypes.c_int
         lib.hook_attn_selftest_wait_limit.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p,
                                                       ctypes.c_void_p]
@@ -229,6 +241,8 @@ class HookAttn:
             raise HookAttnError(rc, "hook_attn_create")
         self._lib = lib
         self._h = h
+        self._index = int(device)
+        self._calls = {name: getattr(lib, name) for name in _AROUND}
         self.device = torch.device("cuda", int(device))
 
     def close(self):
@@ -329,10 +343,30 @@ class HookAttn:
         return q_out, k_out, cu_k
 
     # -- what a decode step needs around the attention --------------------------------------
-    def _checked(self, name: str, *args, stream=None) -> None:
-        rc = int(getattr(self._lib, name)(self._h, *args, self._stream(stream)))
+    # These calls are short, so their arguments are packed by one struct.pack in the order of the C structs.
+    def _checked(self, name: str, stream, *args) -> None:
+        if stream is None:                         # what current_stream().cuda_stream says, without the two objects between
+            stream = torch._C._cuda_getCurrentRawStream(self._index)
+        rc = self._calls[name](self._h, *args, stream)
         if rc != HOOK_ATTN_OK:
             raise HookAttnError(rc, name)
+
+    def _here(self, *tensors) -> bool:
+        """All of them (those that are given) on the handle's device."""
+        index = self._index
+        for t in tensors:
+            if t is not None and t.get_device() != index:
+                return False
+        return True
+
+    def _new(self, like: torch.Tensor, shape, dtype, stream) -> torch.Tensor:
+        """Memory for a call: taken in the order of the stream that the call goes to, so that neither what used it before nor what gets
+        it afterwards is still to run, or already running, there."""
+        if stream is None or stream == torch._C._cuda_getCurrentRawStream(self._index):
+            return like.new_empty(shape, dtype=dtype)
+        other = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(other):
+            return like.new_empty(shape, dtype=dtype)
 
     def hook_rope_append(self, *, q, k, v, k_cache, v_cache, block_table, seq_lens, inv_freq, cu_q_lens=None, positions=None,
                          axis_pairs=None, axis_order: int = HOOK_ROPE_AXES_BLOCKED, pairing: int = HOOK_ROPE_PAIR_HALVES,
@@ -341,43 +375,38 @@ class HookAttn:
         ``inv_freq`` fp32 ``[R / 2]`` gives the frequencies of the pairs and R; ``axis_pairs`` how many pairs each axis has (default:
         one axis); ``positions`` int32 ``[axes, T]`` (default: the rows' places in their sequences).  bf16, fp16 or fp32 in, the
         rotated queries out as bf16, contiguous, like the attention reads them."""
-        total_q, hq, d = q.shape
+        bf16, i32, dtype = torch.bfloat16, torch.int32, q.dtype
+        total_q, hq, d = shape = q.shape
         nb, page, hkv, d2 = k_cache.shape
-        assert d2 == d and v_cache.shape == k_cache.shape and v_cache.stride() == k_cache.stride() and k_cache.stride(3) == 1
-        assert k_cache.dtype == v_cache.dtype == torch.bfloat16
-        assert k.shape == v.shape == (total_q, hkv, d) and q.dtype == k.dtype == v.dtype
-        assert (q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1) or total_q == 0
-        assert block_table.dtype == seq_lens.dtype == torch.int32 and block_table.is_contiguous() and seq_lens.is_contiguous()
-        assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+        seqs, width = block_table.shape
+        pairs, = inv_freq.shape
+        kv_stride = block_stride, token_stride, head_stride, unit = k_cache.stride()
+        (q_row, q_head, q_unit), (k_row, k_head, k_unit), (v_row, v_head, v_unit) = q.stride(), k.stride(), v.stride()
+        if axis_pairs is None:
+            axis_pairs = (pairs,)
+        axes, axis_stride = len(axis_pairs), 0
+        assert d2 == d and v_cache.shape == k_cache.shape and v_cache.stride() == kv_stride and unit == 1
+        assert k_cache.dtype is bf16 and v_cache.dtype is bf16 and k.dtype is dtype and v.dtype is dtype
+        assert k.shape == v.shape == (total_q, hkv, d) and (q_unit == k_unit == v_unit == 1 or total_q == 0)
+        assert block_table.dtype is i32 and seq_lens.dtype is i32 and inv_freq.dtype is torch.float32 and seq_lens.shape == (seqs,)
+        assert block_table.is_contiguous() and seq_lens.is_contiguous() and inv_freq.is_contiguous() and 1 <= axes <= HOOK_ROPE_MAX_AXES
         if q_out is None:
-            q_out = torch.empty((total_q, hq, d), dtype=torch.bfloat16, device=q.device)
-        assert q_out.dtype == torch.bfloat16 and q_out.shape == q.shape and q_out.is_contiguous()
-        pairs = inv_freq.shape[0]
-        axis_pairs = (pairs,) if axis_pairs is None else tuple(axis_pairs)
-        p = HookRopeParams()
-        p.num_seqs, p.total_q, p.num_q_heads, p.num_kv_heads, p.head_dim, p.page_size = seq_lens.shape[0], total_q, hq, hkv, d, page
-        p.num_blocks, p.max_blocks_per_seq = nb, block_table.shape[1]
-        assert block_table.shape[0] == p.num_seqs
-        p.dtype, p.rotary_dim, p.num_axes = _DTYPES[q.dtype], 2 * pairs, len(axis_pairs)
-        p.axis_pairs[:min(len(axis_pairs), HOOK_ROPE_MAX_AXES)] = axis_pairs[:HOOK_ROPE_MAX_AXES]
-        p.axis_order, p.pairing, p.factor = int(axis_order), int(pairing), float(factor)
-        p.q, p.k, p.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
-        p.q_row_stride, p.q_head_stride, _ = q.stride()
-        p.k_row_stride, p.k_head_stride, _ = k.stride()
-        p.v_row_stride, p.v_head_stride, _ = v.stride()
-        p.inv_freq = inv_freq.data_ptr()
+            q_out = self._new(q, shape, bf16, stream)
+        else:
+            assert q_out.dtype is bf16 and q_out.shape == shape and q_out.is_contiguous()
         if positions is not None:
-            assert positions.dtype == torch.int32 and positions.shape == (len(axis_pairs), total_q)
-            assert positions.stride(1) == 1 or total_q <= 1
-            p.positions, p.position_axis_stride = positions.data_ptr(), positions.stride(0)
-        p.q_out, p.k_cache, p.v_cache = q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr()
-        p.kv_block_stride, p.kv_token_stride, p.kv_head_stride, _ = k_cache.stride()
-        p.block_table, p.seq_lens = block_table.data_ptr(), seq_lens.data_ptr()
+            assert positions.dtype is i32 and positions.shape == (axes, total_q)
+            axis_stride, unit = positions.stride()
+            assert unit == 1 or total_q <= 1
         if cu_q_lens is not None:
-            assert cu_q_lens.dtype == torch.int32 and cu_q_lens.is_contiguous() and cu_q_lens.shape[0] == p.num_seqs + 1
-            p.cu_q_lens = cu_q_lens.data_ptr()
-        p.status = _dptr(status)
-        self._checked("hook_rope_append", ctypes.byref(p), stream=stream)
+            assert cu_q_lens.dtype is i32 and cu_q_lens.is_contiguous() and cu_q_lens.shape == (seqs + 1,)
+        assert self._here(q, k, v, k_cache, v_cache, block_table, seq_lens, inv_freq, q_out, positions, cu_q_lens, status)
+        self._checked("hook_rope_append", stream, _ROPE.pack(
+            seqs, total_q, hq, hkv, d, page, nb, width, _DTYPES[dtype], 2 * pairs, axes, *axis_pairs, *_NO_PAIRS[axes:],
+            axis_order, pairing, factor, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head,
+            inv_freq.data_ptr(), 0 if positions is None else positions.data_ptr(), axis_stride, q_out.data_ptr(), k_cache.data_ptr(),
+            v_cache.data_ptr(), block_stride, token_stride, head_stride, block_table.data_ptr(), seq_lens.data_ptr(), 0 if cu_q_lens is None else cu_q_lens.data_ptr(),
+            0 if status is None else status.data_ptr()))
         return q_out
 
     def hook_adjust_logits(self, logits, *, out=None, tokens=None, prompt_lens=None, total_lens=None, repetition=None, presence=None,
@@ -387,103 +416,117 @@ class HookAttn:
         ``out`` (the same type, or fp32).  ``tokens`` int32 ``[rows, max_tokens]`` holds each row's prompt and what was generated;
         the biases are lists in rows (``bias_offsets [rows + 1]``); ``mask`` int32 ``[masks, ceil(vocab / 32)]`` has a bit for each allowed
         token and ``mask_rows`` says which of them a row has (negative: none)."""
-        out = logits if out is None else out
-        rows, vocab = logits.shape
-        assert out.shape == logits.shape and (vocab == 1 or (logits.stride(1) == 1 and out.stride(1) == 1))
-        p = HookLogitsParams()
-        p.num_rows, p.vocab_size, p.dtype, p.out_dtype = rows, vocab, _DTYPES[logits.dtype], _DTYPES[out.dtype]
-        p.logits, p.out = logits.data_ptr(), out.data_ptr()
-        p.logits_row_stride, p.out_row_stride = max(logits.stride(0), vocab), max(out.stride(0), vocab)
+        i32, f32 = torch.int32, torch.float32
+        if out is None:
+            out = logits
+        rows, vocab = shape = logits.shape
+        (in_row, unit), (out_row, out_unit) = logits.stride(), out.stride()
+        assert out.shape == shape and (unit == out_unit == 1 or vocab == 1)
+        per_row = (rows,)
+        max_tokens = token_row = num_bias = num_masks = mask_row = 0
+        at_tokens = at_prompt = at_total = at_offsets = at_bias = at_values = at_mask = at_mask_rows = 0
         if tokens is not None:
-            assert tokens.dtype == torch.int32 and tokens.shape[0] == rows and (tokens.stride(1) == 1 or tokens.shape[1] <= 1)
-            for t in (prompt_lens, total_lens):
-                assert t.dtype == torch.int32 and t.shape == (rows,) and t.is_contiguous()
-            p.max_tokens, p.tokens_row_stride = tokens.shape[1], max(tokens.stride(0), tokens.shape[1])
-            p.tokens, p.prompt_lens, p.total_lens = tokens.data_ptr(), prompt_lens.data_ptr(), total_lens.data_ptr()
-        for name, t in (("repetition", repetition), ("presence", presence), ("frequency", frequency)):
-            if t is not None:
-                assert t.dtype == torch.float32 and t.shape == (rows,) and t.is_contiguous()
-                setattr(p, name, t.data_ptr())
+            num, max_tokens = tokens.shape
+            token_row, unit = tokens.stride()
+            assert tokens.dtype is i32 and prompt_lens.dtype is i32 and total_lens.dtype is i32 and num == rows
+            assert prompt_lens.shape == per_row and total_lens.shape == per_row and (unit == 1 or max_tokens <= 1)
+            assert prompt_lens.is_contiguous() and total_lens.is_contiguous()
+            at_tokens, at_prompt, at_total = tokens.data_ptr(), prompt_lens.data_ptr(), total_lens.data_ptr()
+        strength = []
+        for t in (repetition, presence, frequency):
+            assert t is None or (t.dtype is f32 and t.shape == per_row and t.is_contiguous())
+            strength.append(0 if t is None else t.data_ptr())
         if bias_offsets is not None:
-            assert bias_offsets.dtype == bias_tokens.dtype == torch.int32 and bias_values.dtype == torch.float32
-            assert bias_offsets.shape == (rows + 1,) and bias_tokens.shape == bias_values.shape
+            assert bias_offsets.dtype is i32 and bias_tokens.dtype is i32 and bias_values.dtype is f32
+            assert bias_offsets.shape == (rows + 1,) and bias_tokens.dim() == 1 and bias_tokens.shape == bias_values.shape
             assert bias_offsets.is_contiguous() and bias_tokens.is_contiguous() and bias_values.is_contiguous()
-            p.num_bias = bias_tokens.shape[0]
-            p.bias_offsets, p.bias_tokens, p.bias_values = bias_offsets.data_ptr(), bias_tokens.data_ptr(), bias_values.data_ptr()
+            num_bias, = bias_tokens.shape
+            at_offsets, at_bias, at_values = bias_offsets.data_ptr(), bias_tokens.data_ptr(), bias_values.data_ptr()
         if mask is not None:
-            assert mask.dtype in (torch.int32, torch.uint32) and mask.shape[1] >= (vocab + 31) // 32
-            assert mask.stride(1) == 1 or mask.shape[1] == 1
-            p.num_masks, p.mask, p.mask_row_stride = mask.shape[0], mask.data_ptr(), max(mask.stride(0), mask.shape[1])
+            num_masks, words = mask.shape
+            mask_row, unit = mask.stride()
+            assert (mask.dtype is i32 or mask.dtype is torch.uint32) and (unit == 1 or words == 1) and 32 * words >= vocab
+            at_mask = mask.data_ptr()
             if mask_rows is not None:
-                assert mask_rows.dtype == torch.int32 and mask_rows.shape == (rows,) and mask_rows.is_contiguous()
-                p.mask_rows = mask_rows.data_ptr()
-        p.status = _dptr(status)
-        self._checked("hook_adjust_logits", ctypes.byref(p), stream=stream)
+                assert mask_rows.dtype is i32 and mask_rows.shape == per_row and mask_rows.is_contiguous()
+                at_mask_rows = mask_rows.data_ptr()
+            mask_row = max(mask_row, words)
+        assert self._here(logits, out, tokens, prompt_lens, total_lens, repetition, presence, frequency, bias_offsets, bias_tokens, bias_values,
+                          mask, mask_rows, status)
+        self._checked("hook_adjust_logits", stream, _LOGITS.pack(
+            rows, vocab, max_tokens, num_bias, num_masks, _DTYPES[logits.dtype], _DTYPES[out.dtype], logits.data_ptr(), out.data_ptr(),
+            max(in_row, vocab), max(out_row, vocab), at_tokens, max(token_row, max_tokens), at_prompt, at_total, *strength, at_offsets, at_bias,
+            at_values, at_mask, mask_row, at_mask_rows, 0 if status is None else status.data_ptr()))
         return out
 
-    @staticmethod
-    def _pool(block_table, seq_lens, page_refs, status) -> HookCachePool:
-        for t in (block_table, seq_lens, page_refs):
-            assert t.dtype == torch.int32 and t.is_contiguous()
+    def _pool(self, block_table, seq_lens, page_refs, status) -> bytes:
+        i32 = torch.int32
         seqs, width = block_table.shape
-        assert seq_lens.shape[0] == seqs
-        return HookCachePool(seqs, width, page_refs.shape[0], 16, block_table.data_ptr(), seq_lens.data_ptr(), page_refs.data_ptr(), _dptr(status))
+        blocks, = page_refs.shape
+        assert block_table.dtype is i32 and seq_lens.dtype is i32 and page_refs.dtype is i32 and seq_lens.shape == (seqs,)
+        assert block_table.is_contiguous() and seq_lens.is_contiguous() and page_refs.is_contiguous()
+        assert self._here(block_table, seq_lens, page_refs, status)
+        return _POOL.pack(seqs, width, blocks, HOOK_CACHE_PAGE, block_table.data_ptr(), seq_lens.data_ptr(), page_refs.data_ptr(),
+                          0 if status is None else status.data_ptr())
 
     def hook_cache_fork(self, block_table, seq_lens, page_refs, parents, children, status=None, stream=None) -> None:
         """Sequence ``children[i]`` (empty) becomes a copy of ``parents[i]`` that shares its pages."""
-        assert parents.dtype == children.dtype == torch.int32 and parents.shape == children.shape
-        assert parents.is_contiguous() and children.is_contiguous()
-        pool = self._pool(block_table, seq_lens, page_refs, status)
-        self._checked("hook_cache_fork", ctypes.byref(pool), parents.data_ptr(), children.data_ptr(), parents.shape[0], stream=stream)
+        num, = parents.shape
+        assert parents.dtype is torch.int32 and children.dtype is torch.int32 and children.shape == (num,)
+        assert parents.is_contiguous() and children.is_contiguous() and self._here(parents, children)
+        self._checked("hook_cache_fork", stream, self._pool(block_table, seq_lens, page_refs, status), parents.data_ptr(), children.data_ptr(), num)
 
     def hook_cache_extend(self, block_table, seq_lens, page_refs, new_rows, pairs=None, status=None, stream=None) -> torch.Tensor:
         """Room for ``new_rows[s]`` more tokens in every sequence; returns ``pairs`` int32 ``[seqs, 2]``, the pages to copy before
         anything is appended (-1: none)."""
-        assert new_rows.dtype == torch.int32 and new_rows.shape == seq_lens.shape and new_rows.is_contiguous()
+        seqs, = new_rows.shape
+        assert new_rows.dtype is torch.int32 and seq_lens.shape == (seqs,) and new_rows.is_contiguous()
         if pairs is None:
-            pairs = torch.empty((seq_lens.shape[0], 2), dtype=torch.int32, device=seq_lens.device)
-        assert pairs.dtype == torch.int32 and pairs.shape == (seq_lens.shape[0], 2) and pairs.is_contiguous()
-        pool = self._pool(block_table, seq_lens, page_refs, status)
-        self._checked("hook_cache_extend", ctypes.byref(pool), new_rows.data_ptr(), pairs.data_ptr(), stream=stream)
+            pairs = self._new(new_rows, (seqs, 2), torch.int32, stream)
+        assert pairs.dtype is torch.int32 and pairs.shape == (seqs, 2) and pairs.is_contiguous() and self._here(new_rows, pairs)
+        self._checked("hook_cache_extend", stream, self._pool(block_table, seq_lens, page_refs, status), new_rows.data_ptr(), pairs.data_ptr())
         return pairs
 
     def hook_cache_free(self, block_table, seq_lens, page_refs, seqs, keep_lens=None, status=None, stream=None) -> None:
         """Cuts the sequences ``seqs`` to their first ``keep_lens`` tokens (default: to nothing)."""
-        assert seqs.dtype == torch.int32 and seqs.is_contiguous()
-        assert keep_lens is None or (keep_lens.dtype == torch.int32 and keep_lens.shape == seqs.shape and keep_lens.is_contiguous())
-        pool = self._pool(block_table, seq_lens, page_refs, status)
-        self._checked("hook_cache_free", ctypes.byref(pool), seqs.data_ptr(), _dptr(keep_lens), seqs.shape[0], stream=stream)
+        num, = seqs.shape
+        assert seqs.dtype is torch.int32 and seqs.is_contiguous() and self._here(seqs, keep_lens)
+        assert keep_lens is None or (keep_lens.dtype is torch.int32 and keep_lens.shape == (num,) and keep_lens.is_contiguous())
+        self._checked("hook_cache_free", stream, self._pool(block_table, seq_lens, page_refs, status), seqs.data_ptr(), _dptr(keep_lens), num)
 
     def hook_cache_compact(self, block_table, seq_lens, page_refs, status=None, stream=None):
         """Plans how the used pages move together at the low end of the pool.  Returns ``(block_table, page_refs, page_map, pairs,
         num_pairs)`` as they are once the pairs are copied; the old ones stay as they are."""
         pool = self._pool(block_table, seq_lens, page_refs, status)
-        nb = page_refs.shape[0]
-        table_out, refs_out, page_map = torch.empty_like(block_table), torch.empty_like(page_refs), torch.empty_like(page_refs)
-        pairs = torch.empty((nb // 2, 2), dtype=torch.int32, device=page_refs.device)
-        num_pairs = torch.empty(1, dtype=torch.int32, device=page_refs.device)
-        self._checked("hook_cache_compact", ctypes.byref(pool), table_out.data_ptr(), refs_out.data_ptr(), page_map.data_ptr(),
-                      pairs.data_ptr(), num_pairs.data_ptr(), stream=stream)
+        blocks, = page_refs.shape
+        table_out, refs_out, page_map, pairs, num_pairs = (
+            self._new(page_refs, shape, torch.int32, stream) for shape in (block_table.shape, (blocks,), (blocks,), (blocks // 2, 2), (1,)))
+        self._checked("hook_cache_compact", stream, pool, table_out.data_ptr(), refs_out.data_ptr(), page_map.data_ptr(), pairs.data_ptr(),
+                      num_pairs.data_ptr())
         return table_out, refs_out, page_map, pairs, num_pairs
 
     def hook_cache_copy_pages(self, caches, pairs, num_pairs=None, status=None, stream=None) -> None:
         """Copies pages ``pairs[i] = (source, destination)`` in the ``caches``, a list of ``(k_cache, v_cache)`` of the layers (one
         shape, one set of strides).  ``num_pairs``: int32 ``[1]`` on the device, how many of the pairs count."""
-        assert pairs.dtype == torch.int32 and pairs.dim() == 2 and pairs.shape[1] == 2 and pairs.is_contiguous()
-        assert num_pairs is None or (num_pairs.dtype == torch.int32 and num_pairs.numel() == 1)
-        n = len(caches)
-        if n == 0:
+        num, two = pairs.shape
+        assert pairs.dtype is torch.int32 and two == 2 and pairs.is_contiguous() and self._here(pairs, num_pairs, status)
+        assert num_pairs is None or (num_pairs.dtype is torch.int32 and num_pairs.numel() == 1)
+        layers = len(caches)
+        if layers == 0:
             return
-        first = caches[0][0]
-        shape, stride = first.shape, first.stride()
-        assert first.dtype == torch.bfloat16 and stride[3] == 1
-        ks, vs = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)()
-        for i, (kc, vc) in enumerate(caches):
-            assert kc.shape == vc.shape == shape and kc.stride() == vc.stride() == stride and kc.dtype == vc.dtype == first.dtype
-            ks[i], vs[i] = kc.data_ptr(), vc.data_ptr()
-        p = HookCacheCopyParams(n, shape[0], shape[1], shape[2], shape[3], pairs.shape[0], stride[0], stride[1], stride[2],
-                                ctypes.addressof(ks), ctypes.addressof(vs), pairs.data_ptr(), _dptr(num_pairs), _dptr(status))
-        self._checked("hook_cache_copy_pages", ctypes.byref(p), stream=stream)
+        bf16, index, first = torch.bfloat16, self._index, caches[0][0]
+        blocks, page, heads, dim = shape = first.shape
+        stride = first.stride()
+        assert stride[3] == 1
+        at = []
+        for pair in caches:
+            for c in pair:
+                assert c.shape == shape and c.stride() == stride and c.dtype is bf16 and c.get_device() == index
+                at.append(c.data_ptr())
+        ks, vs = (ctypes.c_void_p * layers)(*at[::2]), (ctypes.c_void_p * layers)(*at[1::2])
+        self._checked("hook_cache_copy_pages", stream, _COPY.pack(
+            layers, blocks, page, heads, dim, num, *stride[:3], ctypes.addressof(ks), ctypes.addressof(vs), pairs.data_ptr(),
+            0 if num_pairs is None else num_pairs.data_ptr(), 0 if status is None else status.data_ptr()))
 
     # -- convenience ---------------------------------------------------------------------
     def plan(self, is_decode: bool, *, q, k_cache, v_cache, block_table, seq_lens, cu_q_lens=None,

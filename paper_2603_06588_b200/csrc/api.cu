@@ -40,7 +40,7 @@ cudaError_t launch_capture(const KernelArgs& a, const HeadCfg& hc, int head_dim,
 cudaError_t launch_rope_append(RopeArgs& a, int dtype, int num_sms, cudaStream_t st);
 // logits.cu
 cudaError_t configure_logits();
-cudaError_t launch_adjust_logits(const LogitsArgs& a, int dtype, int out_dtype, cudaStream_t st);
+cudaError_t launch_adjust_logits(const LogitsArgs& a, int dtype, int out_dtype, int num_sms, cudaStream_t st);
 // cache_pages.cu
 cudaError_t configure_cache_pages();
 cudaError_t launch_fork(const PoolArgs& p, const int32_t* parents, const int32_t* children, int n, cudaStream_t st);
@@ -476,7 +476,7 @@ int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, vo
         return HOOK_ATTN_ERR_INVALID_ARG;
     if (!dtype_ok(p->dtype) || !dtype_ok(p->out_dtype)) return HOOK_ATTN_ERR_INVALID_ARG;
     if (p->out_dtype != p->dtype && p->out_dtype != HOOK_DTYPE_F32) return HOOK_ATTN_ERR_UNSUPPORTED;
-    if (p->vocab_size > kMaxVocab || p->num_rows > 65535) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->vocab_size > kMaxVocab || p->num_rows > 65535 || p->max_tokens > kMaxHistory) return HOOK_ATTN_ERR_UNSUPPORTED;
     if (p->num_rows > 0) {
         if (!p->logits || !p->out || p->logits_row_stride < p->vocab_size || p->out_row_stride < p->vocab_size)
             return HOOK_ATTN_ERR_INVALID_ARG;
@@ -504,7 +504,7 @@ int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, vo
     a.mask = p->mask; a.mask_row = p->mask_row_stride; a.mask_rows = p->mask_rows;
     a.status = p->status;
     a.rows = p->num_rows; a.vocab = p->vocab_size; a.max_tokens = p->max_tokens; a.num_bias = p->num_bias; a.num_masks = p->num_masks;
-    cudaError_t e = launch_adjust_logits(a, p->dtype, p->out_dtype, static_cast<cudaStream_t>(cuda_stream));
+    cudaError_t e = launch_adjust_logits(a, p->dtype, p->out_dtype, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
 }
 

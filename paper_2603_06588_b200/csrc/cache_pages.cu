@@ -15,34 +15,6 @@ __device__ __forceinline__ int pages_of(int len) { return (int)(((int64_t)len + 
 __device__ __forceinline__ int64_t capacity(const PoolArgs& p) { return (int64_t)p.max_blocks * kPage; }
 __device__ __forceinline__ bool page_ok(const PoolArgs& p, int page) { return page >= 0 && page < p.num_blocks; }
 
-// Exclusive prefix sum over the CTA; `total` is the sum.  `sh` holds 33 ints.
-__device__ __forceinline__ int block_scan(int x, int* sh, int& total)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int incl = x;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
-    }
-    __syncthreads();                              // sh may still be read from the scan before
-    if (lane == 31) sh[warp] = incl;
-    __syncthreads();
-    if (warp == 0) {
-        int w = lane < (int)(blockDim.x >> 5) ? sh[lane] : 0, wi = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, wi, o);
-            if (lane >= o) wi += y;
-        }
-        sh[lane] = wi - w;
-        if (lane == 31) sh[32] = wi;
-    }
-    __syncthreads();
-    total = sh[32];
-    return sh[warp] + incl - x;
-}
-
 // One CTA per entry: children[i] gets the pages of parents[i].  An entry is refused (status) when a row is out of range, the
 // child holds pages, the child is listed earlier, the child is a parent of the same call, or the parent's row is broken.
 __global__ void __launch_bounds__(kListThreads) fork_kernel(const PoolArgs p, const int32_t* __restrict__ parents,

@@ -12,9 +12,11 @@ namespace hook_attn {
 
 namespace {
 
-constexpr int kLogitThreads = 256;
-constexpr int kSlice = 8192;                     // entries of a row per CTA: 32 KB of counters, 32 KB of bias places
-constexpr uint32_t kSeen = 0x80000000u;          // top bit of a counter: the token is in the prompt
+// A token's word: the lowest bits count how often it was generated, the next hold 1 + the place of its bias in the row's list,
+// the top bit says that it is in the prompt.  0: nothing but the grammar concerns it.
+constexpr int kCountBits = 20, kPlaceBits = 11;
+constexpr uint32_t kSeen = 0x80000000u, kCountMask = (1u << kCountBits) - 1, kPlaceMask = ((1u << kPlaceBits) - 1) << kCountBits;
+static_assert(kMaxHistory == (int)kCountMask && kMaxRowBias == (int)(kPlaceMask >> kCountBits), "limits of the words");
 
 __device__ __forceinline__ float load_f32(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float load_f32(const __half* p) { return __half2float(*p); }
@@ -23,71 +25,303 @@ __device__ __forceinline__ void store_f32(__nv_bfloat16* p, float x) { *p = __fl
 __device__ __forceinline__ void store_f32(__half* p, float x) { *p = __float2half(x); }
 __device__ __forceinline__ void store_f32(float* p, float x) { *p = x; }
 
-// A CTA owns one slice of one row: it counts the row's tokens that fall into the slice in shared memory (integers, so
-// the order of the atomics is of no account) and then passes over the slice once.
-template <typename TI, typename TO>
-__global__ void __launch_bounds__(kLogitThreads) adjust_logits_kernel(const __grid_constant__ LogitsArgs a)
+// A stretch of one row: the values [lo, hi).  Its words lie so that the eight of a vector are aligned: word 8 belongs to `base`,
+// the stretch's first value whose address is a multiple of 16 bytes; the values of a row before its first such one take the words
+// before it, in the row's first stretch.
+struct Stretch {
+    float rep, inv_rep, pres, freq;
+    const float* bias;             // the row's bias values
+    const uint32_t* grammar;       // its mask, or null
+    int row, total, prompt, b0, b1;
+    int lo, hi, base, first;       // first: the value that word 0 would belong to
+    bool valid, any;               // any: the history or the biases may concern it
+};
+
+// Values of a row before the first one whose address is a multiple of 16 bytes.
+template <typename TI>
+__device__ __forceinline__ int values_before_aligned(const LogitsArgs& a, int row)
 {
-    extern __shared__ uint32_t sh[];
-    uint32_t* count = sh;                        // [kSlice]
-    uint32_t* place = sh + kSlice;               // [kSlice], with biases: 1 + the last entry that names the token
-    const int row = blockIdx.y, v0 = blockIdx.x * kSlice, n = min(kSlice, a.vocab - v0);
-    const int total = a.tokens ? a.total_lens[row] : 0, prompt = a.tokens ? a.prompt_lens[row] : 0;
-    const int b0 = a.bias_offsets ? a.bias_offsets[row] : 0, b1 = a.bias_offsets ? a.bias_offsets[row + 1] : 0;
-    const int grammar = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
-    if (total < 0 || total > a.max_tokens || prompt < 0 || prompt > total || b0 < 0 || b1 < b0 || b1 > a.num_bias || grammar >= a.num_masks) {
-        if (threadIdx.x == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-        return;
+    constexpr uintptr_t kPer16 = 16 / sizeof(TI);
+    const TI* in = static_cast<const TI*>(a.logits) + (int64_t)row * a.in_row;
+    return (int)((kPer16 - reinterpret_cast<uintptr_t>(in) / sizeof(TI) % kPer16) % kPer16);
+}
+
+template <typename TI>
+__device__ __forceinline__ Stretch open_stretch(const LogitsArgs& a, int row, int slice, int length)
+{
+    Stretch s;
+    s.row = row;
+    s.total = a.tokens ? a.total_lens[row] : 0;
+    s.prompt = a.tokens ? a.prompt_lens[row] : 0;
+    s.b0 = a.bias_offsets ? a.bias_offsets[row] : 0;
+    s.b1 = a.bias_offsets ? a.bias_offsets[row + 1] : 0;
+    const int mask = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
+    s.rep = a.repetition ? a.repetition[row] : 1.f;
+    s.inv_rep = __frcp_rn(s.rep);
+    s.pres = a.presence ? a.presence[row] : 0.f;
+    s.freq = a.frequency ? a.frequency[row] : 0.f;
+    s.valid = s.total >= 0 && s.total <= a.max_tokens && s.prompt >= 0 && s.prompt <= s.total && s.b0 >= 0 && s.b1 >= s.b0 &&
+              s.b1 <= a.num_bias && s.b1 - s.b0 <= kMaxRowBias && mask < a.num_masks;
+    s.any = s.valid && (s.total > 0 || s.b1 > s.b0);
+    s.bias = a.bias_values + (s.valid ? s.b0 : 0);
+    s.grammar = s.valid && mask >= 0 ? a.mask + (int64_t)mask * a.mask_row : nullptr;
+    s.base = values_before_aligned<TI>(a, row) + slice * length;
+    s.lo = slice == 0 ? 0 : min(s.base, a.vocab);             // a row with a head may need one stretch less
+    s.hi = min(s.base + length, a.vocab);
+    s.first = s.base - 8;
+    return s;
+}
+
+// A value with a word that is not zero.  Multiplied by 1 / repetition, a positive value is rounded twice.
+__device__ __forceinline__ float edit(float x, uint32_t word, const Stretch& r)
+{
+    const uint32_t made = word & kCountMask;
+    const float scale = word & (kSeen | kCountMask) ? (x > 0.f ? r.inv_rep : r.rep) : 1.f;
+    x = x * scale - (r.freq * (float)made + (made ? r.pres : 0.f));
+    if (word & kPlaceMask) x += r.bias[((word & kPlaceMask) >> kCountBits) - 1];
+    return x;
+}
+
+template <typename T>
+struct alignas(16) Vec {            // eight values: one or two accesses of 16 bytes
+    T x[8];
+};
+
+// A CTA owns one slice of one row: it looks through the row's history for tokens of its slice and counts them in shared memory
+// (integers, so the order of the atomics is of no account), then passes over the slice once, eight values at a time.  Bound by
+// HBM: a value is read once and written once; the history is read by every CTA of the row, from L2.
+// The slice's words lie so that the eight of a vector are aligned: word 8 belongs to the slice's first aligned value, and the
+// values of a row before its first aligned one take the words before it, in the first slice.
+// The row's history as THREADS threads look through it for tokens of a stretch, four at a time.  The first eight tokens of each
+// thread are fetched when it is made, so that they are there when the words are ready to count in.  Integers: the order of the
+// atomics is of no account.
+template <int THREADS>
+struct History {
+    const int32_t* tokens;
+    int tid, head, quads;
+    int4 held[2];
+
+    __device__ __forceinline__ History(const LogitsArgs& a, const Stretch& s, int thread)
+        : tokens(a.tokens + (int64_t)s.row * a.token_row), tid(thread),
+          head(min(s.total, (int)((4 - reinterpret_cast<uintptr_t>(tokens) / 4 % 4) % 4))), quads((s.total - head) / 4)
+    {
+        fetch(tid);
     }
-    for (int i = threadIdx.x; i < n; i += kLogitThreads) {
-        count[i] = 0;
-        if (b1 > b0) place[i] = 0;
+    __device__ __forceinline__ void fetch(int i0)
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            held[u] = i0 + u * THREADS < quads ? reinterpret_cast<const int4*>(tokens + head)[i0 + u * THREADS] : make_int4(-1, -1, -1, -1);
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < total; i += kLogitThreads) {
-        const int t = a.tokens[(int64_t)row * a.token_row + i] - v0;
-        if ((unsigned)t < (unsigned)n) {
-            if (i < prompt) atomicOr(&count[t], kSeen);
-            else atomicAdd(&count[t], 1u);
+    __device__ __forceinline__ void count(const Stretch& s, uint32_t* word)
+    {
+        const unsigned span = s.hi - s.lo;
+        auto take = [&](int t, int i) {
+            if ((unsigned)t - (unsigned)s.lo >= span) return;
+            uint32_t* w = &word[t - s.first];
+            if (i >= s.prompt) atomicAdd(w, 1u);
+            else if (!(*w & kSeen)) atomicOr(w, kSeen);
+        };
+        for (int i0 = tid; i0 < quads; i0 += 2 * THREADS) {
+            const int4 now[2] = {held[0], held[1]};
+            fetch(i0 + 2 * THREADS);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int i = head + 4 * (i0 + u * THREADS);
+                take(now[u].x, i);
+                take(now[u].y, i + 1);
+                take(now[u].z, i + 2);
+                take(now[u].w, i + 3);
+            }
         }
+        const int i = tid < head ? tid : 4 * quads + tid;                 // what no quad covers, six tokens at most
+        if (i < s.total && tid < s.total - 4 * quads) take(tokens[i], i);
     }
-    for (int i = b0 + threadIdx.x; i < b1; i += kLogitThreads) {
-        const int v = a.bias_tokens[i], t = v - v0;
-        if (v < 0 || v >= a.vocab) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-        else if ((unsigned)t < (unsigned)n) atomicMax(&place[t], (uint32_t)(i - b0) + 1u);
+};
+
+// Puts one of the row's biases into its word: of a token that is named twice the last entry counts.  Returns the place of the word
+// where it was zero, else -1.
+__device__ __forceinline__ int place_bias(const LogitsArgs& a, const Stretch& s, uint32_t* word, int i)
+{
+    const int t = a.bias_tokens[i];
+    if (t < 0 || t >= a.vocab) {
+        if (s.lo == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        return -1;
     }
-    __syncthreads();
-    const float rep = a.repetition ? a.repetition[row] : 1.f, pres = a.presence ? a.presence[row] : 0.f;
-    const float freq = a.frequency ? a.frequency[row] : 0.f;
-    const TI* in = static_cast<const TI*>(a.logits) + (int64_t)row * a.in_row + v0;
-    TO* out = static_cast<TO*>(a.out) + (int64_t)row * a.out_row + v0;
-    const uint32_t* words = grammar >= 0 ? a.mask + (int64_t)grammar * a.mask_row : nullptr;
-    for (int i = threadIdx.x; i < n; i += kLogitThreads) {
-        float x = load_f32(in + i);
-        const uint32_t c = count[i];
-        if (c) {
-            x = x > 0.f ? x / rep : x * rep;
-            const uint32_t made = c & ~kSeen;
-            if (made) x = x - freq * (float)made - pres;
-        }
-        if (b1 > b0 && place[i]) x += a.bias_values[b0 + place[i] - 1];
-        if (words && !((words[(v0 + i) >> 5] >> ((v0 + i) & 31)) & 1u)) x = -INFINITY;
-        store_f32(out + i, x);
+    if ((unsigned)t - (unsigned)s.lo >= (unsigned)(s.hi - s.lo)) return -1;
+    uint32_t* w = &word[t - s.first];
+    uint32_t old = *w;
+    const uint32_t mine = (uint32_t)(i - s.b0 + 1) << kCountBits;
+    while ((old & kPlaceMask) < mine) {
+        const uint32_t was = atomicCAS(w, old, (old & ~kPlaceMask) | mine);
+        if (was == old) return old == 0 ? t - s.first : -1;
+        old = was;
     }
+    return -1;
+}
+
+// Eight values that begin at v, with the words of the stretch; `low` and `high` are the mask's words of the first and the last.
+template <typename TI, typename TO>
+__device__ __forceinline__ Vec<TO> edit_eight(const Vec<TI>& raw, const uint4& w0, const uint4& w1, uint32_t low, uint32_t high, int v,
+                                              const Stretch& s)
+{
+    const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+    const uint32_t allowed = __funnelshift_r(low, high, v & 31);          // eight bits that may lie in two words
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        x[k] = load_f32(&raw.x[k]);
+        if (w[k]) x[k] = edit(x[k], w[k], s);
+    }
+    Vec<TO> res;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) store_f32(&res.x[k], (allowed >> k) & 1u ? x[k] : -INFINITY);
+    return res;
 }
 
 template <typename TI, typename TO>
-cudaError_t launch(const LogitsArgs& a, cudaStream_t st)
+__device__ __forceinline__ void edit_one(const TI* in, TO* out, int v, uint32_t w, const Stretch& s)
 {
-    const dim3 grid((a.vocab + kSlice - 1) / kSlice, a.rows);
-    adjust_logits_kernel<TI, TO><<<grid, kLogitThreads, 2 * kSlice * 4, st>>>(a);
+    const float x = edit(load_f32(in + v), w, s);
+    store_f32(out + v, s.grammar && !((s.grammar[v >> 5] >> (v & 31)) & 1u) ? -INFINITY : x);
+}
+
+// Small calls: a CTA takes one stretch, one vector to a thread, whose load is under way while the words are filled.  Bound by the
+// chain of loads (the row's numbers, its history, the words): 3.0 us for 1 x 32000, of which 2.0 us without a history.
+template <typename TI, typename TO, int THREADS>
+__global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_constant__ LogitsArgs a)
+{
+    constexpr int kLength = THREADS * 8;
+    __shared__ __align__(16) uint32_t word[kLength + 8];
+    const int tid = threadIdx.x;
+    const Stretch s = open_stretch<TI>(a, blockIdx.y, blockIdx.x, kLength);
+    if (s.lo >= s.hi) return;
+    if (!s.valid) {
+        if (tid == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        return;
+    }
+    const TI* in = static_cast<const TI*>(a.logits) + (int64_t)s.row * a.in_row;
+    TO* out = static_cast<TO*>(a.out) + (int64_t)s.row * a.out_row;
+    const bool aligned = (reinterpret_cast<uintptr_t>(out + s.base) & 15) == 0;    // in and out reach a multiple of 16 bytes together
+    const int vectors = aligned ? max(s.hi - s.base, 0) / 8 : 0, v = s.base + 8 * tid;
+    History<THREADS> history(a, s, tid);
+    Vec<TI> raw;
+    uint32_t low = ~0u, high = ~0u;
+    if (tid < vectors) {
+        raw = *reinterpret_cast<const Vec<TI>*>(in + v);
+        if (s.grammar) {
+            low = s.grammar[v >> 5];
+            high = s.grammar[(v + 7) >> 5];
+        }
+    }
+    if (s.any) {
+        for (int i = tid; i < (kLength + 8) / 4; i += THREADS) reinterpret_cast<uint4*>(word)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        history.count(s, word);
+        for (int i = s.b0 + tid; i < s.b1; i += THREADS) place_bias(a, s, word, i);
+        __syncthreads();
+    }
+    if (tid < vectors) {
+        const uint4* w = reinterpret_cast<const uint4*>(word + 8 + 8 * tid);
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<Vec<TO>*>(out + v) = edit_eight<TI, TO>(raw, s.any ? w[0] : none, s.any ? w[1] : none, low, high, v, s);
+    }
+    // what no vector covers: the row's head, the values behind the last vector, all of a stretch that is not aligned
+    if (s.lo == 0 && tid < min(s.base, s.hi)) edit_one(in, out, tid, s.any ? word[tid - s.first] : 0u, s);
+    for (int i = s.base + 8 * vectors + tid; i < s.hi; i += THREADS) edit_one(in, out, i, s.any ? word[i - s.first] : 0u, s);
+}
+
+// Large calls: a CTA takes a long stretch, all of whose loads are under way while its words are filled; two CTAs on an SM keep 64
+// registers a thread.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 61 us, 5.4 TB/s); with one, by
+// the issue slots: each stretch of a row looks through the whole history (28 instructions for 32 tokens), and a warp runs the edit for
+// each of the eight values of a lane that any of its lanes has a word for.  (The same with histories of up to 4096 tokens: 78 us, 4.2
+// TB/s; 64 rows of 128000 bf16 to fp32 values with 32768 tokens: 32 us, 1.5 TB/s.)
+constexpr int kLargeThreads = 512, kTogether = 4, kLargeLength = kLargeThreads * kTogether * 8;
+
+struct Large {
+    uint32_t grammar[kLargeLength / 32 + 4];
+    uint32_t word[kLargeLength + 8];
+};
+
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(kLargeThreads, 2) adjust_logits_large_kernel(const __grid_constant__ LogitsArgs a)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    Large& w = *reinterpret_cast<Large*>(smem);
+    const int tid = threadIdx.x;
+    const Stretch s = open_stretch<TI>(a, blockIdx.y, blockIdx.x, kLargeLength);
+    if (s.lo >= s.hi) return;
+    if (!s.valid) {
+        if (tid == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        return;
+    }
+    const TI* in = static_cast<const TI*>(a.logits) + (int64_t)s.row * a.in_row;
+    TO* out = static_cast<TO*>(a.out) + (int64_t)s.row * a.out_row;
+    History<kLargeThreads> history(a, s, tid);
+    const int vectors = (reinterpret_cast<uintptr_t>(out + s.base) & 15) == 0 ? max(s.hi - s.base, 0) / 8 : 0;
+    Vec<TI> raw[kTogether];
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u)
+        if (tid + u * kLargeThreads < vectors) raw[u] = *reinterpret_cast<const Vec<TI>*>(in + s.base + 8 * (tid + u * kLargeThreads));
+    const int mask0 = s.lo >> 5;                                          // the stretch's part of the mask
+    if (s.grammar)
+        for (int i = tid; i <= ((s.hi - 1) >> 5) - mask0; i += kLargeThreads) w.grammar[i] = s.grammar[mask0 + i];
+    if (s.any)
+        for (int i = tid; i < (kLargeLength + 8) / 4; i += kLargeThreads) reinterpret_cast<uint4*>(w.word)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    if (s.any) {
+        history.count(s, w.word);
+        for (int i = s.b0 + tid; i < s.b1; i += kLargeThreads) place_bias(a, s, w.word, i);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u) {
+        const int i = tid + u * kLargeThreads, v = s.base + 8 * i;
+        if (i >= vectors) break;
+        uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
+        if (s.any) {
+            w0 = reinterpret_cast<const uint4*>(w.word + 8)[2 * i];
+            w1 = reinterpret_cast<const uint4*>(w.word + 8)[2 * i + 1];
+        }
+        uint32_t low = ~0u, high = ~0u;
+        if (s.grammar) {
+            low = w.grammar[(v >> 5) - mask0];
+            high = w.grammar[((v + 7) >> 5) - mask0];
+        }
+        *reinterpret_cast<Vec<TO>*>(out + v) = edit_eight<TI, TO>(raw[u], w0, w1, low, high, v, s);
+    }
+    // as in the small kernel: what no vector covers
+    if (s.lo == 0 && tid < min(s.base, s.hi)) edit_one(in, out, tid, s.any ? w.word[tid - s.first] : 0u, s);
+    for (int i = s.base + 8 * vectors + tid; i < s.hi; i += kLargeThreads) edit_one(in, out, i, s.any ? w.word[i - s.first] : 0u, s);
+}
+
+template <typename TI, typename TO, int THREADS>
+cudaError_t launch_small(const LogitsArgs& a, cudaStream_t st)
+{
+    adjust_logits_kernel<TI, TO, THREADS><<<dim3((a.vocab + THREADS * 8 - 1) / (THREADS * 8), a.rows), THREADS, 0, st>>>(a);
     return cudaGetLastError();
+}
+
+template <typename TI, typename TO>
+cudaError_t launch(const LogitsArgs& a, int num_sms, cudaStream_t st)
+{
+    // A long stretch for every SM: 64 x 128000 in 20 us, 32 x 128000 in 12 us, and 21 to 26 us, 12 to 15 us with short ones; 16 x 128000
+    // in 7.8 us either way, fewer rows are faster with short ones (4 x 128000 in 3.9 us, and 6.1 us with long ones).
+    if ((int64_t)a.rows * a.vocab >= (int64_t)num_sms * kLargeLength) {
+        adjust_logits_large_kernel<TI, TO>
+            <<<dim3((a.vocab + kLargeLength - 1) / kLargeLength, a.rows), kLargeThreads, sizeof(Large), st>>>(a);
+        return cudaGetLastError();
+    }
+    // More threads look through a long history side by side: 16000 tokens for 1 x 128000 in 14.2, 9.1, 7.1 us with 128, 256, 512
+    // threads, 2000 in 4.5, 4.1, 4.5 us, 100 in 3.7, 3.8, 4.1 us.
+    if (a.max_tokens > 4096) return launch_small<TI, TO, 512>(a, st);
+    return a.max_tokens > 1024 ? launch_small<TI, TO, 256>(a, st) : launch_small<TI, TO, 128>(a, st);
 }
 
 template <typename TI, typename TO>
 cudaError_t configure()
 {
-    return cudaFuncSetAttribute(adjust_logits_kernel<TI, TO>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kSlice * 4);
+    return cudaFuncSetAttribute(adjust_logits_large_kernel<TI, TO>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Large));
 }
 
 }  // namespace
@@ -102,11 +336,11 @@ cudaError_t configure_logits()
     return e;
 }
 
-cudaError_t launch_adjust_logits(const LogitsArgs& a, int dtype, int out_dtype, cudaStream_t st)
+cudaError_t launch_adjust_logits(const LogitsArgs& a, int dtype, int out_dtype, int num_sms, cudaStream_t st)
 {
-    if (dtype == HOOK_DTYPE_BF16) return out_dtype == dtype ? launch<__nv_bfloat16, __nv_bfloat16>(a, st) : launch<__nv_bfloat16, float>(a, st);
-    if (dtype == HOOK_DTYPE_F16) return out_dtype == dtype ? launch<__half, __half>(a, st) : launch<__half, float>(a, st);
-    return launch<float, float>(a, st);
+    if (dtype == HOOK_DTYPE_BF16) return out_dtype == dtype ? launch<__nv_bfloat16, __nv_bfloat16>(a, num_sms, st) : launch<__nv_bfloat16, float>(a, num_sms, st);
+    if (dtype == HOOK_DTYPE_F16) return out_dtype == dtype ? launch<__half, __half>(a, num_sms, st) : launch<__half, float>(a, num_sms, st);
+    return launch<float, float>(a, num_sms, st);
 }
 
 }  // namespace hook_attn

@@ -7,6 +7,8 @@ namespace hook_attn {
 
 constexpr int kMaxPairs = 64;          // rotated pairs per head: half of the largest head_dim
 constexpr int kMaxVocab = 1 << 20;     // entries per row of logits
+constexpr int kMaxHistory = (1 << 20) - 1;   // tokens of a row's history
+constexpr int kMaxRowBias = 2047;      // bias entries of a row
 constexpr int kMaxPoolSeqs = 16384;    // sequences of a page pool
 constexpr int kCopyLayers = 64;        // layers per launch of the page copy
 
@@ -53,5 +55,33 @@ struct CopyArgs {
     int32_t* status;
     int32_t layers, num_blocks, Hkv, head_dim, max_pairs;
 };
+
+// Exclusive prefix sum over the CTA; `total` is the sum.  `sh` holds 33 ints.
+__device__ __forceinline__ int block_scan(int x, int* sh, int& total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    __syncthreads();                              // sh may still be read from the scan before
+    if (lane == 31) sh[warp] = incl;
+    __syncthreads();
+    if (warp == 0) {
+        int w = lane < (int)(blockDim.x >> 5) ? sh[lane] : 0, wi = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, wi, o);
+            if (lane >= o) wi += y;
+        }
+        sh[lane] = wi - w;
+        if (lane == 31) sh[32] = wi;
+    }
+    __syncthreads();
+    total = sh[32];
+    return sh[warp] + incl - x;
+}
 
 }  // namespace hook_attn

@@ -10,8 +10,8 @@ from paper_2603_06588_b200 import binding
 
 from ._ops import FAKE_HANDLE, no_device, struct_fields
 
-# Relative to the sum of the magnitudes of a value's terms: the division, the product with the count, the two subtractions and the
-# addition of the bias are each rounded to 24 bits: 5 x 2^-24 < 2^-21.
+# Relative to the sum of the magnitudes of a value's terms: the reciprocal, the product with it, the one with the count, the two sums and the
+# addition of the bias are each rounded to 24 bits: 6 x 2^-24 < 2^-21.
 ARITHMETIC = 2.0 ** -21
 SMALLEST = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25, torch.float32: 0.0}    # half a step of the numbers next to zero
 
@@ -60,6 +60,7 @@ def _params(**over):
     (dict(out=0x10000, out_row_stride=1008), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(out_dtype=binding.HOOK_DTYPE_F16), binding.HOOK_ATTN_ERR_UNSUPPORTED),
     (dict(vocab_size=(1 << 20) + 1, logits_row_stride=1 << 21, out_row_stride=1 << 21, mask_row_stride=1 << 16), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(max_tokens=1 << 20, tokens_row_stride=1 << 20), binding.HOOK_ATTN_ERR_UNSUPPORTED),
     (dict(num_rows=65536), binding.HOOK_ATTN_ERR_UNSUPPORTED),
     (dict(logits=0x10001), binding.HOOK_ATTN_ERR_UNSUPPORTED),
     (dict(out=0x20002, dtype=binding.HOOK_DTYPE_F32, out_dtype=binding.HOOK_DTYPE_F32), binding.HOOK_ATTN_ERR_UNSUPPORTED),
@@ -149,6 +150,17 @@ def test_everything_on(eng, dtype, out, vocab):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [(torch.bfloat16, None), (torch.bfloat16, torch.float32), (torch.float16, torch.float32), (torch.float32, None)])
+@pytest.mark.parametrize("vocab", [1, 33, 777, 20011, 300007])
+def test_everything_on_with_long_histories(eng, dtype, out, vocab):
+    """Rows whose history is shared out; rows without one, and one that breaks off inside a load, beside them."""
+    g, x, kw = _random(4, vocab, dtype, 6007, vocab + 1, bias=70)
+    kw["total"][:3] = 6007, 0, 4999
+    kw["prompt"][:3] = 100, 0, 4998
+    _check(eng, x, out, mask=g.random((3, vocab)) < 0.7, mask_rows=[2, -1, 0, 1], **kw)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hist", [1, 255, 4097, 50000])
 def test_long_histories(eng, hist):
     _, x, kw = _random(3, 50021, torch.bfloat16, hist, hist)
@@ -157,10 +169,38 @@ def test_long_histories(eng, hist):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows", [1, 2, 150, 600])
+@pytest.mark.parametrize("rows", [1, 2, 150, 600, 900])
 def test_many_rows(eng, rows):
     g, x, kw = _random(rows, 3001, torch.float32, 64, rows, bias=3)
     _check(eng, x, mask=g.random((rows, 3001)) < 0.5, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out,pad,out_pad,in_place", [
+    (torch.bfloat16, torch.float32, 0, 0, False), (torch.bfloat16, None, 0, 0, True), (torch.float16, None, 5, 3, False),
+    (torch.float16, torch.float32, 0, 0, False), (torch.float32, None, 0, 0, False), (torch.float32, None, 7, 7, True), (torch.float32, None, 1, 2, False)])
+@pytest.mark.parametrize("rows,vocab,hist", [(100, 50023, 300), (500, 12305, 1500), (37, 131072, 9001), (9700, 301, 20)])
+def test_large_batches(eng, dtype, out, pad, out_pad, in_place, rows, vocab, hist):
+    """Long stretches: histories that are counted directly or sorted first (in one bin or three), rows without one, refused and unaligned rows."""
+    g, x, kw = _random(rows, vocab, dtype, hist, rows + vocab, bias=20)
+    kw["total"][:4] = hist, 0, 1, hist - 1
+    kw["prompt"][:4] = hist // 2, 0, 0, hist - 1
+    kw["total"][rows // 2] = hist + 1
+    kw["tokens"][4, ::3] = vocab + 5                            # placeholders
+    _check(eng, x, out, mask=g.random((5, vocab)) < 0.6, mask_rows=g.integers(-1, 5, rows).tolist(), pad=pad, out_pad=out_pad, in_place=in_place,
+           untouched=(rows // 2,), expect_status=binding.HOOK_ATTN_ERR_BOUNDS, **kw)
+
+
+@pytest.mark.gpu
+def test_large_batch_with_many_different_tokens(eng):
+    """A row whose stretches have more words than a warp lists, beside rows that repeat one token."""
+    rows, vocab, hist = 120, 40960, 20000
+    g, x, kw = _random(rows, vocab, torch.bfloat16, hist, 3)
+    kw["total"][:3] = hist
+    kw["prompt"][:3] = 0, hist, hist // 2
+    kw["tokens"][0] = g.permutation(vocab)[:hist]
+    kw["tokens"][1], kw["tokens"][2] = 77, np.arange(hist) // 7
+    _check(eng, x, torch.float32, **kw)
 
 
 @pytest.mark.gpu
@@ -172,8 +212,9 @@ def test_large_vocabulary(eng):
 @pytest.mark.gpu
 @pytest.mark.parametrize("pad,out_pad", [(0, 0), (24, 0), (5, 3), (1, 0), (0, 8)])
 @pytest.mark.parametrize("dtype,out", [(torch.bfloat16, torch.float32), (torch.float32, None), (torch.float16, None)])
-def test_strided_rows(eng, pad, out_pad, dtype, out):
-    g, x, kw = _random(4, 1021, dtype, 100, 11, bias=5)
+@pytest.mark.parametrize("hist", [100, 5000])
+def test_strided_rows(eng, pad, out_pad, dtype, out, hist):
+    g, x, kw = _random(4, 1021, dtype, hist, 11, bias=5)
     _check(eng, x, out, mask=g.random((4, 1021)) < 0.5, pad=pad, out_pad=out_pad, **kw)
 
 
@@ -214,11 +255,23 @@ def test_tokens_and_biases_outside_the_vocabulary(eng):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("entries", [2047, 2048])
+def test_longest_list_of_biases(eng, entries):
+    x = torch.randn(2, 3001, generator=torch.Generator().manual_seed(1))
+    g = np.random.default_rng(entries)
+    bias = [[(5, 1.0)], [(int(t), float(v)) for t, v in zip(g.integers(0, 3001, entries), g.normal(size=entries))]]
+    _check(eng, x, tokens=[[5, 5]] * 2, prompt=[0, 0], total=[2, 2], freq=[1.0, 1.0], bias=bias,
+           **(dict(expect_status=binding.HOOK_ATTN_ERR_BOUNDS, untouched=(1,)) if entries > 2047 else {}))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("over", [dict(total=[5, 9]), dict(total=[5, -1]), dict(prompt=[0, 6]), dict(prompt=[0, -1]), dict(mask_rows=[0, 2])])
 @pytest.mark.parametrize("in_place", [False, True])
-def test_broken_rows_are_left_alone(eng, over, in_place):
+@pytest.mark.parametrize("width", [8, 5000])
+def test_broken_rows_are_left_alone(eng, over, in_place, width):
     x = torch.randn(2, 50, generator=torch.Generator().manual_seed(1))
-    kw = dict(tokens=[[1, 2, 3, 4, 5, 6, 7, 8]] * 2, prompt=[0, 0], total=[5, 5], freq=[0.5, 0.5], mask=np.arange(100).reshape(2, 50) % 3 > 0, mask_rows=[1, 0])
+    over = {k: [width + 1 if v == 9 else v for v in o] for k, o in over.items()}
+    kw = dict(tokens=[[1, 2, 3, 4, 5, 6, 7, 8] + [0] * (width - 8)] * 2, prompt=[0, 0], total=[5, 5], freq=[0.5, 0.5], mask=np.arange(100).reshape(2, 50) % 3 > 0, mask_rows=[1, 0])
     _check(eng, x, expect_status=binding.HOOK_ATTN_ERR_BOUNDS, untouched=(1,), in_place=in_place, **dict(kw, **over))
 
 

@@ -293,7 +293,7 @@ typedef struct {
     int64_t         logits_row_stride, out_row_stride;
     const int32_t*  tokens;      /* [num_rows][max_tokens]: a row's prompt, then what was generated; ids outside
                                     [0, vocab_size) (placeholders) are passed over.  NULL: no penalties */
-    int64_t         tokens_row_stride;
+    int64_t         tokens_row_stride; /* 0: all rows have the same */
     const int32_t*  prompt_lens; /* [num_rows] tokens of the prompt */
     const int32_t*  total_lens;  /* [num_rows] tokens of prompt and generation, prompt_lens <= total_lens <= max_tokens */
     const float*    repetition;  /* [num_rows], > 0; NULL: 1 */
@@ -305,7 +305,7 @@ typedef struct {
     const float*    bias_values; /* [num_bias] */
     const uint32_t* mask;        /* [num_masks][ceil(vocab_size / 32)], bit v % 32 of word v / 32: token v is
                                     allowed.  NULL: no grammar */
-    int64_t         mask_row_stride; /* in words */
+    int64_t         mask_row_stride; /* in words; 0: all masks are the same */
     const int32_t*  mask_rows;   /* [num_rows] row of mask, negative: the row has no grammar.  NULL: row r has mask r */
     int32_t*        status;
 } hook_logits_params;
@@ -329,14 +329,16 @@ typedef struct {
 
 /* children[i] becomes a copy of sequence parents[i] that shares its pages (no data moves).  An entry is passed
  * over, with status HOOK_ATTN_ERR_BOUNDS, when one of its rows does not exist, its child is not empty, is named by
- * an earlier entry or is a parent in this call, or the parent's length or pages are out of range. */
+ * an earlier entry or is a parent in this call, or the parent's length or pages are out of range.  At most 16384
+ * entries, here and in hook_cache_free. */
 int hook_cache_fork(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* parents, const int32_t* children,
                     int32_t num_forks, void* cuda_stream);
 
 /* Room for new_rows[s] >= 0 more tokens in every sequence: the missing pages are taken from the pool, lowest ids
  * first and in the order of the sequences, and seq_lens grows.  A sequence that would write into a partly filled
  * page that it shares gets a page of its own instead, and pairs[s] = (old page, new page) for
- * hook_cache_copy_pages; else pairs[s] = (-1, -1).  Sequences that the pool cannot serve in their turn stay as
+ * hook_cache_copy_pages; else pairs[s] = (-1, -1).  Copy the pairs before anything is appended and before the next
+ * call here: a page that all its sharers leave in one call is free afterwards.  Sequences that the pool cannot serve in their turn stay as
  * they are and set status HOOK_ATTN_ERR_NO_PAGES; those whose length, table or last page is out of range stay as
  * they are and set HOOK_ATTN_ERR_BOUNDS.  pairs: int32 [num_seqs][2]. */
 int hook_cache_extend(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* new_rows, int32_t* pairs,

@@ -4,6 +4,7 @@ Test infrastructure only; shares nothing with the CUDA code.
 """
 from __future__ import annotations
 
+import collections
 import math
 
 import numpy as np
@@ -199,12 +200,13 @@ class Pool:
 def copy_pages(cache, pairs):
     """``cache`` ``[pages, ...]``.  Pairs that depend on one another are not carried out; returns the copy and whether there were any."""
     live = [(s, d) for s, d in pairs if s >= 0 and d >= 0]
+    sources, targets = collections.Counter(s for s, _ in live), collections.Counter(d for _, d in live)
     out, refused = cache.copy(), False
-    for i, (s, d) in enumerate(live):
-        others = live[:i] + live[i + 1:]
+    for s, d in live:
         if s == d:
             continue
-        if max(s, d) >= len(cache) or any(d in (s2, d2) or s == d2 for s2, d2 in others):
+        # its destination is somebody else's destination or source, or its source is a destination (its own is another page)
+        if max(s, d) >= len(cache) or targets[d] > 1 or sources[d] or targets[s]:
             refused = True
             continue
         out[d] = cache[s]

@@ -421,7 +421,7 @@ class HookAttn:
             out = logits
         rows, vocab = shape = logits.shape
         (in_row, unit), (out_row, out_unit) = logits.stride(), out.stride()
-        assert out.shape == shape and (unit == out_unit == 1 or vocab == 1)
+        assert out.shape == shape and (unit == out_unit == 1 or vocab == 1) and (rows <= 1 or (in_row >= vocab and out_row >= vocab))
         per_row = (rows,)
         max_tokens = token_row = num_bias = num_masks = mask_row = 0
         at_tokens = at_prompt = at_total = at_offsets = at_bias = at_values = at_mask = at_mask_rows = 0
@@ -450,12 +450,11 @@ class HookAttn:
             if mask_rows is not None:
                 assert mask_rows.dtype is i32 and mask_rows.shape == per_row and mask_rows.is_contiguous()
                 at_mask_rows = mask_rows.data_ptr()
-            mask_row = max(mask_row, words)
         assert self._here(logits, out, tokens, prompt_lens, total_lens, repetition, presence, frequency, bias_offsets, bias_tokens, bias_values,
                           mask, mask_rows, status)
         self._checked("hook_adjust_logits", stream, _LOGITS.pack(
             rows, vocab, max_tokens, num_bias, num_masks, _DTYPES[logits.dtype], _DTYPES[out.dtype], logits.data_ptr(), out.data_ptr(),
-            max(in_row, vocab), max(out_row, vocab), at_tokens, max(token_row, max_tokens), at_prompt, at_total, *strength, at_offsets, at_bias,
+            max(in_row, vocab), max(out_row, vocab), at_tokens, token_row, at_prompt, at_total, *strength, at_offsets, at_bias,
             at_values, at_mask, mask_row, at_mask_rows, 0 if status is None else status.data_ptr()))
         return out
 

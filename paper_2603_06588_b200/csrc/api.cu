@@ -435,7 +435,8 @@ int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* 
         if ((reinterpret_cast<uintptr_t>(p->q) | reinterpret_cast<uintptr_t>(p->k) | reinterpret_cast<uintptr_t>(p->v)) & (size - 1))
             return HOOK_ATTN_ERR_UNSUPPORTED;
         const int64_t D = p->head_dim;
-        if (p->q == p->q_out && (p->dtype != HOOK_DTYPE_BF16 || p->q_head_stride != D || p->q_row_stride != D * p->num_q_heads))
+        if (p->q == p->q_out && (p->dtype != HOOK_DTYPE_BF16 || (p->num_q_heads > 1 && p->q_head_stride != D) ||
+                                 (p->total_q > 1 && p->q_row_stride != D * p->num_q_heads)))
             return HOOK_ATTN_ERR_INVALID_ARG;       // in place only where every element stays where it is
     }
     int rc = check_handle(handle);
@@ -480,9 +481,9 @@ int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, vo
     if (p->num_rows > 0) {
         if (!p->logits || !p->out || p->logits_row_stride < p->vocab_size || p->out_row_stride < p->vocab_size)
             return HOOK_ATTN_ERR_INVALID_ARG;
-        if (p->tokens && (!p->prompt_lens || !p->total_lens || p->tokens_row_stride < p->max_tokens)) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->tokens && (!p->prompt_lens || !p->total_lens || p->tokens_row_stride < 0)) return HOOK_ATTN_ERR_INVALID_ARG;
         if (p->bias_offsets && p->num_bias > 0 && (!p->bias_tokens || !p->bias_values)) return HOOK_ATTN_ERR_INVALID_ARG;
-        if (p->mask && p->mask_row_stride < (p->vocab_size + 31) / 32) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->mask && p->mask_row_stride < 0) return HOOK_ATTN_ERR_INVALID_ARG;
         if (p->mask && !p->mask_rows && p->num_masks < p->num_rows) return HOOK_ATTN_ERR_INVALID_ARG;
         if (p->logits == p->out && (p->dtype != p->out_dtype || p->logits_row_stride != p->out_row_stride))
             return HOOK_ATTN_ERR_INVALID_ARG;
@@ -515,6 +516,7 @@ int hook_cache_fork(hook_attn_handle* handle, const hook_cache_pool* pool, const
     int rc = prepare_pool(pool, a);
     if (rc != HOOK_ATTN_OK) return rc;
     if (num_forks < 0 || (num_forks > 0 && (!parents || !children))) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (num_forks > kMaxPoolSeqs) return HOOK_ATTN_ERR_UNSUPPORTED;      // every entry is held against all others
     if ((rc = check_handle(handle)) != HOOK_ATTN_OK || num_forks == 0) return rc;
     cudaError_t e = launch_fork(a, parents, children, num_forks, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
@@ -538,6 +540,7 @@ int hook_cache_free(hook_attn_handle* handle, const hook_cache_pool* pool, const
     int rc = prepare_pool(pool, a);
     if (rc != HOOK_ATTN_OK) return rc;
     if (num_entries < 0 || (num_entries > 0 && !seqs)) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (num_entries > kMaxPoolSeqs) return HOOK_ATTN_ERR_UNSUPPORTED;
     if ((rc = check_handle(handle)) != HOOK_ATTN_OK || num_entries == 0) return rc;
     cudaError_t e = launch_free(a, seqs, keep_lens, num_entries, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;

@@ -15,6 +15,36 @@ __device__ __forceinline__ int pages_of(int len) { return (int)(((int64_t)len + 
 __device__ __forceinline__ int64_t capacity(const PoolArgs& p) { return (int64_t)p.max_blocks * kPage; }
 __device__ __forceinline__ bool page_ok(const PoolArgs& p, int page) { return page >= 0 && page < p.num_blocks; }
 
+// A CTA passes over the pool's reference counts in steps of EACH neighbouring pages to a thread: 1, 4 or 16, the fewest that cover the
+// pool in one step (700 pages in one step of 1: a compaction takes 4 us less than with 16), else 16 (100000 pages: seven steps).
+template <int EACH>
+__device__ __forceinline__ void load_refs(const PoolArgs& p, int base, int (&refs)[EACH], int missing)
+{
+    const int first = base + (int)threadIdx.x * EACH;
+    if (EACH % 4 == 0 && first + EACH <= p.num_blocks && (reinterpret_cast<uintptr_t>(p.page_refs) & 15) == 0) {
+#pragma unroll
+        for (int u = 0; u < EACH / 4; ++u) {
+            const int4 r = reinterpret_cast<const int4*>(p.page_refs + first)[u];
+            refs[4 * u] = r.x; refs[4 * u + 1] = r.y; refs[4 * u + 2] = r.z; refs[4 * u + 3] = r.w;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) refs[u] = first + u < p.num_blocks ? p.page_refs[first + u] : missing;
+    }
+}
+
+// Bit u: the thread's page u is free.
+template <int EACH>
+__device__ __forceinline__ uint32_t free_pages(const PoolArgs& p, int base)
+{
+    int refs[EACH];
+    load_refs<EACH>(p, base, refs, 1);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) bits |= (uint32_t)(refs[u] == 0) << u;
+    return bits;
+}
+
 // One CTA per entry: children[i] gets the pages of parents[i].  An entry is refused (status) when a row is out of range, the
 // child holds pages, the child is listed earlier, the child is a parent of the same call, or the parent's row is broken.
 __global__ void __launch_bounds__(kListThreads) fork_kernel(const PoolArgs p, const int32_t* __restrict__ parents,
@@ -80,6 +110,7 @@ __global__ void __launch_bounds__(kListThreads) free_kernel(const PoolArgs p, co
 // that the pool cannot serve in that order stay as they are.
 constexpr int kSplit = 1 << 30;                   // flag in a need: the last page is shared
 
+template <int EACH>
 __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, const int32_t* __restrict__ new_rows,
                                                               int32_t* __restrict__ pairs)
 {
@@ -116,36 +147,36 @@ __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, 
     }
     __syncthreads();
     // how many of the wanted pages there are
-    int have = 0;
-    for (int base = 0; base < p.num_blocks && have < wanted; base += kPoolThreads) {
-        const int page = base + (int)threadIdx.x;
-        have += __syncthreads_count(page < p.num_blocks && p.page_refs[page] == 0);
+    int have = 0, sum;
+    for (int base = 0; base < p.num_blocks && have < wanted; base += kPoolThreads * EACH) {
+        (void)block_scan(__popc(free_pages<EACH>(p, base)), sh, sum);
+        have += sum;
     }
-    // hand them out
+    // hand them out, in the order of their ids
     int rank = 0;
-    for (int base = 0; base < p.num_blocks && rank < wanted; base += kPoolThreads) {
-        const int page = base + (int)threadIdx.x;
-        const bool is_free = page < p.num_blocks && p.page_refs[page] == 0;
-        int total;
-        const int k = rank + block_scan(is_free, sh, total);
-        rank += total;
-        if (!is_free || k >= wanted) continue;
-        int lo = 0, hi = p.num_seqs;              // the last sequence whose first place is <= k
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (first[mid] <= k) lo = mid; else hi = mid;
+    for (int base = 0; base < p.num_blocks && rank < wanted; base += kPoolThreads * EACH) {
+        uint32_t free = free_pages<EACH>(p, base);
+        int k = rank + block_scan(__popc(free), sh, sum);
+        rank += sum;
+        for (; free && k < wanted; ++k, free &= free - 1) {
+            const int page = base + (int)threadIdx.x * EACH + __ffs(free) - 1;
+            int lo = 0, hi = p.num_seqs;          // the last sequence whose first place is <= k
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (first[mid] <= k) lo = mid; else hi = mid;
+            }
+            const int want = need[lo] & ~kSplit, j = k - first[lo];
+            if (first[lo] + want > have) continue;
+            const bool split = need[lo] & kSplit;
+            const int L = p.seq_lens[lo];
+            int32_t* row = p.block_table + (int64_t)lo * p.max_blocks + pages_of(L) - (split ? 1 : 0) + j;
+            if (split && j == 0) {
+                pairs[2 * lo] = *row;
+                pairs[2 * lo + 1] = page;
+            }
+            *row = page;
+            p.page_refs[page] = 1;
         }
-        const int want = need[lo] & ~kSplit, j = k - first[lo];
-        if (first[lo] + want > have) continue;
-        const bool split = need[lo] & kSplit;
-        const int L = p.seq_lens[lo];
-        int32_t* row = p.block_table + (int64_t)lo * p.max_blocks + pages_of(L) - (split ? 1 : 0) + j;
-        if (split && j == 0) {
-            pairs[2 * lo] = *row;
-            pairs[2 * lo + 1] = page;
-        }
-        *row = page;
-        p.page_refs[page] = 1;
     }
     __syncthreads();
     for (int s = threadIdx.x; s < p.num_seqs; s += kPoolThreads) {
@@ -162,32 +193,68 @@ __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, 
     }
 }
 
-// With U pages in use, the k-th used page at U or above moves to the k-th free page below U.
-__global__ void __launch_bounds__(kPoolThreads) compact_kernel(const PoolArgs p, int32_t* __restrict__ table_out,
-                                                               int32_t* __restrict__ refs_out, int32_t* __restrict__ page_map,
+// The table entry of sequence s at j after a move.  In place too: an entry depends on itself alone.
+__device__ __forceinline__ void remap_entry(const PoolArgs& p, const int32_t* page_map, int32_t* table_out, int s, int j)
+{
+    const int64_t at = (int64_t)s * p.max_blocks + j;
+    const int L = p.seq_lens[s];
+    const bool bad = L < 0 || L > capacity(p);
+    int to = -1;
+    if (!bad && j < pages_of(L)) {
+        const int page = p.block_table[at];
+        if (page_ok(p, page)) to = page_map[page];
+        if (to < 0) report(p.status, HOOK_ATTN_ERR_BOUNDS);
+    }
+    if (bad) report(p.status, HOOK_ATTN_ERR_BOUNDS);
+    table_out[at] = to;
+}
+
+// The tables of a large pool, one CTA per sequence.
+__global__ void __launch_bounds__(kListThreads) remap_kernel(const PoolArgs p, const int32_t* page_map, int32_t* table_out)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");       // launched while the map is being made
+    for (int j = threadIdx.x; j < p.max_blocks; j += kListThreads) remap_entry(p, page_map, table_out, blockIdx.x, j);
+}
+
+// With U pages in use, the k-th used page at U or above moves to the k-th free page below U.  table_out: null where the tables are
+// left to remap_kernel.
+template <int EACH>
+__global__ void __launch_bounds__(kPoolThreads) compact_kernel(const PoolArgs p, int32_t* table_out, int32_t* __restrict__ refs_out, int32_t* page_map,
                                                                int32_t* __restrict__ pairs, int32_t* __restrict__ num_pairs)
 {
+    if (!table_out) asm volatile("griddepcontrol.launch_dependents;");
     __shared__ int sh[33];
-    int used = 0;
-    for (int base = 0; base < p.num_blocks; base += kPoolThreads) {
-        const int page = base + (int)threadIdx.x;
-        used += __syncthreads_count(page < p.num_blocks && p.page_refs[page] > 0);
+    int used = 0, sum;
+    for (int base = 0; base < p.num_blocks; base += kPoolThreads * EACH) {
+        int refs[EACH], n = 0;
+        load_refs<EACH>(p, base, refs, 0);
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) n += refs[u] > 0;
+        (void)block_scan(n, sh, sum);
+        used += sum;
     }
     int sources = 0, holes = 0;
-    for (int base = 0; base < p.num_blocks; base += kPoolThreads) {
-        const int page = base + (int)threadIdx.x;
-        const int refs = page < p.num_blocks ? p.page_refs[page] : 0;
-        const bool hole = page < used && refs <= 0, source = page >= used && refs > 0;
-        int total;
-        int k = block_scan(hole, sh, total);
-        if (hole) pairs[2 * (holes + k) + 1] = page;
-        holes += total;
-        k = block_scan(source, sh, total);
-        if (source) pairs[2 * (sources + k)] = page;
-        sources += total;
-        if (page < p.num_blocks) {
-            page_map[page] = refs > 0 ? page : -1;
-            refs_out[page] = page < used && refs > 0 ? refs : 0;
+    for (int base = 0; base < p.num_blocks; base += kPoolThreads * EACH) {
+        int refs[EACH], from = 0, to = 0;
+        load_refs<EACH>(p, base, refs, 0);
+        const int first = base + (int)threadIdx.x * EACH;
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            to += first + u < used && refs[u] <= 0;
+            from += first + u >= used && refs[u] > 0;
+        }
+        int k = holes + block_scan(to, sh, sum);
+        holes += sum;
+        int l = sources + block_scan(from, sh, sum);
+        sources += sum;
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            const int page = first + u;
+            if (page >= p.num_blocks) break;
+            if (page < used && refs[u] <= 0) pairs[2 * k++ + 1] = page;
+            if (page >= used && refs[u] > 0) pairs[2 * l++] = page;
+            page_map[page] = refs[u] > 0 ? page : -1;
+            refs_out[page] = page < used && refs[u] > 0 ? refs[u] : 0;
         }
     }
     __syncthreads();
@@ -202,45 +269,72 @@ __global__ void __launch_bounds__(kPoolThreads) compact_kernel(const PoolArgs p,
         }
     }
     if (threadIdx.x == 0) *num_pairs = sources;
+    if (!table_out) return;
     __syncthreads();
-    const int64_t entries = (int64_t)p.num_seqs * p.max_blocks;
-    for (int64_t e = threadIdx.x; e < entries; e += kPoolThreads) {
-        const int s = (int)(e / p.max_blocks), j = (int)(e % p.max_blocks), L = p.seq_lens[s];
-        int to = -1;
-        if (L < 0 || L > capacity(p)) {
-            report(p.status, HOOK_ATTN_ERR_BOUNDS);
-        } else if (j < pages_of(L)) {
-            const int page = p.block_table[e];
-            if (page_ok(p, page)) to = page_map[page];
-            if (to < 0) report(p.status, HOOK_ATTN_ERR_BOUNDS);
-        }
-        table_out[e] = to;
-    }
+    for (int e = threadIdx.x; e < p.num_seqs * p.max_blocks; e += kPoolThreads) remap_entry(p, page_map, table_out, e / p.max_blocks, e % p.max_blocks);
 }
 
-// A CTA copies one page of one layer's keys or values.  Pairs must not depend on one another: one whose destination is the
-// destination or the source of another pair, or whose source is a destination, is not carried out.
-__global__ void __launch_bounds__(kListThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a)
+// A CTA copies `pairs` pages in `slabs` of the caches (keys or values of a layer).  Pairs must not depend on one another: one whose
+// destination is the destination or the source of another pair, or whose source is a destination, is not carried out, and a CTA looks
+// through all pairs to see that.  Bound by HBM (983 pages of 16 layers, 2.1 GB read and written: 334 us, 6.2 TB/s; equal shares for a
+// grid that is resident at once: 362 us).
+constexpr int kChecked = 8;                      // pairs of a CTA at most
+
+// TIGHT: a page's tokens and heads follow one another without gaps, in either order.
+template <bool TIGHT>
+__global__ void __launch_bounds__(kListThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a, int pairs, int slabs)
 {
-    const int i = blockIdx.x, n = a.num_pairs ? min(max(*a.num_pairs, 0), a.max_pairs) : a.max_pairs;
-    if (i >= n) return;
-    const int src = a.pairs[2 * i], dst = a.pairs[2 * i + 1];
-    if (src < 0 || dst < 0 || src == dst) return;
-    bool bad = src >= a.num_blocks || dst >= a.num_blocks;
+    __shared__ uint32_t refused;
+    const int n = a.num_pairs ? min(max(*a.num_pairs, 0), a.max_pairs) : a.max_pairs;
+    const int p0 = blockIdx.x * pairs, count = min(pairs, n - p0), slab0 = blockIdx.y * slabs, slab1 = min(slab0 + slabs, 2 * a.layers);
+    if (count <= 0) return;
+    int src[kChecked], dst[kChecked];
+#pragma unroll
+    for (int q = 0; q < kChecked; ++q) {
+        src[q] = q < count ? a.pairs[2 * (p0 + q)] : -1;
+        dst[q] = q < count ? a.pairs[2 * (p0 + q) + 1] : -1;
+        if (src[q] < 0 || dst[q] < 0) src[q] = dst[q] = -1;
+    }
+    if (threadIdx.x == 0) refused = 0;
+    __syncthreads();
+    uint32_t bad = 0;
     for (int j = threadIdx.x; j < n; j += kListThreads) {
         const int s = a.pairs[2 * j], d = a.pairs[2 * j + 1];
-        if (j != i && s >= 0 && d >= 0) bad |= d == dst || s == dst || d == src;
+        if (s < 0 || d < 0) continue;
+#pragma unroll
+        for (int q = 0; q < kChecked; ++q)
+            if (j != p0 + q && (d == dst[q] || s == dst[q] || d == src[q])) bad |= 1u << q;
     }
-    if (__syncthreads_or(bad)) {
-        if (threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-        return;
-    }
-    __nv_bfloat16* base = blockIdx.y & 1 ? a.v[blockIdx.y >> 1] : a.k[blockIdx.y >> 1];
-    const int per_row = a.head_dim / 8, total = kPage * a.Hkv * per_row;
-    for (int e = threadIdx.x; e < total; e += kListThreads) {
+    if (bad) atomicOr(&refused, bad);
+    __syncthreads();
+    const int per_row = a.head_dim / 8, pieces = kPage * a.Hkv * per_row;
+    auto place = [&](int e) {
+        if (TIGHT) return (int64_t)e * 8;
         const int c = e % per_row, h = e / per_row % a.Hkv, t = e / per_row / a.Hkv;
-        const int64_t at = (int64_t)t * a.ts + (int64_t)h * a.hs + c * 8;
-        *reinterpret_cast<uint4*>(base + (int64_t)dst * a.bs + at) = *reinterpret_cast<const uint4*>(base + (int64_t)src * a.bs + at);
+        return (int64_t)t * a.ts + (int64_t)h * a.hs + c * 8;
+    };
+#pragma unroll
+    for (int q = 0; q < kChecked; ++q) {
+        const int s = src[q], d = dst[q];
+        if (s == d) continue;
+        if ((refused >> q & 1) || s >= a.num_blocks || d >= a.num_blocks) {
+            if (threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+            continue;
+        }
+        for (int slab = slab0; slab < slab1; ++slab) {
+            __nv_bfloat16* base = slab & 1 ? a.v[slab >> 1] : a.k[slab >> 1];
+            const __nv_bfloat16* in = base + (int64_t)s * a.bs;
+            __nv_bfloat16* out = base + (int64_t)d * a.bs;
+            for (int e0 = threadIdx.x; e0 < pieces; e0 += 4 * kListThreads) {
+                uint4 held[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (e0 + u * kListThreads < pieces) held[u] = *reinterpret_cast<const uint4*>(in + place(e0 + u * kListThreads));
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (e0 + u * kListThreads < pieces) *reinterpret_cast<uint4*>(out + place(e0 + u * kListThreads)) = held[u];
+            }
+        }
     }
 }
 
@@ -248,7 +342,10 @@ __global__ void __launch_bounds__(kListThreads) copy_pages_kernel(const __grid_c
 
 cudaError_t configure_cache_pages()
 {
-    return cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxPoolSeqs * 4);
+    cudaError_t e = cudaFuncSetAttribute(extend_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxPoolSeqs * 4);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(extend_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxPoolSeqs * 4);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(extend_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxPoolSeqs * 4);
+    return e;
 }
 
 cudaError_t launch_fork(const PoolArgs& p, const int32_t* parents, const int32_t* children, int n, cudaStream_t st)
@@ -265,20 +362,44 @@ cudaError_t launch_free(const PoolArgs& p, const int32_t* seqs, const int32_t* k
 
 cudaError_t launch_extend(const PoolArgs& p, const int32_t* new_rows, int32_t* pairs, cudaStream_t st)
 {
-    extend_kernel<<<1, kPoolThreads, 2 * p.num_seqs * 4, st>>>(p, new_rows, pairs);
+    if (p.num_blocks <= kPoolThreads) extend_kernel<1><<<1, kPoolThreads, 2 * p.num_seqs * 4, st>>>(p, new_rows, pairs);
+    else if (p.num_blocks <= 4 * kPoolThreads) extend_kernel<4><<<1, kPoolThreads, 2 * p.num_seqs * 4, st>>>(p, new_rows, pairs);
+    else extend_kernel<16><<<1, kPoolThreads, 2 * p.num_seqs * 4, st>>>(p, new_rows, pairs);
     return cudaGetLastError();
 }
 
 cudaError_t launch_compact(const PoolArgs& p, int32_t* table_out, int32_t* refs_out, int32_t* page_map, int32_t* pairs,
                            int32_t* num_pairs, cudaStream_t st)
 {
-    compact_kernel<<<1, kPoolThreads, 0, st>>>(p, table_out, refs_out, page_map, pairs, num_pairs);
-    return cudaGetLastError();
+    // A second kernel for the tables pays from some 16 entries a thread on (48 x 29 entries: 4 us more).
+    const bool small = (int64_t)p.num_seqs * p.max_blocks <= 16 * kPoolThreads;
+    int32_t* here = small ? table_out : nullptr;
+    if (p.num_blocks <= kPoolThreads) compact_kernel<1><<<1, kPoolThreads, 0, st>>>(p, here, refs_out, page_map, pairs, num_pairs);
+    else if (p.num_blocks <= 4 * kPoolThreads) compact_kernel<4><<<1, kPoolThreads, 0, st>>>(p, here, refs_out, page_map, pairs, num_pairs);
+    else compact_kernel<16><<<1, kPoolThreads, 0, st>>>(p, here, refs_out, page_map, pairs, num_pairs);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || small) return e;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.num_seqs);
+    cfg.blockDim = dim3(kListThreads);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, remap_kernel, p, static_cast<const int32_t*>(page_map), table_out);
 }
 
 cudaError_t launch_copy_pages(const CopyArgs& a, cudaStream_t st)
 {
-    copy_pages_kernel<<<dim3(a.max_pairs, 2 * a.layers), kListThreads, 0, st>>>(a);
+    // A CTA for every slab of every pair; with many pairs, which each CTA has to look through, several of both for a CTA.
+    const bool many = a.max_pairs > 2048;
+    const int pairs = many ? kChecked : 1, slabs = many ? (2 * a.layers < 4 ? 2 * a.layers : 4) : 1;
+    const dim3 grid((a.max_pairs + pairs - 1) / pairs, (2 * a.layers + slabs - 1) / slabs);
+    const bool tight = (a.hs == a.head_dim && a.ts == (int64_t)a.Hkv * a.head_dim) || (a.ts == a.head_dim && a.hs == (int64_t)kPage * a.head_dim);
+    if (tight) copy_pages_kernel<true><<<grid, kListThreads, 0, st>>>(a, pairs, slabs);
+    else copy_pages_kernel<false><<<grid, kListThreads, 0, st>>>(a, pairs, slabs);
     return cudaGetLastError();
 }
 

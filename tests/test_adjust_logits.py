@@ -52,9 +52,10 @@ def _params(**over):
     (dict(logits=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(out_row_stride=999), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(prompt_lens=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
-    (dict(tokens_row_stride=63), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(tokens_row_stride=-1), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(tokens_row_stride=0, mask_row_stride=0), binding.HOOK_ATTN_ERR_CUDA),
     (dict(bias_values=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
-    (dict(mask_row_stride=31), binding.HOOK_ATTN_ERR_INVALID_ARG),
+    (dict(mask_row_stride=-1), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(num_masks=1), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(out=0x10000, out_dtype=binding.HOOK_DTYPE_F32), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(out=0x10000, out_row_stride=1008), binding.HOOK_ATTN_ERR_INVALID_ARG),
@@ -273,6 +274,26 @@ def test_broken_rows_are_left_alone(eng, over, in_place, width):
     over = {k: [width + 1 if v == 9 else v for v in o] for k, o in over.items()}
     kw = dict(tokens=[[1, 2, 3, 4, 5, 6, 7, 8] + [0] * (width - 8)] * 2, prompt=[0, 0], total=[5, 5], freq=[0.5, 0.5], mask=np.arange(100).reshape(2, 50) % 3 > 0, mask_rows=[1, 0])
     _check(eng, x, expect_status=binding.HOOK_ATTN_ERR_BOUNDS, untouched=(1,), in_place=in_place, **dict(kw, **over))
+
+
+@pytest.mark.gpu
+def test_shared_histories_and_rows_that_overlap(eng):
+    """Rows may share one history and one mask by a stride of 0; logits that overlap are refused."""
+    x = torch.randn(3, 100, generator=torch.Generator().manual_seed(4)).cuda()
+    tokens, lens = torch.arange(20, dtype=torch.int32, device="cuda").expand(3, 20), torch.full((3,), 20, dtype=torch.int32, device="cuda")
+    freq, mask = torch.full((3,), 0.5, device="cuda"), torch.full((1, 4), 0x7fff00ff, dtype=torch.int32, device="cuda")
+    got = eng.hook_adjust_logits(x, out=torch.empty_like(x), tokens=tokens, prompt_lens=lens - 10, total_lens=lens, frequency=freq, mask=mask.expand(3, 4))
+    want = x.clone()
+    want[:, 10:20] -= 0.5
+    bits = torch.arange(100, device="cuda")
+    want[:, (0x7fff00ff >> (bits % 32)) & 1 == 0] = float("-inf")
+    assert torch.equal(got, want)
+    with pytest.raises(AssertionError):
+        eng.hook_adjust_logits(x[:1].expand(3, 100), out=torch.empty_like(x))
+    with pytest.raises(AssertionError):
+        eng.hook_adjust_logits(x.cpu())
+    with pytest.raises(AssertionError):
+        eng.hook_adjust_logits(x, tokens=tokens.cpu(), prompt_lens=lens, total_lens=lens)
 
 
 @pytest.mark.gpu

@@ -94,6 +94,8 @@ def test_list_refusals():
     lib, p, bad = binding.load_library(), ctypes.byref(_pool_params()), binding.HOOK_ATTN_ERR_INVALID_ARG
     assert lib.hook_cache_fork(FAKE_HANDLE, p, None, 0x1000, 1, None) == bad
     assert lib.hook_cache_fork(FAKE_HANDLE, p, 0x1000, 0x1000, -1, None) == bad
+    assert lib.hook_cache_fork(FAKE_HANDLE, p, 0x1000, 0x1000, 16385, None) == binding.HOOK_ATTN_ERR_UNSUPPORTED
+    assert lib.hook_cache_free(FAKE_HANDLE, p, 0x1000, None, 16385, None) == binding.HOOK_ATTN_ERR_UNSUPPORTED
     assert lib.hook_cache_extend(FAKE_HANDLE, p, 0x1000, None, None) == bad
     assert lib.hook_cache_free(FAKE_HANDLE, p, None, None, 1, None) == bad
     assert lib.hook_cache_compact(FAKE_HANDLE, p, 0x1000, 0x30000, 0x3000, 0x4000, 0x5000, None) == bad      # the counts in place
@@ -180,6 +182,23 @@ class Both:
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("num_blocks", [16383, 16385, 70001])
+def test_large_pools(eng, num_blocks):
+    """More pages than one step of a scan, most of them taken, so that the free ones lie far apart; and a view that no vector load may touch."""
+    g = np.random.default_rng(num_blocks)
+    both = Both(eng, 60, 2000, num_blocks)
+    both.extend(g.integers(0, num_blocks * 16 // 60, 60).tolist())
+    both.free(g.integers(0, 60, 30).tolist(), g.integers(0, num_blocks * 10 // 60, 30).tolist())
+    both.fork([0, 1, 2], [57, 58, 59])
+    both.extend(g.integers(0, 3000, 60).tolist())
+    both.free([3, 9, 27, 31])
+    both.dev["page_refs"] = torch.cat([both.dev["page_refs"][:1], both.dev["page_refs"]])[1:]
+    both.compact(adopt=False)
+    both.extend(g.integers(0, 500, 60).tolist())
+    both.compact()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("seed", range(6))
 @pytest.mark.parametrize("num_seqs,max_blocks,num_blocks", [(1, 1, 1), (3, 4, 7), (40, 9, 150), (300, 40, 3000), (1100, 5, 2500)])
 def test_random_life(eng, seed, num_seqs, max_blocks, num_blocks):
@@ -245,7 +264,9 @@ def test_broken_pools_are_reported(eng, break_it):
     if break_it != "refs":
         both.fork([1], [3])
     both.extend([1, 1, 0, 0])
+    both.extend([0, 0, -1, 5])
     both.free([1, 7, -1])
+    both.free([2], [-1])
 
 
 @pytest.mark.gpu
@@ -327,12 +348,13 @@ def test_dependent_pairs_are_refused(eng, pairs):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n", [300, 2000])
+@pytest.mark.parametrize("n", [300, 2000, 5003])
 def test_many_pairs(eng, n):
     g = np.random.default_rng(n)
     order = g.permutation(2 * n)
     pairs = [(int(order[g.integers(0, n)]), int(order[n + i])) for i in range(n)]
     _check_copy(eng, pairs, pages=2 * n, hkv=1, layers=1)
+    _check_copy(eng, pairs, pages=2 * n, hkv=1, layers=2, count=n // 3)
     pairs[n // 2] = (pairs[n // 2][0], pairs[3][1])               # one destination twice: neither is carried out
     _check_copy(eng, pairs, pages=2 * n, hkv=1, layers=1, expect_status=binding.HOOK_ATTN_ERR_BOUNDS)
 

@@ -231,6 +231,9 @@ def test_unaligned_rows(eng, rot, offset):
 def test_in_place_queries(eng, adjacent):
     c = _case([9, 3], [0, 20], 4, 2, 128, 64, torch.bfloat16, fused=False)
     _check(eng, c, _freq(64), (64,), adjacent=adjacent, in_place=True)
+    c = _case([1], [20], 4, 2, 128, 64, torch.bfloat16, fused=False, decode=True)
+    c["q"] = torch.as_strided(c["q"], (1, 4, 128), (7, 128, 1))   # the stride of a single row is of no account
+    _check(eng, c, _freq(64), (64,), adjacent=adjacent, in_place=True)
 
 
 @pytest.mark.gpu
@@ -271,6 +274,17 @@ def test_many_sequences(eng):
     n = [i % 3 for i in range(700)]
     c = _case(n, [i % 5 for i in range(700)], 1, 1, 64, 8, torch.bfloat16)
     _check(eng, c, _freq(8), (8,))
+
+
+@pytest.mark.gpu
+def test_tensors_elsewhere_are_refused(eng):
+    c = _case([1], [3], 2, 2, 64, 32, torch.bfloat16, decode=True)
+    k, v = _views(c["cache"], "contiguous", 64)
+    kw = dict(q=c["q"], k=c["k"], v=c["v"], k_cache=k, v_cache=v, block_table=c["block_table"], seq_lens=c["seq_lens"], inv_freq=torch.ones(32))
+    with pytest.raises(AssertionError):
+        eng.hook_rope_append(**kw)
+    with pytest.raises(AssertionError):
+        eng.hook_rope_append(**dict({n: t.cuda() for n, t in kw.items()}, seq_lens=c["seq_lens"]))
 
 
 @pytest.mark.gpu

@@ -113,25 +113,34 @@ struct History {
         for (int u = 0; u < 2; ++u)
             held[u] = i0 + u * THREADS < quads ? reinterpret_cast<const int4*>(tokens + head)[i0 + u * THREADS] : make_int4(-1, -1, -1, -1);
     }
+    // Most tokens belong to other stretches: a token costs its test and one predicated reduction in shared memory, no branch.
     __device__ __forceinline__ void count(const Stretch& s, uint32_t* word)
     {
-        const unsigned span = s.hi - s.lo;
-        auto take = [&](int t, int i) {
-            if ((unsigned)t - (unsigned)s.lo >= span) return;
-            uint32_t* w = &word[t - s.first];
-            if (i >= s.prompt) atomicAdd(w, 1u);
-            else if (!(*w & kSeen)) atomicOr(w, kSeen);
+        const uint32_t span = s.hi - s.lo, at = smem_u32(word) + 4 * (s.lo - s.first);
+        auto see = [&](int t) {
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.or.b32 [%2], %3;\n\t}"
+                         ::"r"((uint32_t)t - (uint32_t)s.lo), "r"(span), "r"(at + 4 * ((uint32_t)t - (uint32_t)s.lo)), "r"(kSeen) : "memory");
         };
+        auto make = [&](int t) {
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.u32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], %3;\n\t}"
+                         ::"r"((uint32_t)t - (uint32_t)s.lo), "r"(span), "r"(at + 4 * ((uint32_t)t - (uint32_t)s.lo)), "r"(1u) : "memory");
+        };
+        auto take = [&](int t, int i) { i < s.prompt ? see(t) : make(t); };
+        const int seen = s.prompt <= head ? 0 : (s.prompt - head) / 4;    // quads that lie in the prompt; the next may do so in part
         for (int i0 = tid; i0 < quads; i0 += 2 * THREADS) {
             const int4 now[2] = {held[0], held[1]};
             fetch(i0 + 2 * THREADS);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int i = head + 4 * (i0 + u * THREADS);
-                take(now[u].x, i);
-                take(now[u].y, i + 1);
-                take(now[u].z, i + 2);
-                take(now[u].w, i + 3);
+                const int quad = i0 + u * THREADS, i = head + 4 * quad;
+                const int4 t = now[u];
+                if (quad < seen) {
+                    see(t.x); see(t.y); see(t.z); see(t.w);
+                } else if (i >= s.prompt) {
+                    make(t.x); make(t.y); make(t.z); make(t.w);
+                } else {
+                    take(t.x, i); take(t.y, i + 1); take(t.z, i + 2); take(t.w, i + 3);
+                }
             }
         }
         const int i = tid < head ? tid : 4 * quads + tid;                 // what no quad covers, six tokens at most
@@ -231,25 +240,28 @@ __global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_con
     for (int i = s.base + 8 * vectors + tid; i < s.hi; i += THREADS) edit_one(in, out, i, s.any ? word[i - s.first] : 0u, s);
 }
 
-// Large calls: a CTA takes a long stretch, all of whose loads are under way while its words are filled; two CTAs on an SM keep 64
-// registers a thread.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 61 us, 5.4 TB/s); with one, by
-// the issue slots: each stretch of a row looks through the whole history (28 instructions for 32 tokens), and a warp runs the edit for
-// each of the eight values of a lane that any of its lanes has a word for.  (The same with histories of up to 4096 tokens: 78 us, 4.2
-// TB/s; 64 rows of 128000 bf16 to fp32 values with 32768 tokens: 32 us, 1.5 TB/s.)
-constexpr int kLargeThreads = 512, kTogether = 4, kLargeLength = kLargeThreads * kTogether * 8;
+// Large calls: a CTA takes a long stretch, all of whose loads are under way while its words are filled; CTAs of 256 or 512 threads, 1024
+// threads on an SM with 64 registers each.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 55 us, 6.0
+// TB/s).  With one, by the chain of loads before a stretch's edits and by the issue slots: each stretch of a row looks through the whole
+// history, and a warp runs the edit for each of the eight values of a lane that any of its lanes has a word for (the same with
+// histories of up to 4096 tokens: 74 us, 4.5 TB/s; 64 rows of 128000 bf16 to fp32 values with up to 32768 tokens: 28 us, 1.9 TB/s).
+constexpr int kTogether = 4;
 
+template <int THREADS>
 struct Large {
-    uint32_t grammar[kLargeLength / 32 + 4];
-    uint32_t word[kLargeLength + 8];
+    static constexpr int kLength = THREADS * kTogether * 8;               // values of a stretch
+    uint32_t grammar[kLength / 32 + 4];
+    uint32_t word[kLength + 8];
 };
 
-template <typename TI, typename TO>
-__global__ void __launch_bounds__(kLargeThreads, 2) adjust_logits_large_kernel(const __grid_constant__ LogitsArgs a)
+template <typename TI, typename TO, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) adjust_logits_large_kernel(const __grid_constant__ LogitsArgs a)
 {
     extern __shared__ __align__(16) uint8_t smem[];
-    Large& w = *reinterpret_cast<Large*>(smem);
+    Large<THREADS>& w = *reinterpret_cast<Large<THREADS>*>(smem);
+    constexpr int kLength = Large<THREADS>::kLength;
     const int tid = threadIdx.x;
-    const Stretch s = open_stretch<TI>(a, blockIdx.y, blockIdx.x, kLargeLength);
+    const Stretch s = open_stretch<TI>(a, blockIdx.y, blockIdx.x, kLength);
     if (s.lo >= s.hi) return;
     if (!s.valid) {
         if (tid == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
@@ -257,26 +269,26 @@ __global__ void __launch_bounds__(kLargeThreads, 2) adjust_logits_large_kernel(c
     }
     const TI* in = static_cast<const TI*>(a.logits) + (int64_t)s.row * a.in_row;
     TO* out = static_cast<TO*>(a.out) + (int64_t)s.row * a.out_row;
-    History<kLargeThreads> history(a, s, tid);
+    History<THREADS> history(a, s, tid);
     const int vectors = (reinterpret_cast<uintptr_t>(out + s.base) & 15) == 0 ? max(s.hi - s.base, 0) / 8 : 0;
     Vec<TI> raw[kTogether];
 #pragma unroll
     for (int u = 0; u < kTogether; ++u)
-        if (tid + u * kLargeThreads < vectors) raw[u] = *reinterpret_cast<const Vec<TI>*>(in + s.base + 8 * (tid + u * kLargeThreads));
+        if (tid + u * THREADS < vectors) raw[u] = *reinterpret_cast<const Vec<TI>*>(in + s.base + 8 * (tid + u * THREADS));
     const int mask0 = s.lo >> 5;                                          // the stretch's part of the mask
     if (s.grammar)
-        for (int i = tid; i <= ((s.hi - 1) >> 5) - mask0; i += kLargeThreads) w.grammar[i] = s.grammar[mask0 + i];
+        for (int i = tid; i <= ((s.hi - 1) >> 5) - mask0; i += THREADS) w.grammar[i] = s.grammar[mask0 + i];
     if (s.any)
-        for (int i = tid; i < (kLargeLength + 8) / 4; i += kLargeThreads) reinterpret_cast<uint4*>(w.word)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < (kLength + 8) / 4; i += THREADS) reinterpret_cast<uint4*>(w.word)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     if (s.any) {
         history.count(s, w.word);
-        for (int i = s.b0 + tid; i < s.b1; i += kLargeThreads) place_bias(a, s, w.word, i);
+        for (int i = s.b0 + tid; i < s.b1; i += THREADS) place_bias(a, s, w.word, i);
         __syncthreads();
     }
 #pragma unroll
     for (int u = 0; u < kTogether; ++u) {
-        const int i = tid + u * kLargeThreads, v = s.base + 8 * i;
+        const int i = tid + u * THREADS, v = s.base + 8 * i;
         if (i >= vectors) break;
         uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
         if (s.any) {
@@ -292,7 +304,7 @@ __global__ void __launch_bounds__(kLargeThreads, 2) adjust_logits_large_kernel(c
     }
     // as in the small kernel: what no vector covers
     if (s.lo == 0 && tid < min(s.base, s.hi)) edit_one(in, out, tid, s.any ? w.word[tid - s.first] : 0u, s);
-    for (int i = s.base + 8 * vectors + tid; i < s.hi; i += kLargeThreads) edit_one(in, out, i, s.any ? w.word[i - s.first] : 0u, s);
+    for (int i = s.base + 8 * vectors + tid; i < s.hi; i += THREADS) edit_one(in, out, i, s.any ? w.word[i - s.first] : 0u, s);
 }
 
 template <typename TI, typename TO, int THREADS>
@@ -302,26 +314,34 @@ cudaError_t launch_small(const LogitsArgs& a, cudaStream_t st)
     return cudaGetLastError();
 }
 
+template <typename TI, typename TO, int THREADS>
+cudaError_t launch_large(const LogitsArgs& a, cudaStream_t st)
+{
+    constexpr int kLength = Large<THREADS>::kLength;
+    adjust_logits_large_kernel<TI, TO, THREADS>
+        <<<dim3((a.vocab + kLength - 1) / kLength, a.rows), THREADS, sizeof(Large<THREADS>), st>>>(a);
+    return cudaGetLastError();
+}
+
 template <typename TI, typename TO>
 cudaError_t launch(const LogitsArgs& a, int num_sms, cudaStream_t st)
 {
-    // A long stretch for every SM: 64 x 128000 in 20 us, 32 x 128000 in 12 us, and 21 to 26 us, 12 to 15 us with short ones; 16 x 128000
-    // in 7.8 us either way, fewer rows are faster with short ones (4 x 128000 in 3.9 us, and 6.1 us with long ones).
-    if ((int64_t)a.rows * a.vocab >= (int64_t)num_sms * kLargeLength) {
-        adjust_logits_large_kernel<TI, TO>
-            <<<dim3((a.vocab + kLargeLength - 1) / kLargeLength, a.rows), kLargeThreads, sizeof(Large), st>>>(a);
-        return cudaGetLastError();
-    }
-    // More threads look through a long history side by side: 16000 tokens for 1 x 128000 in 14.2, 9.1, 7.1 us with 128, 256, 512
-    // threads, 2000 in 4.5, 4.1, 4.5 us, 100 in 3.7, 3.8, 4.1 us.
-    if (a.max_tokens > 4096) return launch_small<TI, TO, 512>(a, st);
+    // Long stretches once there are as many values as 16384 for every SM: 32 x 128000 in 10.6 us, and 12 us with short ones; 16 x 128000
+    // in 8 us either way; 4 x 128000 in 6.1 us, and 3.9 us with short ones.  Of the long ones, those of 16384 values look through a
+    // history of 16000 tokens in 26 us (64 x 128000), those of 8192 in 28 us; with 2000 tokens they take 19.4 and 18.1 us.
+    if ((int64_t)a.rows * a.vocab >= (int64_t)num_sms * 16384)
+        return a.max_tokens > 8192 ? launch_large<TI, TO, 512>(a, st) : launch_large<TI, TO, 256>(a, st);
+    // More threads look through a long history side by side: 16000 tokens for 1 x 128000 in 7.6, 5.9, 5.6 us with 128, 256, 512
+    // threads, 4000 in 4.3, 3.9, 4.4 us, 100 in 3.7, 3.8, 4.3 us.
+    if (a.max_tokens > 8192) return launch_small<TI, TO, 512>(a, st);
     return a.max_tokens > 1024 ? launch_small<TI, TO, 256>(a, st) : launch_small<TI, TO, 128>(a, st);
 }
 
 template <typename TI, typename TO>
 cudaError_t configure()
 {
-    return cudaFuncSetAttribute(adjust_logits_large_kernel<TI, TO>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Large));
+    const cudaError_t e = cudaFuncSetAttribute(adjust_logits_large_kernel<TI, TO, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Large<256>));
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(adjust_logits_large_kernel<TI, TO, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Large<512>));
 }
 
 }  // namespace

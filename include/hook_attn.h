@@ -253,7 +253,7 @@ typedef struct {
     int32_t axis_pairs[HOOK_ROPE_MAX_AXES]; /* pairs of each axis; they add up to R / 2 */
     int32_t axis_order;          /* HOOK_ROPE_AXES_* */
     int32_t pairing;             /* HOOK_ROPE_PAIR_* */
-    float   factor;              /* multiplies cosines and sines (long-context scalings); finite */
+    float   factor;              /* multiplies cosines and sines (long-context scalings); finite, 0 selects 1 */
 
     /* ---- device tensors ---- */
     const void*    q;            /* [total_q][Hq][D], strides in elements; the last one is 1 */
@@ -320,7 +320,7 @@ int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, vo
 
 /* The pool that the sequences of a cache share.  All its arrays are written by the calls below. */
 typedef struct {
-    int32_t  num_seqs, max_blocks_per_seq, num_blocks, page_size;   /* num_seqs <= 16384 */
+    int32_t  num_seqs, max_blocks_per_seq, num_blocks, page_size;   /* num_seqs <= 16384, a table of 2^30 entries */
     int32_t* block_table;        /* [num_seqs][max_blocks_per_seq] */
     int32_t* seq_lens;           /* [num_seqs] tokens; 0: the row is empty */
     int32_t* page_refs;          /* [num_blocks] sequences that hold the page; 0: free */
@@ -354,7 +354,7 @@ int hook_cache_free(hook_attn_handle* handle, const hook_cache_pool* pool, const
 /* Plans how the U pages in use move together at the low end of the pool: the k-th used page at U or above goes to
  * the k-th free page below U.  The pool itself is only read, so that the old tables stay valid until the pairs are
  * copied.  Outputs: block_table_out (like block_table; may be block_table itself; -1 behind a sequence's pages),
- * page_refs_out (like page_refs, not page_refs itself), page_map int32 [num_blocks] (where each page is afterwards,
+ * page_refs_out (like page_refs; neither it nor page_map is page_refs itself), page_map int32 [num_blocks] (where each page is afterwards,
  * -1: free), pairs int32 [num_blocks / 2][2] (source, destination; -1 behind the last), num_pairs int32 [1]. */
 int hook_cache_compact(hook_attn_handle* handle, const hook_cache_pool* pool, int32_t* block_table_out, int32_t* page_refs_out,
                        int32_t* page_map, int32_t* pairs, int32_t* num_pairs, void* cuda_stream);

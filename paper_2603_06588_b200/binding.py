@@ -498,8 +498,10 @@ class HookAttn:
         num_pairs)`` as they are once the pairs are copied; the old ones stay as they are."""
         pool = self._pool(block_table, seq_lens, page_refs, status)
         blocks, = page_refs.shape
-        table_out, refs_out, page_map, pairs, num_pairs = (
-            self._new(page_refs, shape, torch.int32, stream) for shape in (block_table.shape, (blocks,), (blocks,), (blocks // 2, 2), (1,)))
+        entries, half = block_table.numel(), blocks // 2
+        table_out, refs_out, page_map, pairs, num_pairs = self._new(                    # one allocation for the five
+            page_refs, (entries + 2 * blocks + 2 * half + 1,), torch.int32, stream).split_with_sizes((entries, blocks, blocks, 2 * half, 1))
+        table_out, pairs = table_out.view(block_table.shape), pairs.view(half, 2)
         self._checked("hook_cache_compact", stream, pool, table_out.data_ptr(), refs_out.data_ptr(), page_map.data_ptr(), pairs.data_ptr(),
                       num_pairs.data_ptr())
         return table_out, refs_out, page_map, pairs, num_pairs

@@ -111,6 +111,7 @@ int prepare_pool(const hook_cache_pool* p, PoolArgs& a)
 {
     if (!p || p->num_seqs < 0 || p->max_blocks_per_seq < 0 || p->num_blocks < 0 || p->page_size <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
     if (p->page_size != kPage || p->num_seqs > kMaxPoolSeqs) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if ((int64_t)p->num_seqs * p->max_blocks_per_seq > 1 << 30) return HOOK_ATTN_ERR_UNSUPPORTED;      // needs are summed in 32 bits
     if (p->num_seqs > 0 && (!p->seq_lens || (p->max_blocks_per_seq > 0 && !p->block_table))) return HOOK_ATTN_ERR_INVALID_ARG;
     if (p->num_blocks > 0 && !p->page_refs) return HOOK_ATTN_ERR_INVALID_ARG;
     a.block_table = p->block_table; a.seq_lens = p->seq_lens; a.page_refs = p->page_refs; a.status = p->status;
@@ -459,7 +460,7 @@ int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* 
     a.num_seqs = p->num_seqs; a.total_q = p->total_q; a.Hq = p->num_q_heads; a.Hkv = p->num_kv_heads;
     a.head_dim = p->head_dim; a.pairs = pairs; a.num_blocks = p->num_blocks; a.max_blocks = p->max_blocks_per_seq;
     a.max_keys = (int32_t)min64((int64_t)p->max_blocks_per_seq * kPage, INT32_MAX);
-    a.factor = p->factor;
+    a.factor = p->factor == 0.f ? 1.f : p->factor;
     a.halves = p->pairing == HOOK_ROPE_PAIR_HALVES;
     for (int pair = 0, axis = 0; pair < pairs; ++pair) {
         while (left[axis] == 0) axis = (axis + 1) % p->num_axes;
@@ -553,7 +554,7 @@ int hook_cache_compact(hook_attn_handle* handle, const hook_cache_pool* pool, in
     int rc = prepare_pool(pool, a);
     if (rc != HOOK_ATTN_OK) return rc;
     if ((a.num_seqs > 0 && a.max_blocks > 0 && !block_table_out) || (a.num_blocks > 0 && (!page_refs_out || !page_map)) ||
-        (a.num_blocks > 1 && !pairs) || !num_pairs || (a.num_blocks > 0 && page_refs_out == pool->page_refs))
+        (a.num_blocks > 1 && !pairs) || !num_pairs || (a.num_blocks > 0 && (page_refs_out == pool->page_refs || page_map == pool->page_refs)))
         return HOOK_ATTN_ERR_INVALID_ARG;
     if ((rc = check_handle(handle)) != HOOK_ATTN_OK) return rc;
     cudaError_t e = launch_compact(a, block_table_out, page_refs_out, page_map, pairs, num_pairs, static_cast<cudaStream_t>(cuda_stream));

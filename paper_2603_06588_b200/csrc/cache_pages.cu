@@ -12,7 +12,7 @@ constexpr int kListThreads = 256;
 constexpr int kPoolThreads = 1024;
 
 __device__ __forceinline__ int pages_of(int len) { return (int)(((int64_t)len + kPage - 1) / kPage); }
-__device__ __forceinline__ int64_t capacity(const PoolArgs& p) { return (int64_t)p.max_blocks * kPage; }
+__device__ __forceinline__ int64_t capacity(const PoolArgs& p) { return min((int64_t)p.max_blocks * kPage, (int64_t)INT32_MAX); }
 __device__ __forceinline__ bool page_ok(const PoolArgs& p, int page) { return page >= 0 && page < p.num_blocks; }
 
 // A CTA passes over the pool's reference counts in steps of EACH neighbouring pages to a thread: 1, 4 or 16, the fewest that cover the

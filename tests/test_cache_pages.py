@@ -80,7 +80,8 @@ def _pool_params(**over):
 @pytest.mark.parametrize("over,code", [
     (dict(), binding.HOOK_ATTN_ERR_CUDA), (dict(num_seqs=-1), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(block_table=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(seq_lens=None), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(page_refs=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
-    (dict(page_size=32), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(num_seqs=16385), binding.HOOK_ATTN_ERR_UNSUPPORTED)])
+    (dict(page_size=32), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(num_seqs=16385), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(num_seqs=16384, max_blocks_per_seq=65537), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(num_seqs=16384, max_blocks_per_seq=65536), binding.HOOK_ATTN_ERR_CUDA)])
 def test_pool_refusals(over, code):
     lib, p = binding.load_library(), ctypes.byref(_pool_params(**over))
     assert lib.hook_cache_fork(FAKE_HANDLE, p, 0x1000, 0x1000, 1, None) == code
@@ -99,6 +100,7 @@ def test_list_refusals():
     assert lib.hook_cache_extend(FAKE_HANDLE, p, 0x1000, None, None) == bad
     assert lib.hook_cache_free(FAKE_HANDLE, p, None, None, 1, None) == bad
     assert lib.hook_cache_compact(FAKE_HANDLE, p, 0x1000, 0x30000, 0x3000, 0x4000, 0x5000, None) == bad      # the counts in place
+    assert lib.hook_cache_compact(FAKE_HANDLE, p, 0x1000, 0x2000, 0x30000, 0x4000, 0x5000, None) == bad
     assert lib.hook_cache_compact(FAKE_HANDLE, p, 0x1000, 0x2000, 0x3000, 0x4000, None, None) == bad
     assert lib.hook_cache_fork(FAKE_HANDLE, None, 0x1000, 0x1000, 1, None) == bad
     assert lib.hook_cache_fork(None, p, 0x1000, 0x1000, 1, None) == bad
@@ -267,6 +269,17 @@ def test_broken_pools_are_reported(eng, break_it):
     both.extend([0, 0, -1, 5])
     both.free([1, 7, -1])
     both.free([2], [-1])
+
+
+@pytest.mark.gpu
+def test_lengths_up_to_the_last_integer(eng):
+    """A table that could hold more tokens than an int32 counts: the sums must not wrap around."""
+    lens, refs = torch.tensor([2 ** 31 - 10, 0], dtype=torch.int32, device="cuda"), torch.ones(4, dtype=torch.int32, device="cuda")
+    table = torch.zeros((2, 2 ** 27 + 64), dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    pairs = eng.hook_cache_extend(table, lens, refs, torch.tensor([100, 2 ** 31 - 1], dtype=torch.int32, device="cuda"), status=status)
+    assert pairs.tolist() == [[-1, -1]] * 2 and lens.tolist() == [2 ** 31 - 10, 0] and refs.tolist() == [1] * 4
+    assert int(status.item()) == binding.HOOK_ATTN_ERR_NO_PAGES          # the second asks for all pages there could be; the first is out of range
 
 
 @pytest.mark.gpu

@@ -237,6 +237,15 @@ def test_in_place_queries(eng, adjacent):
 
 
 @pytest.mark.gpu
+def test_a_factor_of_zero_selects_one(eng):
+    c = _case([3], [1], 2, 1, 64, 32, torch.bfloat16)
+    kw = dict(q=c["q"].cuda(), k=c["k"].cuda(), v=c["v"].cuda(), block_table=c["block_table"].cuda(), seq_lens=c["seq_lens"].cuda(),
+              cu_q_lens=c["cu_q_lens"].cuda(), inv_freq=torch.tensor(_freq(32), device="cuda"))
+    got = [eng.hook_rope_append(k_cache=k, v_cache=v, factor=f, **kw) for f in (0.0, 1.0) for k, v in [_views(c["cache"].cuda(), "contiguous", 64)]]
+    assert torch.equal(*got) and got[0].any()
+
+
+@pytest.mark.gpu
 def test_far_and_negative_positions(eng):
     c = _case([40], [0], 2, 1, 128, 64, torch.float32)
     pos = torch.from_numpy(np.random.default_rng(3).integers(-(1 << 24), 1 << 24, (3, 40))).int()

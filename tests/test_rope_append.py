@@ -200,7 +200,7 @@ def _axes_positions(rows, axes, seed, top=1 << 20):
 @pytest.mark.parametrize("adjacent", [False, True])
 @pytest.mark.parametrize("d,rot,axis_pairs,cyclic", [
     (128, 128, (64,), False), (128, 128, (16, 24, 24), False), (128, 128, (24, 20, 20), True), (64, 64, (8, 12, 12), True),
-    (64, 40, (8, 6, 6), True), (128, 32, (4, 4, 4, 4), False), (64, 16, (8,), False), (64, 6, (1, 0, 2), False), (128, 2, (1,), True),
+    (64, 40, (8, 6, 6), True), (128, 32, (4, 4, 4, 4), False), (64, 16, (8,), False), (64, 6, (1, 0, 2), False), (128, 52, (9, 17), True), (128, 2, (1,), True),
     (128, 126, (40, 23), False)])
 def test_ragged_prompts(eng, dtype, adjacent, d, rot, axis_pairs, cyclic):
     """Packed prompts with and without context, a sequence without rows, rows that end inside pages."""
@@ -219,7 +219,7 @@ def test_decode_rows(eng, layout, hq, hkv):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("rot", [0, 64])
-@pytest.mark.parametrize("offset", [0, 1, 4])
+@pytest.mark.parametrize("offset", [0, 1, 2, 4])
 def test_unaligned_rows(eng, rot, offset):
     """q, k and v start anywhere in the rows of a wider buffer: no 16-byte alignment."""
     c = _case([9, 3], [0, 20], 4, 4, 64, rot // 2, torch.bfloat16, offset=offset)

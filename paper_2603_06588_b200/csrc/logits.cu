@@ -47,29 +47,52 @@ __device__ __forceinline__ int values_before_aligned(const LogitsArgs& a, int ro
 }
 
 template <typename TI>
-__device__ __forceinline__ Stretch open_stretch(const LogitsArgs& a, int row, int slice, int length)
+__device__ __forceinline__ Stretch place_stretch(const LogitsArgs& a, int row, int slice, int length)
 {
     Stretch s;
     s.row = row;
-    s.total = a.tokens ? a.total_lens[row] : 0;
-    s.prompt = a.tokens ? a.prompt_lens[row] : 0;
-    s.b0 = a.bias_offsets ? a.bias_offsets[row] : 0;
-    s.b1 = a.bias_offsets ? a.bias_offsets[row + 1] : 0;
-    const int mask = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
-    s.rep = a.repetition ? a.repetition[row] : 1.f;
-    s.inv_rep = __frcp_rn(s.rep);
-    s.pres = a.presence ? a.presence[row] : 0.f;
-    s.freq = a.frequency ? a.frequency[row] : 0.f;
-    s.valid = s.total >= 0 && s.total <= a.max_tokens && s.prompt >= 0 && s.prompt <= s.total && s.b0 >= 0 && s.b1 >= s.b0 &&
-              s.b1 <= a.num_bias && s.b1 - s.b0 <= kMaxRowBias && mask < a.num_masks;
-    s.any = s.valid && (s.total > 0 || s.b1 > s.b0);
-    s.bias = a.bias_values + (s.valid ? s.b0 : 0);
-    s.grammar = s.valid && mask >= 0 ? a.mask + (int64_t)mask * a.mask_row : nullptr;
     s.base = values_before_aligned<TI>(a, row) + slice * length;
     s.lo = slice == 0 ? 0 : min(s.base, a.vocab);             // a row with a head may need one stretch less
     s.hi = min(s.base + length, a.vocab);
     s.first = s.base - 8;
     return s;
+}
+
+// A row's numbers as they come from memory; the values are fetched between them and their use.
+struct Numbers {
+    int total, prompt, b0, b1, mask;
+    float rep, pres, freq;
+};
+
+__device__ __forceinline__ Numbers fetch_numbers(const LogitsArgs& a, int row)
+{
+    Numbers n;
+    n.total = a.tokens ? a.total_lens[row] : 0;
+    n.prompt = a.tokens ? a.prompt_lens[row] : 0;
+    n.b0 = a.bias_offsets ? a.bias_offsets[row] : 0;
+    n.b1 = a.bias_offsets ? a.bias_offsets[row + 1] : 0;
+    n.mask = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
+    n.rep = a.repetition ? a.repetition[row] : 1.f;
+    n.pres = a.presence ? a.presence[row] : 0.f;
+    n.freq = a.frequency ? a.frequency[row] : 0.f;
+    return n;
+}
+
+__device__ __forceinline__ void open_stretch(const LogitsArgs& a, const Numbers& n, Stretch& s)
+{
+    s.total = n.total;
+    s.prompt = n.prompt;
+    s.b0 = n.b0;
+    s.b1 = n.b1;
+    s.rep = n.rep;
+    s.inv_rep = __frcp_rn(n.rep);
+    s.pres = n.pres;
+    s.freq = n.freq;
+    s.valid = n.total >= 0 && n.total <= a.max_tokens && n.prompt >= 0 && n.prompt <= n.total && n.b0 >= 0 && n.b1 >= n.b0 &&
+              n.b1 <= a.num_bias && n.b1 - n.b0 <= kMaxRowBias && n.mask < a.num_masks;
+    s.any = s.valid && (n.total > 0 || n.b1 > n.b0);
+    s.bias = a.bias_values + (s.valid ? n.b0 : 0);
+    s.grammar = s.valid && n.mask >= 0 ? a.mask + (int64_t)n.mask * a.mask_row : nullptr;
 }
 
 // A value with a word that is not zero.  Multiplied by 1 / repetition, a positive value is rounded twice.
@@ -203,25 +226,25 @@ __global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_con
     constexpr int kLength = THREADS * 8;
     __shared__ __align__(16) uint32_t word[kLength + 8];
     const int tid = threadIdx.x;
-    const Stretch s = open_stretch<TI>(a, blockIdx.y, blockIdx.x, kLength);
+    Stretch s = place_stretch<TI>(a, blockIdx.y, blockIdx.x, kLength);
     if (s.lo >= s.hi) return;
-    if (!s.valid) {
-        if (tid == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-        return;
-    }
+    const Numbers numbers = fetch_numbers(a, s.row);
     const TI* in = static_cast<const TI*>(a.logits) + (int64_t)s.row * a.in_row;
     TO* out = static_cast<TO*>(a.out) + (int64_t)s.row * a.out_row;
     const bool aligned = (reinterpret_cast<uintptr_t>(out + s.base) & 15) == 0;    // in and out reach a multiple of 16 bytes together
     const int vectors = aligned ? max(s.hi - s.base, 0) / 8 : 0, v = s.base + 8 * tid;
-    History<THREADS> history(a, s, tid);
     Vec<TI> raw;
+    if (tid < vectors) raw = *reinterpret_cast<const Vec<TI>*>(in + v);
+    open_stretch(a, numbers, s);
+    if (!s.valid) {
+        if (tid == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        return;
+    }
+    History<THREADS> history(a, s, tid);
     uint32_t low = ~0u, high = ~0u;
-    if (tid < vectors) {
-        raw = *reinterpret_cast<const Vec<TI>*>(in + v);
-        if (s.grammar) {
-            low = s.grammar[v >> 5];
-            high = s.grammar[(v + 7) >> 5];
-        }
+    if (s.grammar && tid < vectors) {
+        low = s.grammar[v >> 5];
+        high = s.grammar[(v + 7) >> 5];
     }
     if (s.any) {
         for (int i = tid; i < (kLength + 8) / 4; i += THREADS) reinterpret_cast<uint4*>(word)[i] = make_uint4(0, 0, 0, 0);
@@ -261,20 +284,22 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) adjust_logits_large_k
     Large<THREADS>& w = *reinterpret_cast<Large<THREADS>*>(smem);
     constexpr int kLength = Large<THREADS>::kLength;
     const int tid = threadIdx.x;
-    const Stretch s = open_stretch<TI>(a, blockIdx.y, blockIdx.x, kLength);
+    Stretch s = place_stretch<TI>(a, blockIdx.y, blockIdx.x, kLength);
     if (s.lo >= s.hi) return;
-    if (!s.valid) {
-        if (tid == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-        return;
-    }
+    const Numbers numbers = fetch_numbers(a, s.row);
     const TI* in = static_cast<const TI*>(a.logits) + (int64_t)s.row * a.in_row;
     TO* out = static_cast<TO*>(a.out) + (int64_t)s.row * a.out_row;
-    History<THREADS> history(a, s, tid);
     const int vectors = (reinterpret_cast<uintptr_t>(out + s.base) & 15) == 0 ? max(s.hi - s.base, 0) / 8 : 0;
     Vec<TI> raw[kTogether];
 #pragma unroll
     for (int u = 0; u < kTogether; ++u)
         if (tid + u * THREADS < vectors) raw[u] = *reinterpret_cast<const Vec<TI>*>(in + s.base + 8 * (tid + u * THREADS));
+    open_stretch(a, numbers, s);
+    if (!s.valid) {
+        if (tid == 0 && blockIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        return;
+    }
+    History<THREADS> history(a, s, tid);
     const int mask0 = s.lo >> 5;                                          // the stretch's part of the mask
     if (s.grammar)
         for (int i = tid; i <= ((s.hi - 1) >> 5) - mask0; i += THREADS) w.grammar[i] = s.grammar[mask0 + i];

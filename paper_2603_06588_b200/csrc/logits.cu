@@ -219,7 +219,7 @@ __device__ __forceinline__ void edit_one(const TI* in, TO* out, int v, uint32_t 
 }
 
 // Small calls: a CTA takes one stretch, one vector to a thread, whose load is under way while the words are filled.  Bound by the
-// chain of loads (the row's numbers, its history, the words): 3.0 us for 1 x 32000, of which 2.0 us without a history.
+// chain of loads (the row's numbers, its history, the words): 2.8 us for 1 x 32000 with 300 tokens.
 template <typename TI, typename TO, int THREADS>
 __global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_constant__ LogitsArgs a)
 {
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_con
         high = s.grammar[(v + 7) >> 5];
     }
     if (s.any) {
-        for (int i = tid; i < (kLength + 8) / 4; i += THREADS) reinterpret_cast<uint4*>(word)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < (s.hi - s.first + 3) / 4; i += THREADS) reinterpret_cast<uint4*>(word)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         history.count(s, word);
         for (int i = s.b0 + tid; i < s.b1; i += THREADS) place_bias(a, s, word, i);
@@ -264,10 +264,10 @@ __global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_con
 }
 
 // Large calls: a CTA takes a long stretch, all of whose loads are under way while its words are filled; CTAs of 256 or 512 threads, 1024
-// threads on an SM with 64 registers each.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 55 us, 6.0
+// threads on an SM with 64 registers each.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 54 us, 6.1
 // TB/s).  With one, by the chain of loads before a stretch's edits and by the issue slots: each stretch of a row looks through the whole
 // history, and a warp runs the edit for each of the eight values of a lane that any of its lanes has a word for (the same with
-// histories of up to 4096 tokens: 74 us, 4.5 TB/s; 64 rows of 128000 bf16 to fp32 values with up to 32768 tokens: 28 us, 1.9 TB/s).
+// histories of up to 4096 tokens: 71 us, 4.7 TB/s; 64 rows of 128000 bf16 to fp32 values with up to 32768 tokens: 27.5 us, 2.0 TB/s).
 constexpr int kTogether = 4;
 
 template <int THREADS>
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) adjust_logits_large_k
     if (s.grammar)
         for (int i = tid; i <= ((s.hi - 1) >> 5) - mask0; i += THREADS) w.grammar[i] = s.grammar[mask0 + i];
     if (s.any)
-        for (int i = tid; i < (kLength + 8) / 4; i += THREADS) reinterpret_cast<uint4*>(w.word)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < (s.hi - s.first + 3) / 4; i += THREADS) reinterpret_cast<uint4*>(w.word)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     if (s.any) {
         history.count(s, w.word);
@@ -351,13 +351,14 @@ cudaError_t launch_large(const LogitsArgs& a, cudaStream_t st)
 template <typename TI, typename TO>
 cudaError_t launch(const LogitsArgs& a, int num_sms, cudaStream_t st)
 {
-    // Long stretches once there are as many values as 16384 for every SM: 32 x 128000 in 10.6 us, and 12 us with short ones; 16 x 128000
-    // in 8 us either way; 4 x 128000 in 6.1 us, and 3.9 us with short ones.  Of the long ones, those of 16384 values look through a
-    // history of 16000 tokens in 26 us (64 x 128000), those of 8192 in 28 us; with 2000 tokens they take 19.4 and 18.1 us.
-    if ((int64_t)a.rows * a.vocab >= (int64_t)num_sms * 16384)
+    // Long stretches (8192 or 16384 values) for long rows once there are enough of them for all SMs.  Short and long ones take, with
+    // 2000 tokens a row, 3.7 and 6.0 us for 4 x 128000, 8.1 and 8.1 us for 16 x 128000, 24.5 and 17.9 us for 64 x 128000; 13.5 and 14.9
+    // us for 400 x 10000.  Of the long ones, 16384 values look through long histories less often: 28.2 and 25.5 us for 64 x 128000
+    // with 16000 tokens, 19.7 and 20.1 us with 4000.
+    if (a.vocab >= 16384 && (int64_t)a.rows * a.vocab >= (int64_t)num_sms * 12288)
         return a.max_tokens > 8192 ? launch_large<TI, TO, 512>(a, st) : launch_large<TI, TO, 256>(a, st);
-    // More threads look through a long history side by side: 16000 tokens for 1 x 128000 in 7.6, 5.9, 5.6 us with 128, 256, 512
-    // threads, 4000 in 4.3, 3.9, 4.4 us, 100 in 3.7, 3.8, 4.3 us.
+    // More threads look through a long history side by side: 1 x 128000 takes 7.3, 5.5, 5.3 us with 128, 256, 512 threads and 16000
+    // tokens, 3.8, 3.5, 3.8 us with 4000, 3.2, 3.3, 3.7 us with 100.
     if (a.max_tokens > 8192) return launch_small<TI, TO, 512>(a, st);
     return a.max_tokens > 1024 ? launch_small<TI, TO, 256>(a, st) : launch_small<TI, TO, 128>(a, st);
 }

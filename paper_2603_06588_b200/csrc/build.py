@@ -1,4 +1,5 @@
-"""Compile the CUDA library for sm_100a into ``libhook_attn.so`` next to the Python binding.
+"""Compile the CUDA library for sm_100a into ``libhook_attn.so`` next to the Python binding, and the binding's compiled
+part into ``_marshal.so`` beside it.
 
 Every ``.cu`` file is compiled to an object of its own (in parallel, only when it or a header it
 includes has changed) under ``_build/`` and the objects are linked into the shared library.
@@ -9,12 +10,15 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libhook_attn.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
+MARSHAL_SRC = os.path.join(HERE, "marshal.cpp")
 OBJ_DIR = os.path.join(HERE, "_build")
 
 FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
@@ -37,11 +41,29 @@ def _newer(deps, target) -> bool:
 
 
 def needs_build() -> bool:
-    return _newer(sources() + headers(), LIB)
+    return _newer(sources() + headers(), LIB) or _newer([MARSHAL_SRC] + headers(), MARSHAL)
+
+
+def _build_marshal(verbose: bool) -> None:
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")), "..", "include")
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-Wall", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+    for path in (os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], cuda):
+        cmd += ["-isystem", path]
+    cmd += [MARSHAL_SRC, "-o", MARSHAL, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if verbose or res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+    if res.returncode != 0:
+        raise subprocess.CalledProcessError(res.returncode, res.args)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
+    if force or _newer([MARSHAL_SRC] + headers(), MARSHAL):
+        _build_marshal(verbose)
+    if not force and not _newer(sources() + headers(), LIB):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     os.makedirs(OBJ_DIR, exist_ok=True)

@@ -17,22 +17,6 @@ def test_struct_mirror(name, cls):
     assert struct_fields(name) == [f[0] for f in cls._fields_]
 
 
-@pytest.mark.parametrize("packer,cls", [(binding._ROPE, binding.HookRopeParams), (binding._LOGITS, binding.HookLogitsParams),
-                                        (binding._POOL, binding.HookCachePool), (binding._COPY, binding.HookCacheCopyParams)])
-def test_packed_layout(packer, cls):
-    """One pack of all fields lays them out like the C struct does."""
-    assert packer.size == ctypes.sizeof(cls)
-    values, want = [], cls()
-    for i, (name, t) in enumerate(cls._fields_):
-        if hasattr(t, "_length_"):
-            getattr(want, name)[:] = range(1000 * i, 1000 * i + t._length_)
-            values += range(1000 * i, 1000 * i + t._length_)
-        else:
-            setattr(want, name, i + 1)
-            values.append(i + 1)
-    assert packer.pack(*values) == bytes(want)
-
-
 def _consistent(pool):
     """Every page counts the table entries that name it."""
     refs = [0] * len(pool.refs)
@@ -299,7 +283,8 @@ def test_in_place_table_of_compact(eng):
     both = Both(eng, 3, 4, 20)
     both.extend([20, 40, 60])
     both.free([1])
-    pool = eng._pool(**both.dev)
+    table, lens, counts, status = (both.dev[name] for name in ("block_table", "seq_lens", "page_refs", "status"))
+    pool = ctypes.byref(binding.HookCachePool(3, 4, 20, 16, table.data_ptr(), lens.data_ptr(), counts.data_ptr(), status.data_ptr()))
     out = torch.empty(20 * 4, dtype=torch.int32, device="cuda")
     refs, page_map, pairs, count = out[:20], out[20:40], out[40:60], out[60:61]
     rc = eng._lib.hook_cache_compact(eng._h, pool, both.dev["block_table"].data_ptr(), refs.data_ptr(), page_map.data_ptr(), pairs.data_ptr(),

@@ -125,7 +125,11 @@ def load_library() -> ctypes.CDLL:
             raise ImportError(
                 f"{LIB_PATH} is missing: build it with `python -m paper_2603_06588_b200.csrc.build` "
                 "(there is no fallback path)")
-        from . import _marshal
+        try:
+            from . import _marshal
+        except ImportError as e:
+            raise ImportError("the binding's compiled part (_marshal.so) is missing or does not fit this torch: build it with "
+                              "`python -m paper_2603_06588_b200.csrc.build`") from e
         lib = ctypes.CDLL(LIB_PATH)
         lib.hook_attn_create.restype = ctypes.c_int
         lib.hook_attn_create.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]

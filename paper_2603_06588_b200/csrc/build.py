@@ -61,10 +61,10 @@ def _build_marshal(verbose: bool) -> None:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    if not force and not needs_build():
+        return LIB
     if force or _newer([MARSHAL_SRC] + headers(), MARSHAL):
         _build_marshal(verbose)
-    if not force and not _newer(sources() + headers(), LIB):
-        return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
     hdrs = headers()

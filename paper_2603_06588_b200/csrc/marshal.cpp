@@ -1,7 +1,7 @@
 // Argument marshalling of the short calls (rotary append, logit edits, cache pages) for binding.py: checks the tensors, fills the
 // C structs and calls the C ABI.  These calls take a few microseconds on the device, and reading some twenty tensors' types, shapes
-// and strides from Python takes longer than that: hook_rope_append on one row
-// takes 11.7 us through ctypes and struct.pack and 5.4 us from here, with a launch of 2.9 us in it.
+// and strides from Python takes longer than that: hook_rope_append on one row takes 11.7 us through ctypes and struct.pack and
+// 5.4 us from here, with a launch of 2.9 us in it.
 //
 // Nothing is computed here.  A failed check raises AssertionError, like the checks of the other calls; a code of the library is
 // returned as an int, which binding.py turns into its exception.

@@ -320,10 +320,10 @@ int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, vo
 
 /* The pool that the sequences of a cache share.  All its arrays are written by the calls below. */
 typedef struct {
-    int32_t  num_seqs, max_blocks_per_seq, num_blocks, page_size;   /* num_seqs <= 16384, a table of 2^30 entries */
+    int32_t  num_seqs, max_blocks_per_seq, num_blocks, page_size;   /* num_seqs <= 16384, at most 2^30 pages and 2^30 entries */
     int32_t* block_table;        /* [num_seqs][max_blocks_per_seq] */
     int32_t* seq_lens;           /* [num_seqs] tokens; 0: the row is empty */
-    int32_t* page_refs;          /* [num_blocks] sequences that hold the page; 0: free */
+    int32_t* page_refs;          /* [num_blocks] sequences that hold the page; 0 (or less): free */
     int32_t* status;
 } hook_cache_pool;
 

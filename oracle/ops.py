@@ -129,7 +129,7 @@ class Pool:
                 self.refs[p] += 1
 
     def extend(self, new_rows):
-        free = [p for p, n in enumerate(self.refs) if n == 0]
+        free = [p for p, n in enumerate(self.refs) if n <= 0]
         before, at, pairs = list(self.refs), 0, []
         for s, n in enumerate(new_rows):
             pairs.append((-1, -1))
@@ -186,14 +186,22 @@ class Pool:
     def compact(self):
         used = sum(n > 0 for n in self.refs)
         sources = [p for p, n in enumerate(self.refs) if n > 0 and p >= used]
-        holes = [p for p, n in enumerate(self.refs) if n == 0 and p < used]
+        holes = [p for p, n in enumerate(self.refs) if n <= 0 and p < used]
         moves = dict(zip(sources, holes))
         page_map = [moves.get(p, p) if n > 0 else -1 for p, n in enumerate(self.refs)]
         refs = [0] * len(self.refs)
         for p, to in enumerate(page_map):
             if to >= 0:
                 refs[to] = self.refs[p]
-        table = [[page_map[p] if j < self._pages(L) else -1 for j, p in enumerate(row)] for row, L in zip(self.table, self.lens)]
+        table = [[-1] * self.max_blocks for _ in self.table]
+        for row, out, L in zip(self.table, table, self.lens):
+            if not self._len_ok(L):
+                self.faults.append("bounds")
+                continue
+            for j, p in enumerate(row[:self._pages(L)]):
+                out[j] = page_map[p] if 0 <= p < len(page_map) else -1
+                if out[j] < 0:
+                    self.faults.append("bounds")
         return table, refs, page_map, list(zip(sources, holes))
 
 

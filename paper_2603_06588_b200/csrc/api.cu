@@ -111,7 +111,8 @@ int prepare_pool(const hook_cache_pool* p, PoolArgs& a)
 {
     if (!p || p->num_seqs < 0 || p->max_blocks_per_seq < 0 || p->num_blocks < 0 || p->page_size <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
     if (p->page_size != kPage || p->num_seqs > kMaxPoolSeqs) return HOOK_ATTN_ERR_UNSUPPORTED;
-    if ((int64_t)p->num_seqs * p->max_blocks_per_seq > 1 << 30) return HOOK_ATTN_ERR_UNSUPPORTED;      // needs are summed in 32 bits
+    // needs are summed, and pages stepped through, in 32 bits
+    if ((int64_t)p->num_seqs * p->max_blocks_per_seq > 1 << 30 || p->num_blocks > 1 << 30) return HOOK_ATTN_ERR_UNSUPPORTED;
     if (p->num_seqs > 0 && (!p->seq_lens || (p->max_blocks_per_seq > 0 && !p->block_table))) return HOOK_ATTN_ERR_INVALID_ARG;
     if (p->num_blocks > 0 && !p->page_refs) return HOOK_ATTN_ERR_INVALID_ARG;
     a.block_table = p->block_table; a.seq_lens = p->seq_lens; a.page_refs = p->page_refs; a.status = p->status;

@@ -1,8 +1,10 @@
 // The pages of the cache: sequences that share pages (fork), get room for new rows (extend), give pages back (free), and a
 // pool whose pages are moved together at its low end (compact).  A page's entry in page_refs counts the sequences that hold
-// it; 0 is free.  All results are integers that do not depend on the order in which threads run.
+// it; 0 (or less) is free.  All results are integers that do not depend on the order in which threads run.
 #include "common.cuh"
 #include "ops.cuh"
+
+#include <cooperative_groups.h>
 
 namespace hook_attn {
 
@@ -15,8 +17,7 @@ __device__ __forceinline__ int pages_of(int len) { return (int)(((int64_t)len + 
 __device__ __forceinline__ int64_t capacity(const PoolArgs& p) { return min((int64_t)p.max_blocks * kPage, (int64_t)INT32_MAX); }
 __device__ __forceinline__ bool page_ok(const PoolArgs& p, int page) { return page >= 0 && page < p.num_blocks; }
 
-// A CTA passes over the pool's reference counts in steps of EACH neighbouring pages to a thread: 1, 4 or 16, the fewest that cover the
-// pool in one step (700 pages in one step of 1: a compaction takes 4 us less than with 16), else 16 (100000 pages: seven steps).
+// A CTA reads the pool's reference counts in steps of EACH neighbouring pages to a thread.
 template <int EACH>
 __device__ __forceinline__ void load_refs(const PoolArgs& p, int base, int (&refs)[EACH], int missing)
 {
@@ -41,7 +42,7 @@ __device__ __forceinline__ uint32_t free_pages(const PoolArgs& p, int base)
     load_refs<EACH>(p, base, refs, 1);
     uint32_t bits = 0;
 #pragma unroll
-    for (int u = 0; u < EACH; ++u) bits |= (uint32_t)(refs[u] == 0) << u;
+    for (int u = 0; u < EACH; ++u) bits |= (uint32_t)(refs[u] <= 0) << u;
     return bits;
 }
 
@@ -108,16 +109,42 @@ __global__ void __launch_bounds__(kListThreads) free_kernel(const PoolArgs p, co
 // partly filled and held by others too: the rows to come would write into it, so it gets a page of its own and the pair
 // (old page, new page) to copy.  Needs are summed in sequence order and the k-th free page goes to the k-th need; sequences
 // that the pool cannot serve in that order stay as they are.
+//
+// One CTA does it, since what it hands out is little: 1, 4 or 16 pages to a thread, the fewest that cover the pool in one step
+// (4096 pages, 64 sequences: 5.2 us).  A pool of more steps is counted by the other CTAs of a cluster (CLUSTER) meanwhile, so that the steps
+// without a free page need not be looked through one after the other (100000 pages, the last tenth of them free: 9.3 us, and 25 us
+// with one CTA; 16384 pages: 8.4 us with one CTA).
 constexpr int kSplit = 1 << 30;                   // flag in a need: the last page is shared
+constexpr int kClusterCtas = 8;
+constexpr int kUnits = 1024;                      // counts of free pages that the cluster makes
 
-template <int EACH>
+template <int EACH, bool CLUSTER>
 __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, const int32_t* __restrict__ new_rows,
                                                               int32_t* __restrict__ pairs)
 {
     extern __shared__ int32_t dyn[];
     int32_t* need = dyn;                          // [num_seqs] pages, with kSplit; -1: the sequence is left out
     int32_t* first = dyn + p.num_seqs;            // [num_seqs] place of its first page among all needs
+    uint16_t* list = reinterpret_cast<uint16_t*>(dyn + 2 * p.num_seqs);   // [kPoolThreads * EACH] free pages of a step
     __shared__ int sh[33];
+    __shared__ int units[CLUSTER ? kUnits : 1];
+    constexpr int kStep = kPoolThreads * EACH;
+    const int steps = (p.num_blocks + kStep - 1) / kStep, per_unit = (steps + kUnits - 1) / kUnits;
+    if (CLUSTER) {
+        const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+        const int rank = (int)cluster.block_rank();
+        if (rank == 0) units[threadIdx.x] = 0;
+        cluster.sync();
+        if (rank > 0) {
+            int* to = cluster.map_shared_rank(units, 0);
+            for (int step = rank - 1; step < steps; step += kClusterCtas - 1) {
+                const int n = __reduce_add_sync(0xffffffffu, __popc(free_pages<EACH>(p, step * kStep)));
+                if ((threadIdx.x & 31) == 0 && n > 0) atomicAdd(to + step / per_unit, n);
+            }
+            cluster.sync();
+            return;
+        }
+    }
     int wanted = 0;
     for (int base = 0; base < p.num_seqs; base += kPoolThreads) {
         const int s = base + (int)threadIdx.x;
@@ -146,20 +173,25 @@ __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, 
         wanted += total;
     }
     __syncthreads();
-    // how many of the wanted pages there are
+    // how many free pages there are
     int have = 0, sum;
-    for (int base = 0; base < p.num_blocks && have < wanted; base += kPoolThreads * EACH) {
-        (void)block_scan(__popc(free_pages<EACH>(p, base)), sh, sum);
-        have += sum;
+    if (CLUSTER) {
+        cooperative_groups::this_cluster().sync();
+        (void)block_scan(units[threadIdx.x], sh, have);
+    } else {
+        (void)block_scan(__popc(free_pages<EACH>(p, 0)), sh, have);
     }
-    // hand them out, in the order of their ids
+    // hand them out, in the order of their ids: a step's free pages as a list, then one page to a thread
     int rank = 0;
-    for (int base = 0; base < p.num_blocks && rank < wanted; base += kPoolThreads * EACH) {
+    for (int step = 0; step < steps && rank < wanted; ++step) {
+        if (CLUSTER && units[step / per_unit] == 0) continue;
+        const int base = step * kStep;
         uint32_t free = free_pages<EACH>(p, base);
-        int k = rank + block_scan(__popc(free), sh, sum);
-        rank += sum;
-        for (; free && k < wanted; ++k, free &= free - 1) {
-            const int page = base + (int)threadIdx.x * EACH + __ffs(free) - 1;
+        int i = block_scan(__popc(free), sh, sum);
+        for (; free && rank + i < wanted; ++i, free &= free - 1) list[i] = (uint16_t)(threadIdx.x * EACH + __ffs(free) - 1);
+        __syncthreads();
+        for (i = threadIdx.x; i < sum && rank + i < wanted; i += kPoolThreads) {
+            const int page = base + list[i], k = rank + i;
             int lo = 0, hi = p.num_seqs;          // the last sequence whose first place is <= k
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -177,6 +209,7 @@ __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, 
             *row = page;
             p.page_refs[page] = 1;
         }
+        rank += sum;
     }
     __syncthreads();
     for (int s = threadIdx.x; s < p.num_seqs; s += kPoolThreads) {
@@ -194,7 +227,8 @@ __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, 
 }
 
 // The table entry of sequence s at j after a move.  In place too: an entry depends on itself alone.
-__device__ __forceinline__ void remap_entry(const PoolArgs& p, const int32_t* page_map, int32_t* table_out, int s, int j)
+template <typename Where>
+__device__ __forceinline__ void remap_entry(const PoolArgs& p, int32_t* table_out, int s, int j, Where where)
 {
     const int64_t at = (int64_t)s * p.max_blocks + j;
     const int L = p.seq_lens[s];
@@ -202,76 +236,138 @@ __device__ __forceinline__ void remap_entry(const PoolArgs& p, const int32_t* pa
     int to = -1;
     if (!bad && j < pages_of(L)) {
         const int page = p.block_table[at];
-        if (page_ok(p, page)) to = page_map[page];
+        if (page_ok(p, page)) to = where(page);
         if (to < 0) report(p.status, HOOK_ATTN_ERR_BOUNDS);
     }
     if (bad) report(p.status, HOOK_ATTN_ERR_BOUNDS);
     table_out[at] = to;
 }
 
-// The tables of a large pool, one CTA per sequence.
-__global__ void __launch_bounds__(kListThreads) remap_kernel(const PoolArgs p, const int32_t* page_map, int32_t* table_out)
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");       // launched while the map is being made
-    for (int j = threadIdx.x; j < p.max_blocks; j += kListThreads) remap_entry(p, page_map, table_out, blockIdx.x, j);
-}
-
-// With U pages in use, the k-th used page at U or above moves to the k-th free page below U.  table_out: null where the tables are
-// left to remap_kernel.
-template <int EACH>
+// With U pages in use, the k-th used page at U or above moves to the k-th free page below U.  One CTA for a pool of at most one page
+// a thread and small tables (700 pages: 3.4 us, and 8.1 us in three kernels).
 __global__ void __launch_bounds__(kPoolThreads) compact_kernel(const PoolArgs p, int32_t* table_out, int32_t* __restrict__ refs_out, int32_t* page_map,
                                                                int32_t* __restrict__ pairs, int32_t* __restrict__ num_pairs)
 {
-    if (!table_out) asm volatile("griddepcontrol.launch_dependents;");
     __shared__ int sh[33];
-    int used = 0, sum;
-    for (int base = 0; base < p.num_blocks; base += kPoolThreads * EACH) {
-        int refs[EACH], n = 0;
-        load_refs<EACH>(p, base, refs, 0);
-#pragma unroll
-        for (int u = 0; u < EACH; ++u) n += refs[u] > 0;
-        (void)block_scan(n, sh, sum);
-        used += sum;
-    }
-    int sources = 0, holes = 0;
-    for (int base = 0; base < p.num_blocks; base += kPoolThreads * EACH) {
-        int refs[EACH], from = 0, to = 0;
-        load_refs<EACH>(p, base, refs, 0);
-        const int first = base + (int)threadIdx.x * EACH;
-#pragma unroll
-        for (int u = 0; u < EACH; ++u) {
-            to += first + u < used && refs[u] <= 0;
-            from += first + u >= used && refs[u] > 0;
-        }
-        int k = holes + block_scan(to, sh, sum);
-        holes += sum;
-        int l = sources + block_scan(from, sh, sum);
-        sources += sum;
-#pragma unroll
-        for (int u = 0; u < EACH; ++u) {
-            const int page = first + u;
-            if (page >= p.num_blocks) break;
-            if (page < used && refs[u] <= 0) pairs[2 * k++ + 1] = page;
-            if (page >= used && refs[u] > 0) pairs[2 * l++] = page;
-            page_map[page] = refs[u] > 0 ? page : -1;
-            refs_out[page] = page < used && refs[u] > 0 ? refs[u] : 0;
-        }
+    const int page = threadIdx.x;
+    int refs[1], used, sum;
+    load_refs<1>(p, 0, refs, 0);
+    (void)block_scan(refs[0] > 0, sh, used);
+    const bool hole = page < used && refs[0] <= 0, source = page >= used && refs[0] > 0;
+    const int k = block_scan(hole | source << 16, sh, sum), moved = sum >> 16;
+    if (hole) pairs[2 * (k & 0xffff) + 1] = page;
+    if (source) pairs[2 * (k >> 16)] = page;
+    if (page < p.num_blocks) {
+        page_map[page] = refs[0] > 0 ? page : -1;
+        refs_out[page] = page < used && refs[0] > 0 ? refs[0] : 0;
     }
     __syncthreads();
-    for (int k = threadIdx.x; k < p.num_blocks / 2; k += kPoolThreads) {
-        if (k < sources) {
-            const int from = pairs[2 * k], to = pairs[2 * k + 1];
-            page_map[from] = to;
-            refs_out[to] = p.page_refs[from];
-        } else {
-            pairs[2 * k] = -1;
-            pairs[2 * k + 1] = -1;
-        }
+    if (page < moved) {
+        const int from = pairs[2 * page], to = pairs[2 * page + 1];
+        page_map[from] = to;
+        refs_out[to] = p.page_refs[from];
+    } else if (page < p.num_blocks / 2) {
+        pairs[2 * page] = -1;
+        pairs[2 * page + 1] = -1;
     }
-    if (threadIdx.x == 0) *num_pairs = sources;
-    if (!table_out) return;
+    if (page == 0) *num_pairs = moved;
     __syncthreads();
-    for (int e = threadIdx.x; e < p.num_seqs * p.max_blocks; e += kPoolThreads) remap_entry(p, page_map, table_out, e / p.max_blocks, e % p.max_blocks);
+    for (int e = threadIdx.x; e < p.num_seqs * p.max_blocks; e += kPoolThreads)
+        remap_entry(p, table_out, e / p.max_blocks, e % p.max_blocks, [&](int at) { return page_map[at]; });
+}
+
+// The same for larger pools and tables, in three kernels with a CTA for every kSegment pages: how many of them are used (the counts lie in refs_out,
+// which is written last); the plan; what follows from all pairs.  Between the last two page_map names a moving page's pair, and a free
+// page's that is moved to, as -2 - pair.  4096 pages: 8.5 to 9.7 us, and 9.1 to 9.5 us with one CTA; 100000 pages: 9 to 10 us, and 140 to
+// 173 us with one CTA.
+constexpr int kSegment = 4 * kPoolThreads;
+
+__global__ void __launch_bounds__(kPoolThreads) count_used_kernel(const PoolArgs p, int32_t* __restrict__ counts)
+{
+    asm volatile("griddepcontrol.launch_dependents;");
+    __shared__ int sh[33];
+    int refs[4], n = 0, sum;
+    load_refs<4>(p, blockIdx.x * kSegment, refs, 0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) n += refs[u] > 0;
+    (void)block_scan(n, sh, sum);
+    if (threadIdx.x == 0) counts[blockIdx.x] = sum;
+}
+
+__global__ void __launch_bounds__(kPoolThreads) plan_kernel(const PoolArgs p, const int32_t* counts, int32_t* __restrict__ page_map,
+                                                            int32_t* __restrict__ pairs, int32_t* __restrict__ num_pairs)
+{
+    asm volatile("griddepcontrol.launch_dependents;");
+    __shared__ int sh[33];
+    const int segments = gridDim.x, start = blockIdx.x * kSegment, first = start + (int)threadIdx.x * 4;
+    int refs[4], n = 0, part = 0, used, before, low = 0;
+    load_refs<4>(p, start, refs, 0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int s = threadIdx.x; s < segments; s += kPoolThreads) {
+        const int c = counts[s];
+        n += c;
+        part += s < (int)blockIdx.x ? c : 0;
+    }
+    (void)block_scan(n, sh, used);
+    (void)block_scan(part, sh, before);           // used pages before this segment
+    if (start + kSegment >= used) {               // used pages below `used`: they stay
+        const int edge = used / kSegment;
+        int there[4];
+        load_refs<4>(p, edge * kSegment, there, 0);
+        n = 0;
+        for (int s = threadIdx.x; s < edge; s += kPoolThreads) n += counts[s];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) n += there[u] > 0 && edge * kSegment + (int)threadIdx.x * 4 + u < used;
+        (void)block_scan(n, sh, low);
+        if (threadIdx.x == 0 && (int)blockIdx.x == segments - 1) *num_pairs = used - low;
+    }
+    int both = 0, sum;                            // free pages below `used`, and 2^16 for each used page from there on
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        both += first + u < used && refs[u] <= 0;
+        both += (first + u >= used && refs[u] > 0) << 16;
+    }
+    both = block_scan(both, sh, sum);
+    int k = start - before + (both & 0xffff), l = (start > used ? before - low : 0) + (both >> 16);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int page = first + u;
+        if (page >= p.num_blocks) break;
+        int to = refs[u] > 0 ? page : -1;
+        if (page < used && refs[u] <= 0) {
+            to = -2 - k;
+            pairs[2 * k++ + 1] = page;
+        }
+        if (page >= used && refs[u] > 0) {
+            to = -2 - l;
+            pairs[2 * l++] = page;
+        }
+        page_map[page] = to;
+    }
+}
+
+__global__ void __launch_bounds__(kListThreads) finish_kernel(const PoolArgs p, int32_t* table_out, int32_t* __restrict__ refs_out, int32_t* page_map,
+                                                              int32_t* pairs, const int32_t* __restrict__ num_pairs)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t step = (int64_t)gridDim.x * kListThreads, me = (int64_t)blockIdx.x * kListThreads + threadIdx.x;
+    for (int64_t page = me; page < p.num_blocks; page += step) {
+        const int t = page_map[page], r = p.page_refs[page];
+        int refs = max(r, 0);
+        if (t <= -2) {
+            const int32_t* pair = pairs + 2 * (-2 - t);
+            refs = r > 0 ? 0 : p.page_refs[pair[0]];
+            page_map[page] = r > 0 ? pair[1] : -1;
+        }
+        refs_out[page] = refs;
+    }
+    for (int64_t k = *num_pairs + me; k < p.num_blocks / 2; k += step) pairs[2 * k] = pairs[2 * k + 1] = -1;
+    // What another thread makes of a page's entry in the meantime is what is made of it here.
+    for (int64_t e = me; e < (int64_t)p.num_seqs * p.max_blocks; e += step)
+        remap_entry(p, table_out, (int)(e / p.max_blocks), (int)(e % p.max_blocks), [&](int page) {
+            const int t = __ldcg(page_map + page);
+            return t > -2 ? t : p.page_refs[page] > 0 ? pairs[2 * (-2 - t) + 1] : -1;
+        });
 }
 
 // A CTA copies `pairs` pages in `slabs` of the caches (keys or values of a layer).  Pairs must not depend on one another: one whose
@@ -340,11 +436,17 @@ __global__ void __launch_bounds__(kListThreads) copy_pages_kernel(const __grid_c
 
 }  // namespace
 
+static size_t extend_bytes(int num_seqs, int each) { return 2 * (size_t)num_seqs * 4 + (size_t)each * kPoolThreads * 2; }
+
 cudaError_t configure_cache_pages()
 {
-    cudaError_t e = cudaFuncSetAttribute(extend_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxPoolSeqs * 4);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(extend_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxPoolSeqs * 4);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(extend_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxPoolSeqs * 4);
+    const auto allow = [](auto* kernel, int each) {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)extend_bytes(kMaxPoolSeqs, each));
+    };
+    cudaError_t e = allow(extend_kernel<1, false>, 1);
+    if (e == cudaSuccess) e = allow(extend_kernel<4, false>, 4);
+    if (e == cudaSuccess) e = allow(extend_kernel<16, false>, 16);
+    if (e == cudaSuccess) e = allow(extend_kernel<16, true>, 16);
     return e;
 }
 
@@ -360,35 +462,64 @@ cudaError_t launch_free(const PoolArgs& p, const int32_t* seqs, const int32_t* k
     return cudaGetLastError();
 }
 
+template <int EACH>
+static cudaError_t extend(const PoolArgs& p, const int32_t* new_rows, int32_t* pairs, cudaStream_t st)
+{
+    extend_kernel<EACH, false><<<1, kPoolThreads, extend_bytes(p.num_seqs, EACH), st>>>(p, new_rows, pairs);
+    return cudaGetLastError();
+}
+
 cudaError_t launch_extend(const PoolArgs& p, const int32_t* new_rows, int32_t* pairs, cudaStream_t st)
 {
-    if (p.num_blocks <= kPoolThreads) extend_kernel<1><<<1, kPoolThreads, 2 * p.num_seqs * 4, st>>>(p, new_rows, pairs);
-    else if (p.num_blocks <= 4 * kPoolThreads) extend_kernel<4><<<1, kPoolThreads, 2 * p.num_seqs * 4, st>>>(p, new_rows, pairs);
-    else extend_kernel<16><<<1, kPoolThreads, 2 * p.num_seqs * 4, st>>>(p, new_rows, pairs);
-    return cudaGetLastError();
+    if (p.num_blocks <= kPoolThreads) return extend<1>(p, new_rows, pairs, st);
+    if (p.num_blocks <= 4 * kPoolThreads) return extend<4>(p, new_rows, pairs, st);
+    if (p.num_blocks <= 16 * kPoolThreads) return extend<16>(p, new_rows, pairs, st);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kClusterCtas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kClusterCtas);
+    cfg.blockDim = dim3(kPoolThreads);
+    cfg.dynamicSmemBytes = extend_bytes(p.num_seqs, 16);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, extend_kernel<16, true>, p, new_rows, pairs);
+}
+
+// A kernel that may start while the one before it in the stream runs, and waits for it itself.
+template <typename... P, typename... A>
+static cudaError_t launch_after(void (*kernel)(P...), int grid, int threads, cudaStream_t st, A... args)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
 cudaError_t launch_compact(const PoolArgs& p, int32_t* table_out, int32_t* refs_out, int32_t* page_map, int32_t* pairs,
                            int32_t* num_pairs, cudaStream_t st)
 {
-    // A second kernel for the tables pays from some 16 entries a thread on (48 x 29 entries: 4 us more).
-    const bool small = (int64_t)p.num_seqs * p.max_blocks <= 16 * kPoolThreads;
-    int32_t* here = small ? table_out : nullptr;
-    if (p.num_blocks <= kPoolThreads) compact_kernel<1><<<1, kPoolThreads, 0, st>>>(p, here, refs_out, page_map, pairs, num_pairs);
-    else if (p.num_blocks <= 4 * kPoolThreads) compact_kernel<4><<<1, kPoolThreads, 0, st>>>(p, here, refs_out, page_map, pairs, num_pairs);
-    else compact_kernel<16><<<1, kPoolThreads, 0, st>>>(p, here, refs_out, page_map, pairs, num_pairs);
+    const int64_t entries = (int64_t)p.num_seqs * p.max_blocks;
+    if (p.num_blocks == 0 || (p.num_blocks <= kPoolThreads && entries <= 16 * kPoolThreads)) {
+        compact_kernel<<<1, kPoolThreads, 0, st>>>(p, table_out, refs_out, page_map, pairs, num_pairs);
+        return cudaGetLastError();
+    }
+    const int segments = (p.num_blocks + kSegment - 1) / kSegment;
+    const int64_t blocks = ((entries > p.num_blocks ? entries : p.num_blocks) + kListThreads - 1) / kListThreads;
+    count_used_kernel<<<segments, kPoolThreads, 0, st>>>(p, refs_out);
     cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || small) return e;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.num_seqs);
-    cfg.blockDim = dim3(kListThreads);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, remap_kernel, p, static_cast<const int32_t*>(page_map), table_out);
+    if (e == cudaSuccess) e = launch_after(plan_kernel, segments, kPoolThreads, st, p, refs_out, page_map, pairs, num_pairs);
+    if (e == cudaSuccess)
+        e = launch_after(finish_kernel, (int)(blocks < 4096 ? blocks : 4096), kListThreads, st, p, table_out, refs_out, page_map, pairs, num_pairs);
+    return e;
 }
 
 cudaError_t launch_copy_pages(const CopyArgs& a, cudaStream_t st)

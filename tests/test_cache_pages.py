@@ -65,7 +65,8 @@ def _pool_params(**over):
     (dict(), binding.HOOK_ATTN_ERR_CUDA), (dict(num_seqs=-1), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(block_table=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(seq_lens=None), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(page_refs=None), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(page_size=32), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(num_seqs=16385), binding.HOOK_ATTN_ERR_UNSUPPORTED),
-    (dict(num_seqs=16384, max_blocks_per_seq=65537), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(num_seqs=16384, max_blocks_per_seq=65536), binding.HOOK_ATTN_ERR_CUDA)])
+    (dict(num_seqs=16384, max_blocks_per_seq=65537), binding.HOOK_ATTN_ERR_UNSUPPORTED),
+    (dict(num_blocks=2 ** 30 + 1), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(num_blocks=2 ** 30), binding.HOOK_ATTN_ERR_CUDA), (dict(num_seqs=16384, max_blocks_per_seq=65536), binding.HOOK_ATTN_ERR_CUDA)])
 def test_pool_refusals(over, code):
     lib, p = binding.load_library(), ctypes.byref(_pool_params(**over))
     assert lib.hook_cache_fork(FAKE_HANDLE, p, 0x1000, 0x1000, 1, None) == code
@@ -292,6 +293,62 @@ def test_in_place_table_of_compact(eng):
     torch.cuda.synchronize()
     want_table, want_refs, _, _ = both.want.compact()
     assert rc == 0 and both.dev["block_table"].tolist() == want_table and refs.tolist() == want_refs
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("num_blocks", [1, 2, 1023, 1024, 1025, 4095, 4096, 4097, 8192, 8193, 12289])
+@pytest.mark.parametrize("shape", ["all", "none", "low", "high", "odd", "one high", "one free", "below 0"])
+def test_compact_at_the_edges(eng, num_blocks, shape):
+    """Pools of whole and broken segments, with the count of used pages on and beside their edges, small and large tables, in place too."""
+    used = {"all": lambda i: True, "none": lambda i: False, "low": lambda i: i < min(4096, num_blocks // 2), "high": lambda i: i >= num_blocks // 2,
+            "odd": lambda i: i % 2, "one high": lambda i: i == num_blocks - 1, "one free": lambda i: i != num_blocks // 3, "below 0": lambda i: i % 3 == 0}[shape]
+    both = Both(eng, 3, 6000, num_blocks)
+    w = both.want
+    w.refs = [1 + i % 5 if used(i) else (-2 if shape == "below 0" else 0) for i in range(num_blocks)]
+    held = [i for i in range(num_blocks) if used(i)]
+    g = np.random.default_rng(num_blocks)
+    for s in (0, 2):
+        mine = g.permutation(held)[:5990].tolist()
+        w.table[s][:len(mine)] = mine
+        w.lens[s] = 16 * len(mine) - (3 if mine else 0)
+    both.load()
+    both.compact(adopt=False)
+    table = both.dev["block_table"]
+    pool = ctypes.byref(binding.HookCachePool(3, 6000, num_blocks, 16, *(both.dev[n].data_ptr() for n in ("block_table", "seq_lens", "page_refs", "status"))))
+    refs, page_map, pairs, count = (torch.empty(n, dtype=torch.int32, device="cuda") for n in (num_blocks, num_blocks, num_blocks, 1))
+    want_table, want_refs, want_map, moves = w.compact()
+    assert eng._lib.hook_cache_compact(eng._h, pool, table.data_ptr(), refs.data_ptr(), page_map.data_ptr(), pairs.data_ptr(), count.data_ptr(),
+                                       torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert table.tolist() == want_table and refs.tolist() == want_refs and page_map.tolist() == want_map and count.tolist() == [len(moves)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("num_blocks", [20, 5000])
+def test_compact_reports_tables_that_name_free_pages(eng, num_blocks):
+    both = Both(eng, 3, 6, num_blocks)
+    w = both.want
+    w.refs = [int(i % 2) for i in range(num_blocks)]
+    w.table[0][:4], w.lens[0] = [1, 0, num_blocks - 2, num_blocks - 1], 64     # a free page that is moved to, one that is not, and one beyond the pool
+    w.table[1][:2], w.lens[1] = [num_blocks, -5], 20
+    both.load()
+    both.compact(adopt=False)
+
+
+@pytest.mark.gpu
+def test_extend_in_a_pool_of_many_million_pages(eng):
+    """More steps than the counts that are made of them; the free pages far apart, among them the first and the last."""
+    n, i32 = 17 * 2 ** 20 + 5, dict(dtype=torch.int32, device="cuda")
+    at = [0, 5, 16383, 16384, 40000, 2 ** 20, 2 ** 24 - 1, 2 ** 24, 2 ** 24 + 70000, n - 2, n - 1]
+    refs = torch.ones(n, **i32)
+    refs[torch.tensor(at, device="cuda")] = 0
+    table, lens, status = torch.full((5, 4), -1, **i32), torch.zeros(5, **i32), torch.zeros(1, **i32)
+    pairs = eng.hook_cache_extend(table, lens, refs, torch.tensor([33, 16, 64, 1, 40], **i32), status=status)
+    assert table.tolist() == [at[:3] + [-1], at[3:4] + [-1] * 3, at[4:8], at[8:9] + [-1] * 3, [-1] * 4]       # the last one finds two of three
+    assert lens.tolist() == [33, 16, 64, 1, 0] and pairs.tolist() == [[-1, -1]] * 5 and int(status.item()) == binding.HOOK_ATTN_ERR_NO_PAGES
+    assert int((refs == 0).sum()) == 2 and int(refs[n - 1]) == 0 and int(refs[n - 2]) == 0
+    eng.hook_cache_extend(table, lens, refs, torch.tensor([15, 0, 0, 15, 32], **i32))
+    assert table[4].tolist() == at[9:] + [-1] * 2 and lens.tolist() == [48, 16, 64, 16, 32] and int(refs.min()) == 1
 
 
 def _cache(layout, pages, hkv, d, layers, seed):

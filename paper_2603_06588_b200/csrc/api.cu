@@ -48,7 +48,7 @@ cudaError_t launch_free(const PoolArgs& p, const int32_t* seqs, const int32_t* k
 cudaError_t launch_extend(const PoolArgs& p, const int32_t* new_rows, int32_t* pairs, cudaStream_t st);
 cudaError_t launch_compact(const PoolArgs& p, int32_t* table_out, int32_t* refs_out, int32_t* page_map, int32_t* pairs,
                            int32_t* num_pairs, cudaStream_t st);
-cudaError_t launch_copy_pages(const CopyArgs& a, cudaStream_t st);
+cudaError_t launch_copy_pages(const CopyArgs& a, int num_sms, cudaStream_t st);
 }  // namespace hook_attn
 
 using namespace hook_attn;
@@ -591,7 +591,7 @@ int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params
             a.k[l] = static_cast<__nv_bfloat16*>(p->k_caches[l0 + l]);
             a.v[l] = static_cast<__nv_bfloat16*>(p->v_caches[l0 + l]);
         }
-        if (launch_copy_pages(a, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return HOOK_ATTN_ERR_CUDA;
+        if (launch_copy_pages(a, handle->num_sms, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return HOOK_ATTN_ERR_CUDA;
     }
     return HOOK_ATTN_OK;
 }

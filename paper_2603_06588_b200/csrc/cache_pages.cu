@@ -370,65 +370,87 @@ __global__ void __launch_bounds__(kListThreads) finish_kernel(const PoolArgs p, 
         });
 }
 
-// A CTA copies `pairs` pages in `slabs` of the caches (keys or values of a layer).  Pairs must not depend on one another: one whose
-// destination is the destination or the source of another pair, or whose source is a destination, is not carried out, and a CTA looks
-// through all pairs to see that.  Bound by HBM (983 pages of 16 layers, 2.1 GB read and written: 334 us, 6.2 TB/s; equal shares for a
-// grid that is resident at once: 362 us).
-constexpr int kChecked = 8;                      // pairs of a CTA at most
+// A unit is a page of one slab (the keys or the values of a layer), and from kMany pairs on eight pages of four slabs, since the pairs of
+// a unit are held against all others: they must not depend on one another, and one whose destination is the destination or the source of
+// another pair, or whose source is a destination, is not carried out.  How many pairs there are is known on the device alone, so a
+// fixed number of CTAs goes through the units, slab after slab (page after page, all slabs of each: 62 -> 69 us for 256 pairs in 32
+// slabs).  32 CTAs for an SM: with one for each unit that there could be, 20 of 2048 pairs in 32 slabs take 36 us, with 64 10 us, with
+// 32 7 us; all 2048 take 1 % longer than with 64.  Bound by HBM (983 pages of 16 layers, 2.1 GB read and written: 320 us, the copy rate).
+constexpr int kChecked = 8;                      // pairs of a unit at most
+constexpr int kMany = 2048;
+constexpr int kCopyCtas = 32;
 
-// TIGHT: a page's tokens and heads follow one another without gaps, in either order.
-template <bool TIGHT>
-__global__ void __launch_bounds__(kListThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a, int pairs, int slabs)
+// TIGHT: a page's tokens and heads follow one another without gaps, in either order.  CHECKED: 1 for lists that cannot be long (the
+// registers of eight leave room for fewer CTAs on an SM: 256 pairs of (-1, -1) in 32 slabs 7.7 us, and 14 us).
+template <bool TIGHT, int CHECKED>
+__global__ void __launch_bounds__(kListThreads, CHECKED == 1 ? 6 : 4) copy_pages_kernel(const __grid_constant__ CopyArgs a)
 {
     __shared__ uint32_t refused;
-    const int n = a.num_pairs ? min(max(*a.num_pairs, 0), a.max_pairs) : a.max_pairs;
-    const int p0 = blockIdx.x * pairs, count = min(pairs, n - p0), slab0 = blockIdx.y * slabs, slab1 = min(slab0 + slabs, 2 * a.layers);
-    if (count <= 0) return;
-    int src[kChecked], dst[kChecked];
-#pragma unroll
-    for (int q = 0; q < kChecked; ++q) {
-        src[q] = q < count ? a.pairs[2 * (p0 + q)] : -1;
-        dst[q] = q < count ? a.pairs[2 * (p0 + q) + 1] : -1;
-        if (src[q] < 0 || dst[q] < 0) src[q] = dst[q] = -1;
-    }
-    if (threadIdx.x == 0) refused = 0;
-    __syncthreads();
-    uint32_t bad = 0;
-    for (int j = threadIdx.x; j < n; j += kListThreads) {
-        const int s = a.pairs[2 * j], d = a.pairs[2 * j + 1];
-        if (s < 0 || d < 0) continue;
-#pragma unroll
-        for (int q = 0; q < kChecked; ++q)
-            if (j != p0 + q && (d == dst[q] || s == dst[q] || d == src[q])) bad |= 1u << q;
-    }
-    if (bad) atomicOr(&refused, bad);
-    __syncthreads();
+    const int n = a.num_pairs ? min(max(*a.num_pairs, 0), a.max_pairs) : a.max_pairs, slabs = 2 * a.layers;
+    if (n == 0) return;
+    const bool many = CHECKED > 1 && n > kMany;
+    const uint32_t pairs = many ? CHECKED : 1, some = many ? min(slabs, 4) : 1;              // of a unit
+    const uint32_t groups = ((uint32_t)n + pairs - 1) / pairs, rows = (slabs + some - 1) / some;
+    const uint32_t next_group = gridDim.x % groups, next_row = gridDim.x / groups;
     const int per_row = a.head_dim / 8, pieces = kPage * a.Hkv * per_row;
     auto place = [&](int e) {
         if (TIGHT) return (int64_t)e * 8;
         const int c = e % per_row, h = e / per_row % a.Hkv, t = e / per_row / a.Hkv;
         return (int64_t)t * a.ts + (int64_t)h * a.hs + c * 8;
     };
-#pragma unroll
-    for (int q = 0; q < kChecked; ++q) {
-        const int s = src[q], d = dst[q];
-        if (s == d) continue;
-        if ((refused >> q & 1) || s >= a.num_blocks || d >= a.num_blocks) {
-            if (threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-            continue;
+    uint32_t group = blockIdx.x % groups;
+    for (uint32_t row = blockIdx.x / groups; row < rows;) {
+        const int p0 = (int)(group * pairs), count = min((int)pairs, n - p0), slab0 = (int)(row * some), slab1 = min(slab0 + (int)some, slabs);
+        row += next_row;
+        group += next_group;
+        if (group >= groups) {
+            group -= groups;
+            ++row;
         }
-        for (int slab = slab0; slab < slab1; ++slab) {
-            __nv_bfloat16* base = slab & 1 ? a.v[slab >> 1] : a.k[slab >> 1];
-            const __nv_bfloat16* in = base + (int64_t)s * a.bs;
-            __nv_bfloat16* out = base + (int64_t)d * a.bs;
-            for (int e0 = threadIdx.x; e0 < pieces; e0 += 4 * kListThreads) {
-                uint4 held[4];
+        int src[CHECKED], dst[CHECKED];
+        bool live = false;
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (e0 + u * kListThreads < pieces) held[u] = *reinterpret_cast<const uint4*>(in + place(e0 + u * kListThreads));
+        for (int q = 0; q < CHECKED; ++q) {
+            src[q] = q < count ? a.pairs[2 * (p0 + q)] : -1;
+            dst[q] = q < count ? a.pairs[2 * (p0 + q) + 1] : -1;
+            if (src[q] < 0 || dst[q] < 0) src[q] = dst[q] = -1;
+            live |= src[q] >= 0;
+        }
+        if (!live) continue;
+        __syncthreads();                          // the unit before is done with it
+        if (threadIdx.x == 0) refused = 0;
+        __syncthreads();
+        uint32_t bad = 0;
+        for (int j = threadIdx.x; j < n; j += kListThreads) {
+            const int s = a.pairs[2 * j], d = a.pairs[2 * j + 1];
+            if (s < 0 || d < 0) continue;
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (e0 + u * kListThreads < pieces) *reinterpret_cast<uint4*>(out + place(e0 + u * kListThreads)) = held[u];
+            for (int q = 0; q < CHECKED; ++q)
+                if (j != p0 + q && (d == dst[q] || s == dst[q] || d == src[q])) bad |= 1u << q;
+        }
+        if (bad) atomicOr(&refused, bad);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < CHECKED; ++q) {
+            const int s = src[q], d = dst[q];
+            if (s == d) continue;
+            if ((refused >> q & 1) || s >= a.num_blocks || d >= a.num_blocks) {
+                if (threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+                continue;
+            }
+            for (int slab = slab0; slab < slab1; ++slab) {
+                __nv_bfloat16* base = slab & 1 ? a.v[slab >> 1] : a.k[slab >> 1];
+                const __nv_bfloat16* in = base + (int64_t)s * a.bs;
+                __nv_bfloat16* out = base + (int64_t)d * a.bs;
+                for (int e0 = threadIdx.x; e0 < pieces; e0 += 4 * kListThreads) {
+                    uint4 held[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (e0 + u * kListThreads < pieces) held[u] = *reinterpret_cast<const uint4*>(in + place(e0 + u * kListThreads));
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (e0 + u * kListThreads < pieces) *reinterpret_cast<uint4*>(out + place(e0 + u * kListThreads)) = held[u];
+                }
             }
         }
     }
@@ -522,15 +544,15 @@ cudaError_t launch_compact(const PoolArgs& p, int32_t* table_out, int32_t* refs_
     return e;
 }
 
-cudaError_t launch_copy_pages(const CopyArgs& a, cudaStream_t st)
+cudaError_t launch_copy_pages(const CopyArgs& a, int num_sms, cudaStream_t st)
 {
-    // A CTA for every slab of every pair; with many pairs, which each CTA has to look through, several of both for a CTA.
-    const bool many = a.max_pairs > 2048;
-    const int pairs = many ? kChecked : 1, slabs = many ? (2 * a.layers < 4 ? 2 * a.layers : 4) : 1;
-    const dim3 grid((a.max_pairs + pairs - 1) / pairs, (2 * a.layers + slabs - 1) / slabs);
+    const int64_t units = (int64_t)a.max_pairs * 2 * a.layers, most = (int64_t)num_sms * kCopyCtas;
+    const int grid = (int)(units < most ? units : most);
     const bool tight = (a.hs == a.head_dim && a.ts == (int64_t)a.Hkv * a.head_dim) || (a.ts == a.head_dim && a.hs == (int64_t)kPage * a.head_dim);
-    if (tight) copy_pages_kernel<true><<<grid, kListThreads, 0, st>>>(a, pairs, slabs);
-    else copy_pages_kernel<false><<<grid, kListThreads, 0, st>>>(a, pairs, slabs);
+    const bool few = a.max_pairs <= kMany;
+    const auto kernel = tight ? (few ? copy_pages_kernel<true, 1> : copy_pages_kernel<true, kChecked>)
+                              : (few ? copy_pages_kernel<false, 1> : copy_pages_kernel<false, kChecked>);
+    kernel<<<grid, kListThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 

@@ -423,3 +423,25 @@ def test_nothing_to_do(eng):
     both.compact()
     _check_copy(eng, [])
     eng.hook_cache_copy_pages([], torch.zeros((1, 2), dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("max_pairs,count", [(2048, 2048), (2048, 2047), (2049, 2049), (2049, 3), (2100, None), (9000, 2048), (9000, 8999), (9000, 0)])
+@pytest.mark.parametrize("layers", [1, 3, 5])
+def test_copy_of_many_pairs(eng, max_pairs, count, layers):
+    """Long lists, of which few or all count, some of them dead, some that depend on one another."""
+    pages, g = 20000, np.random.default_rng(max_pairs + layers)
+    perm = g.permutation(pages)[:2 * max_pairs].reshape(max_pairs, 2)
+    perm[g.integers(0, max_pairs, 7)] = -1
+    a, b = max_pairs // 2, max_pairs // 3
+    if count != 0:
+        perm[a, 1] = perm[0, 0] = perm[b, 1] = 17                  # two with one destination, which is a third one's source
+    cache = torch.randint(-2 ** 15, 2 ** 15, (layers, 2, pages, 16, 1, 64), generator=torch.Generator().manual_seed(5), dtype=torch.int32)
+    cache = cache.to(torch.int16).cuda().view(torch.bfloat16)
+    before, status = cache.clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    pairs = torch.tensor(perm, dtype=torch.int32, device="cuda")
+    eng.hook_cache_copy_pages([(c[0], c[1]) for c in cache], pairs, None if count is None else torch.tensor([count], dtype=torch.int32, device="cuda"), status=status)
+    moved, refused = ops.copy_pages(np.arange(pages), [tuple(p) for p in perm[:max_pairs if count is None else count].tolist()])
+    want = before.view(torch.int16)[:, :, torch.tensor(moved, device="cuda")]
+    assert torch.equal(cache.view(torch.int16), want)
+    assert int(status.item()) == (binding.HOOK_ATTN_ERR_BOUNDS if refused else 0)

@@ -110,11 +110,6 @@ struct alignas(16) Vec {            // eight values: one or two accesses of 16 b
     T x[8];
 };
 
-// A CTA owns one slice of one row: it looks through the row's history for tokens of its slice and counts them in shared memory
-// (integers, so the order of the atomics is of no account), then passes over the slice once, eight values at a time.  Bound by
-// HBM: a value is read once and written once; the history is read by every CTA of the row, from L2.
-// The slice's words lie so that the eight of a vector are aligned: word 8 belongs to the slice's first aligned value, and the
-// values of a row before its first aligned one take the words before it, in the first slice.
 // The row's history as THREADS threads look through it for tokens of a stretch, four at a time.  The first eight tokens of each
 // thread are fetched when it is made, so that they are there when the words are ready to count in.  Integers: the order of the
 // atomics is of no account.

@@ -315,7 +315,7 @@ typedef struct {
  *   x = seen ? (x > 0 ? x / repetition : x * repetition) : x;   x -= frequency * c + presence * (c > 0);
  *   x += bias[v];   x = -inf if the grammar forbids v (whatever x is; a mask may forbid all).
  * A row whose lengths, bias offsets or mask row are out of range sets status and its part of out is not written; a
- * bias for a token outside the vocabulary sets status and is passed over.  vocab_size <= 2^20, max_tokens < 2^20. */
+ * bias for a token outside the vocabulary sets status and is passed over.  vocab_size <= 2^20, max_tokens < 2^20, num_rows < 2^16. */
 int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, void* cuda_stream);
 
 /* The pool that the sequences of a cache share.  All its arrays are written by the calls below. */
@@ -364,7 +364,7 @@ typedef struct {
     int64_t kv_block_stride, kv_token_stride, kv_head_stride;   /* of every layer's caches, in elements */
     void* const*   k_caches;     /* HOST array [num_layers] of device pointers */
     void* const*   v_caches;     /* HOST array [num_layers] */
-    const int32_t* pairs;        /* [max_pairs][2] source and destination page; a negative one: passed over */
+    const int32_t* pairs;        /* [max_pairs][2] source and destination page; a negative one: passed over; max_pairs <= 2^30 */
     const int32_t* num_pairs;    /* device int32 [1], how many of them count; NULL: max_pairs */
     int32_t*       status;
 } hook_cache_copy_params;

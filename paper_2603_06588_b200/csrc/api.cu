@@ -566,7 +566,7 @@ int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params
 {
     if (!p || p->num_layers < 0 || p->num_blocks < 0 || p->page_size <= 0 || p->num_kv_heads <= 0 || p->head_dim <= 0 || p->max_pairs < 0)
         return HOOK_ATTN_ERR_INVALID_ARG;
-    if ((p->head_dim != 64 && p->head_dim != 128) || p->page_size != kPage || p->num_kv_heads > kMaxHeads) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if ((p->head_dim != 64 && p->head_dim != 128) || p->page_size != kPage || p->num_kv_heads > kMaxHeads || p->max_pairs > 1 << 30) return HOOK_ATTN_ERR_UNSUPPORTED;
     if (p->num_layers > 0 && p->max_pairs > 0) {
         if (!p->k_caches || !p->v_caches || !p->pairs) return HOOK_ATTN_ERR_INVALID_ARG;
         if (p->kv_block_stride <= 0 || p->kv_token_stride <= 0 || p->kv_head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;

@@ -182,7 +182,7 @@ def test_many_rows(eng, rows):
     (torch.float16, torch.float32, 0, 0, False), (torch.float32, None, 0, 0, False), (torch.float32, None, 7, 7, True), (torch.float32, None, 1, 2, False)])
 @pytest.mark.parametrize("rows,vocab,hist", [(100, 50023, 300), (130, 20005, 1500), (37, 131072, 9001), (300, 20000, 8193), (9700, 301, 20)])
 def test_large_batches(eng, dtype, out, pad, out_pad, in_place, rows, vocab, hist):
-    """Long stretches: histories that are counted directly or sorted first (in one bin or three), rows without one, refused and unaligned rows."""
+    """Long stretches of both lengths and short ones, rows without a history, refused and unaligned rows."""
     g, x, kw = _random(rows, vocab, dtype, hist, rows + vocab, bias=20)
     kw["total"][:4] = hist, 0, 1, hist - 1
     kw["prompt"][:4] = hist // 2, 0, 0, hist - 1

@@ -97,7 +97,8 @@ def test_list_refusals():
     (dict(k_caches=None), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(kv_block_stride=0), binding.HOOK_ATTN_ERR_INVALID_ARG),
     (dict(head_dim=80), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(page_size=8), binding.HOOK_ATTN_ERR_UNSUPPORTED),
     (dict(kv_head_stride=132), binding.HOOK_ATTN_ERR_UNSUPPORTED), (dict(address=0x10008), binding.HOOK_ATTN_ERR_UNSUPPORTED),
-    (dict(address=0), binding.HOOK_ATTN_ERR_INVALID_ARG)])
+    (dict(address=0), binding.HOOK_ATTN_ERR_INVALID_ARG), (dict(max_pairs=2 ** 30), binding.HOOK_ATTN_ERR_CUDA),
+    (dict(max_pairs=2 ** 30 + 1), binding.HOOK_ATTN_ERR_UNSUPPORTED)])
 def test_copy_refusals(over, code):
     at = over.pop("address", 0x10000) if "address" in over else 0x10000
     ptrs = (ctypes.c_void_p * 2)(0x10000, at)
@@ -445,3 +446,30 @@ def test_copy_of_many_pairs(eng, max_pairs, count, layers):
     want = before.view(torch.int16)[:, :, torch.tensor(moved, device="cuda")]
     assert torch.equal(cache.view(torch.int16), want)
     assert int(status.item()) == (binding.HOOK_ATTN_ERR_BOUNDS if refused else 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("num_blocks", [900, 5000, 20000, 70000])
+def test_pools_in_a_graph_on_another_stream(eng, num_blocks):
+    """All calls on a pool captured once and replayed, each replay on the state that the one before left."""
+    both, g = Both(eng, 40, 400, num_blocks), np.random.default_rng(num_blocks)
+    both.extend((g.integers(0, num_blocks * 8 // 40, 40) * (np.arange(40) < 35)).tolist())
+    parents, children, seqs, keep = [0, 1, 2], [37, 38, 39], [5, 6, 37, 38, 39], [30, 7, 0, 0, 0]
+    new = g.integers(0, 60, 40).tolist()
+    args = [both._i32(x) for x in (parents, children, new, seqs, keep)]
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        eng.hook_cache_fork(**both.dev, parents=args[0], children=args[1])
+        pairs = eng.hook_cache_extend(**both.dev, new_rows=args[2])
+        eng.hook_cache_free(**both.dev, seqs=args[3], keep_lens=args[4])
+        table, refs, page_map, moves, count = eng.hook_cache_compact(**both.dev)
+    for _ in range(3):
+        graph.replay()
+        both.want.fork(parents, children)
+        want_pairs = both.want.extend(new)
+        both.want.free(seqs, keep)
+        want_table, want_refs, want_map, want_moves = both.want.compact()
+        both.compare()
+        assert [tuple(p) for p in pairs.tolist()] == want_pairs
+        assert table.tolist() == want_table and refs.tolist() == want_refs and page_map.tolist() == want_map and count.tolist() == [len(want_moves)]
+        assert [tuple(p) for p in moves.tolist()] == want_moves + [(-1, -1)] * (num_blocks // 2 - len(want_moves))

@@ -39,7 +39,6 @@ HOOK_DTYPE_BF16, HOOK_DTYPE_F16, HOOK_DTYPE_F32 = 0, 1, 2
 HOOK_ROPE_AXES_BLOCKED, HOOK_ROPE_AXES_CYCLIC = 0, 1
 HOOK_ROPE_PAIR_HALVES, HOOK_ROPE_PAIR_ADJACENT = 0, 1
 HOOK_ROPE_MAX_AXES = 4
-HOOK_CACHE_PAGE = 16             # tokens per page of the cache
 # Arguments between the handle and the stream: p an address, i an int32.
 _AROUND = {"hook_rope_append": "p", "hook_adjust_logits": "p", "hook_cache_fork": "pppi", "hook_cache_extend": "ppp",
            "hook_cache_free": "pppi", "hook_cache_compact": "pppppp", "hook_cache_copy_pages": "p"}
@@ -338,7 +337,7 @@ class HookAttn:
     # These calls are short: a compiled module checks the tensors (AssertionError), fills the C structs, allocates the results and calls
     # the library (one row of hook_rope_append: 11.7 us a call with the same done here, 5.4 us with it, of which the launch is 2.9).
     def _short(self, name: str, call, stream, *args):
-        got = call(self._calls[name], self._h.value or 0, self._index, stream, *args)
+        got = call(self._calls[name], self._h.value if self._h else 0, self._index, stream, *args)
         if type(got) is int:
             if got != HOOK_ATTN_OK:
                 raise HookAttnError(got, name)

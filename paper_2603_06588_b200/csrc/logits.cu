@@ -258,11 +258,11 @@ __global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_con
     for (int i = s.base + 8 * vectors + tid; i < s.hi; i += THREADS) edit_one(in, out, i, s.any ? word[i - s.first] : 0u, s);
 }
 
-// Large calls: a CTA takes a long stretch, all of whose loads are under way while its words are filled; CTAs of 256 or 512 threads, 1024
-// threads on an SM with 64 registers each.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 54 us, 6.1
+// Large calls: a CTA takes a long stretch, all of whose loads are under way while its words are filled; four CTAs of 256 threads on an
+// SM or one of 1024, with 64 registers each.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 54 us, 6.1
 // TB/s).  With one, by the chain of loads before a stretch's edits and by the issue slots: each stretch of a row looks through the whole
 // history, and a warp runs the edit for each of the eight values of a lane that any of its lanes has a word for (the same with
-// histories of up to 4096 tokens: 71 us, 4.7 TB/s; 64 rows of 128000 bf16 to fp32 values with up to 32768 tokens: 27.5 us, 2.0 TB/s).
+// histories of up to 4096 tokens: 71 us, 4.7 TB/s; 64 rows of 128000 bf16 to fp32 values with up to 32768 tokens: 27 us, 2.0 TB/s).
 constexpr int kTogether = 4;
 
 template <int THREADS>
@@ -346,12 +346,13 @@ cudaError_t launch_large(const LogitsArgs& a, cudaStream_t st)
 template <typename TI, typename TO>
 cudaError_t launch(const LogitsArgs& a, int num_sms, cudaStream_t st)
 {
-    // Long stretches (8192 or 16384 values) for long rows once there are enough of them for all SMs.  Short and long ones take, with
-    // 2000 tokens a row, 3.7 and 6.0 us for 4 x 128000, 8.1 and 8.1 us for 16 x 128000, 24.5 and 17.9 us for 64 x 128000; 13.5 and 14.9
-    // us for 400 x 10000.  Of the long ones, 16384 values look through long histories less often: 28.2 and 25.5 us for 64 x 128000
-    // with 16000 tokens, 19.7 and 20.1 us with 4000.
-    if (a.vocab >= 16384 && (int64_t)a.rows * a.vocab >= (int64_t)num_sms * 12288)
-        return a.max_tokens > 8192 ? launch_large<TI, TO, 512>(a, st) : launch_large<TI, TO, 256>(a, st);
+    // Long stretches (8192 or 32768 values) for long rows once there are enough of them for all SMs.  Short and long ones take 4.9 and
+    // 5.5 us for 8 x 128000 with 4000 tokens a row, 6.9 and 6.4 us for 12 x 128000, 13.7 and 9.3 us for 32 x 128000; 10.0 and 11.3 us
+    // for 12 x 128000 with 16000 tokens, 13.6 and 12.8 us with 32768.  Of the long ones, 32768 values look through long histories less
+    // often: with 8192 and 32768, 64 x 128000 takes 14.5 and 16.2 us with 4000 tokens, 20.4 and 20.5 us with 12000, 26.9 and 23.1 us
+    // with 24000.
+    if (a.vocab >= 16384 && (int64_t)a.rows * a.vocab >= (int64_t)num_sms * 10240)
+        return a.max_tokens > 12288 ? launch_large<TI, TO, 1024>(a, st) : launch_large<TI, TO, 256>(a, st);
     // More threads look through a long history side by side: 1 x 128000 takes 7.3, 5.5, 5.3 us with 128, 256, 512 threads and 16000
     // tokens, 3.8, 3.5, 3.8 us with 4000, 3.2, 3.3, 3.7 us with 100.
     if (a.max_tokens > 8192) return launch_small<TI, TO, 512>(a, st);
@@ -362,7 +363,7 @@ template <typename TI, typename TO>
 cudaError_t configure()
 {
     const cudaError_t e = cudaFuncSetAttribute(adjust_logits_large_kernel<TI, TO, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Large<256>));
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(adjust_logits_large_kernel<TI, TO, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Large<512>));
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(adjust_logits_large_kernel<TI, TO, 1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Large<1024>));
 }
 
 }  // namespace

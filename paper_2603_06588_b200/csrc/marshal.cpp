@@ -21,6 +21,8 @@
 
 namespace {
 
+constexpr int kPage = 16;                        // tokens of a page
+
 struct Refused {
     const char* why;
 };
@@ -304,7 +306,7 @@ hook_cache_pool pool_of(Call& c, const at::Tensor** table = nullptr)
     p.num_seqs = narrow(t.size(0));
     p.max_blocks_per_seq = narrow(t.size(1));
     p.num_blocks = narrow(refs.size(0));
-    p.page_size = 16;
+    p.page_size = kPage;
     p.block_table = Call::pointer<int32_t>(&t);
     p.seq_lens = Call::pointer<int32_t>(&lens);
     p.page_refs = Call::pointer<int32_t>(&refs);

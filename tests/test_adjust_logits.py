@@ -302,3 +302,16 @@ def test_same_bits_every_time(eng):
     first = _check(eng, x, torch.float32, **kw).clone()
     for _ in range(3):
         assert torch.equal(_check(eng, x, torch.float32, **kw), first)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out,pad,in_place", [(torch.bfloat16, torch.float32, 0, False), (torch.float16, None, 3, True), (torch.float32, None, 0, True)])
+@pytest.mark.parametrize("rows,vocab,hist", [(13, 128000, 12289), (60, 32771, 20000), (130, 16384, 13000), (100, 16400, 12288)])
+def test_long_histories_in_large_batches(eng, dtype, out, pad, in_place, rows, vocab, hist):
+    """Stretches of 32768 values: rows of several, of one and of part of one."""
+    g, x, kw = _random(rows, vocab, dtype, hist, rows + vocab, bias=20)
+    kw["total"][:4] = hist, 0, 1, hist - 1
+    kw["prompt"][:4] = hist // 2, 0, 0, hist - 1
+    kw["total"][rows // 2] = -1
+    _check(eng, x, out, mask=g.random((5, vocab)) < 0.6, mask_rows=g.integers(-1, 5, rows).tolist(), pad=pad, in_place=in_place,
+           untouched=(rows // 2,), expect_status=binding.HOOK_ATTN_ERR_BOUNDS, **kw)

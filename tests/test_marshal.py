@@ -118,3 +118,12 @@ def test_results_are_the_tensors_given(eng):
     assert pairs.tolist() == [[-1, -1]] * 2 and pool["seq_lens"].tolist() == [1, 1]
     table, refs, page_map, moves, count = eng.hook_cache_compact(**pool)
     assert table.shape == (2, 3) and refs.shape == (8,) and page_map.shape == (8,) and moves.shape == (4, 2) and count.shape == (1,)
+
+
+@pytest.mark.gpu
+def test_closed_handle(eng):
+    mine = binding.HookAttn(0)
+    mine.close()
+    with pytest.raises(binding.HookAttnError) as e:
+        mine.hook_adjust_logits(torch.zeros((2, 40), device="cuda"))
+    assert e.value.code == binding.HOOK_ATTN_ERR_INVALID_ARG

@@ -20,6 +20,8 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = 8;       // rows per CTA at most: one warp looks each of them up
+template <int V>
+constexpr int kResident = V == 8 ? 6 : 8;      // CTAs on an SM: 40 registers with runs of eight (held to 32, 65536 rows take 443 us)
 
 // Where a row of the call goes.
 struct RowPlace {
@@ -176,25 +178,29 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
     }
 }
 
+template <typename T, int V>
+cudaError_t issue(RopeArgs& a, int num_sms, cudaStream_t st)
+{
+    // As many rows per CTA as let all CTAs be resident at once, up to kRopeRows (1024 rows of 32/8 heads: 7.1 us, and 9.1 us with a few
+    // CTAs in a second wave).
+    const int resident = num_sms * kResident<V>;
+    a.rows_per_cta = (a.total_q + resident - 1) / resident;
+    if (a.rows_per_cta > kRopeRows) a.rows_per_cta = kRopeRows;
+    rope_append_kernel<T, V><<<(a.total_q + a.rows_per_cta - 1) / a.rows_per_cta, kRopeThreads, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
 template <typename T>
 cudaError_t launch(RopeArgs& a, int num_sms, cudaStream_t st)
 {
-    // As many rows per CTA as let all CTAs be resident at once, up to kRopeRows (5003 rows: 11.6 us, and 13.1 us with one row less to a
-    // CTA and a second wave).
-    const int resident = num_sms * 8;
-    a.rows_per_cta = (a.total_q + resident - 1) / resident;
-    if (a.rows_per_cta > kRopeRows) a.rows_per_cta = kRopeRows;
-    const int grid = (a.total_q + a.rows_per_cta - 1) / a.rows_per_cta;
     // The widest run that divides the rotated half and the strides and on whose multiples the tensors start (16384 rows of 32/8 heads,
     // bf16: 75, 82, 123 and 201 us with runs of 8, 4, 2 and 1: the work to find an item is the same for all).
     const int64_t strides = a.q_row | a.q_head | a.k_row | a.k_head | a.v_row | a.v_head | a.pairs;
     const uintptr_t at = (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) / sizeof(T);
     const bool by16 = ((reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & 15) == 0;
-    if (((strides & 7) == 0) && by16) rope_append_kernel<T, 8><<<grid, kRopeThreads, 0, st>>>(a);
-    else if (((strides | at) & 3) == 0) rope_append_kernel<T, 4><<<grid, kRopeThreads, 0, st>>>(a);
-    else if (((strides | at) & 1) == 0) rope_append_kernel<T, 2><<<grid, kRopeThreads, 0, st>>>(a);
-    else rope_append_kernel<T, 1><<<grid, kRopeThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    if (((strides & 7) == 0) && by16) return issue<T, 8>(a, num_sms, st);
+    if (((strides | at) & 3) == 0) return issue<T, 4>(a, num_sms, st);
+    return ((strides | at) & 1) == 0 ? issue<T, 2>(a, num_sms, st) : issue<T, 1>(a, num_sms, st);
 }
 
 }  // namespace

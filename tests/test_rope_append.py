@@ -300,3 +300,14 @@ def test_tensors_elsewhere_are_refused(eng):
 def test_nothing_to_do(eng):
     c = _case([0, 0], [3, 4], 2, 2, 64, 32, torch.bfloat16)
     _check(eng, c, _freq(32), (32,))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seqs", [31, 128, 129, 1025, 4100])
+def test_many_sequences(eng, seqs):
+    """More of them than a warp looks at side by side, many without a row, in runs too."""
+    g = np.random.default_rng(seqs)
+    q_lens = g.integers(0, 4, seqs) * (g.random(seqs) < 0.6)
+    q_lens[seqs // 3:seqs // 2] = 0
+    q_lens[-1] = g.integers(0, 2)
+    _check(eng, _case(q_lens.tolist(), g.integers(0, 40, seqs).tolist(), 2, 1, 64, 32, torch.bfloat16), _freq(32), (32,))

@@ -304,7 +304,7 @@ def test_nothing_to_do(eng):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("seqs", [31, 128, 129, 1025, 4100])
-def test_many_sequences(eng, seqs):
+def test_sequences_narrowed_down(eng, seqs):
     """More of them than a warp looks at side by side, many without a row, in runs too."""
     g = np.random.default_rng(seqs)
     q_lens = g.integers(0, 4, seqs) * (g.random(seqs) < 0.6)

@@ -117,6 +117,7 @@ __global__ void __launch_bounds__(kListThreads) free_kernel(const PoolArgs p, co
 constexpr int kSplit = 1 << 30;                   // flag in a need: the last page is shared
 constexpr int kClusterCtas = 8;
 constexpr int kUnits = 1024;                      // counts of free pages that the cluster makes
+static_assert(kUnits == kPoolThreads, "a thread clears and sums one");
 
 template <int EACH, bool CLUSTER>
 __global__ void __launch_bounds__(kPoolThreads) extend_kernel(const PoolArgs p, const int32_t* __restrict__ new_rows,

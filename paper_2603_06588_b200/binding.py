@@ -116,19 +116,26 @@ class HookAttnError(RuntimeError):
 _lib = _compiled = None
 
 
+class _Missing:
+    """In the place of the compiled part where that cannot be loaded: the short calls raise, the others do not need it."""
+
+    def __init__(self, why: ImportError):
+        self.why = why
+
+    def __getattr__(self, name):
+        raise ImportError("the binding's compiled part (_marshal.so) is missing or does not fit this torch: build it with "
+                          "`python -m paper_2603_06588_b200.csrc.build`") from self.why
+
+
 def load_library() -> ctypes.CDLL:
-    """Load the compiled CUDA library; raises if it has not been built."""
+    """Load the compiled CUDA library; raises if it has not been built.  The compiled part of the binding is loaded beside it; where it
+    is missing, the calls that it marshals raise."""
     global _lib, _compiled
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError(
                 f"{LIB_PATH} is missing: build it with `python -m paper_2603_06588_b200.csrc.build` "
                 "(there is no fallback path)")
-        try:
-            from . import _marshal
-        except ImportError as e:
-            raise ImportError("the binding's compiled part (_marshal.so) is missing or does not fit this torch: build it with "
-                              "`python -m paper_2603_06588_b200.csrc.build`") from e
         lib = ctypes.CDLL(LIB_PATH)
         lib.hook_attn_create.restype = ctypes.c_int
         lib.hook_attn_create.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]
@@ -162,6 +169,10 @@ def load_library() -> ctypes.CDLL:
                                                       ctypes.c_void_p]
         lib.hook_attn_strerror.restype = ctypes.c_char_p
         lib.hook_attn_strerror.argtypes = [ctypes.c_int]
+        try:
+            from . import _marshal
+        except ImportError as e:
+            _marshal = _Missing(e)
         _lib, _compiled = lib, _marshal
     return _lib
 

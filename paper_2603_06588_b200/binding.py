@@ -123,7 +123,7 @@ class _Missing:
         self.why = why
 
     def __getattr__(self, name):
-        raise ImportError("the binding's compiled part (_marshal.so) is missing or does not fit this torch: build it with "
+        raise ImportError("the binding's compiled part (_marshal.so) is missing or was built for another torch or Python: build it with "
                           "`python -m paper_2603_06588_b200.csrc.build`") from self.why
 
 

@@ -40,8 +40,19 @@ def _newer(deps, target) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _marshal_stale() -> bool:
+    """Older than its sources, or made for another torch or Python than these, which it says when it is imported."""
+    if _newer([MARSHAL_SRC] + headers(), MARSHAL):
+        return True
+    try:
+        from .. import _marshal  # noqa: F401
+    except ImportError:
+        return True
+    return False
+
+
 def needs_build() -> bool:
-    return _newer(sources() + headers(), LIB) or _newer([MARSHAL_SRC] + headers(), MARSHAL)
+    return _newer(sources() + headers(), LIB) or _marshal_stale()
 
 
 def _build_marshal(verbose: bool) -> None:
@@ -49,7 +60,7 @@ def _build_marshal(verbose: bool) -> None:
     base = os.path.dirname(torch.__file__)
     cuda = os.path.join(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")), "..", "include")
     cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-Wall", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", f'-DHOOK_TORCH_VERSION="{torch.__version__}"']
     for path in (os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], cuda):
         cmd += ["-isystem", path]
     cmd += [MARSHAL_SRC, "-o", MARSHAL, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
@@ -81,7 +92,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-3] + ".o") for s in sources()]
     subprocess.run([nvcc, "-shared", "-cudart", "static", "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB] + objs,
                    check=True)
-    if force or _newer([MARSHAL_SRC] + headers(), MARSHAL):        # last: the attention's calls do without it
+    if force or _marshal_stale():        # last: the attention's calls do without it
         _build_marshal(verbose)
     return LIB
 

@@ -436,6 +436,19 @@ PyMethodDef methods[] = {CALL(rope_append), CALL(adjust_logits), CALL(cache_fork
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the short calls of libhook_attn.so.", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 
+// This file reads tensors by the layout of the torch and the Python that it was compiled for: with others it is not loaded.
+bool made_for_these()
+{
+    PyObject* torch = Py_Version >> 16 == PY_VERSION_HEX >> 16 ? PyImport_ImportModule("torch") : nullptr;
+    PyObject* version = torch ? PyObject_GetAttrString(torch, "__version__") : nullptr;
+    Py_XDECREF(torch);
+    const bool same = version && PyUnicode_Check(version) && PyUnicode_CompareWithASCIIString(version, HOOK_TORCH_VERSION) == 0;
+    if (!PyErr_Occurred() && !same)
+        PyErr_Format(PyExc_ImportError, "_marshal.so was built for torch %s and Python %d.%d", HOOK_TORCH_VERSION, PY_MAJOR_VERSION, PY_MINOR_VERSION);
+    Py_XDECREF(version);
+    return same;
+}
+
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&definition); }
+PyMODINIT_FUNC PyInit__marshal() { return made_for_these() ? PyModule_Create(&definition) : nullptr; }

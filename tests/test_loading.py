@@ -37,6 +37,10 @@ def _run(tmp_path, code, compiled):
     for name in os.listdir(PKG):
         if name.endswith((".py", ".so")) and (compiled or not name.startswith("_marshal")):
             os.symlink(os.path.join(PKG, name), copy / name)
+    _again(tmp_path, code)
+
+
+def _again(tmp_path, code):
     got = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, env=dict(os.environ, PYTHONPATH=str(tmp_path)), capture_output=True, text=True,
                          timeout=300)
     assert got.returncode == 0, got.stderr[-2000:]
@@ -48,3 +52,16 @@ def test_the_attention_loads_without_the_compiled_part(tmp_path):
 
 def test_with_the_compiled_part_the_short_calls_are_there(tmp_path):
     _run(tmp_path, HANDLE + "assert callable(eng._marshal.rope_append) and eng._marshal.__file__.endswith('.so')\n", compiled=True)
+
+
+def test_a_compiled_part_for_another_torch_is_refused(tmp_path):
+    """Its calls raise, and the build sees that it has to be made again."""
+    other = "import torch\ntorch.__version__ = '1.0.0'\n"
+    stale = ("from paper_2603_06588_b200.csrc import build\nbuild._newer = lambda deps, target: False\nassert build.needs_build() is %s\n"
+             "try:\n    from paper_2603_06588_b200 import _marshal\nexcept ImportError as e:\n    assert 'torch' in str(e)\nelse:\n    assert not %s\n")
+    _run(tmp_path, other + HANDLE + CALLS, compiled=True)
+    (tmp_path / "paper_2603_06588_b200" / "csrc").mkdir()
+    for name in ("__init__.py", "build.py"):
+        os.symlink(os.path.join(PKG, "csrc", name), tmp_path / "paper_2603_06588_b200" / "csrc" / name)
+    _again(tmp_path, other + stale % (True, True))
+    _again(tmp_path, stale % (False, False))

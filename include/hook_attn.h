@@ -329,8 +329,8 @@ typedef struct {
 
 /* children[i] becomes a copy of sequence parents[i] that shares its pages (no data moves).  An entry is passed
  * over, with status HOOK_ATTN_ERR_BOUNDS, when one of its rows does not exist, its child is not empty, is named by
- * an earlier entry or is a parent in this call, or the parent's length or pages are out of range.  At most 16384
- * entries, here and in hook_cache_free. */
+ * an earlier entry or is a parent in this call, or the parent's length or pages are out of range or nobody holds one of
+ * its pages.  At most 16384 entries, here and in hook_cache_free. */
 int hook_cache_fork(hook_attn_handle* handle, const hook_cache_pool* pool, const int32_t* parents, const int32_t* children,
                     int32_t num_forks, void* cuda_stream);
 

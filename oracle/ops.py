@@ -120,7 +120,7 @@ class Pool:
                 self.faults.append("bounds")
                 continue
             held = self.table[a][:self._pages(self.lens[a])]
-            if any(not 0 <= p < len(self.refs) for p in held):
+            if any(not 0 <= p < len(self.refs) or self.refs[p] <= 0 for p in held):
                 self.faults.append("bounds")
                 continue
             self.table[b][:len(held)] = held

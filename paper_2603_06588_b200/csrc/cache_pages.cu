@@ -47,7 +47,8 @@ __device__ __forceinline__ uint32_t free_pages(const PoolArgs& p, int base)
 }
 
 // One CTA per entry: children[i] gets the pages of parents[i].  An entry is refused (status) when a row is out of range, the
-// child holds pages, the child is listed earlier, the child is a parent of the same call, or the parent's row is broken.
+// child holds pages, the child is listed earlier, the child is a parent of the same call, or the parent's row is broken: its length or
+// a page is out of range, or nobody holds a page of it.  Which counts are above 0 does not change during the call.
 __global__ void __launch_bounds__(kListThreads) fork_kernel(const PoolArgs p, const int32_t* __restrict__ parents,
                                                             const int32_t* __restrict__ children, int n)
 {
@@ -61,7 +62,7 @@ __global__ void __launch_bounds__(kListThreads) fork_kernel(const PoolArgs p, co
     }
     const int pages = bad ? 0 : pages_of(L);
     const int32_t* from = p.block_table + (int64_t)parent * p.max_blocks;
-    for (int j = threadIdx.x; j < pages; j += kListThreads) bad |= !page_ok(p, from[j]);
+    for (int j = threadIdx.x; j < pages; j += kListThreads) bad |= !page_ok(p, from[j]) || p.page_refs[from[j]] <= 0;
     if (__syncthreads_or(bad)) {
         if (threadIdx.x == 0) report(p.status, HOOK_ATTN_ERR_BOUNDS);
         return;

@@ -473,3 +473,25 @@ def test_pools_in_a_graph_on_another_stream(eng, num_blocks):
         assert [tuple(p) for p in pairs.tolist()] == want_pairs
         assert table.tolist() == want_table and refs.tolist() == want_refs and page_map.tolist() == want_map and count.tolist() == [len(want_moves)]
         assert [tuple(p) for p in moves.tolist()] == want_moves + [(-1, -1)] * (num_blocks // 2 - len(want_moves))
+
+
+def test_oracle_forks_held_pages_alone():
+    pool = ops.Pool(3, 2, 4)
+    pool.extend([20, 0, 0])
+    pool.refs[1] = 0
+    pool.fork([0], [1])
+    assert pool.faults == ["bounds"] and pool.lens == [20, 0, 0] and pool.refs == [1, 0, 0, 0]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [0, -2])
+def test_pages_that_nobody_holds_are_not_forked(eng, count):
+    """A fork would raise their count to 1, and parent and child would then append into one page that neither seems to share."""
+    both = Both(eng, 7, 4, 30)
+    both.extend([20, 33, 5, 0, 0, 0, 0])
+    both.want.refs[both.want.table[0][1]] = count
+    both.want.refs[both.want.table[2][0]] = count
+    both.load()
+    both.fork([0, 1, 0, 2], [3, 4, 5, 6])
+    assert both.want.lens == [20, 33, 5, 0, 33, 0, 0]
+    both.extend([0, 1, 0, 0, 1, 0, 0])

@@ -502,7 +502,7 @@ int hook_adjust_logits(hook_attn_handle* handle, const hook_logits_params* p, vo
     a.tokens = p->tokens; a.token_row = p->tokens_row_stride;
     a.prompt_lens = p->prompt_lens; a.total_lens = p->total_lens;
     a.repetition = p->repetition; a.presence = p->presence; a.frequency = p->frequency;
-    a.bias_offsets = p->num_bias > 0 ? p->bias_offsets : nullptr;
+    a.bias_offsets = p->bias_offsets;             // of an empty list too: they may name entries that are not there
     a.bias_tokens = p->bias_tokens; a.bias_values = p->bias_values;
     a.mask = p->mask; a.mask_row = p->mask_row_stride; a.mask_rows = p->mask_rows;
     a.status = p->status;

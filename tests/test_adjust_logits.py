@@ -315,3 +315,14 @@ def test_long_histories_in_large_batches(eng, dtype, out, pad, in_place, rows, v
     kw["total"][rows // 2] = -1
     _check(eng, x, out, mask=g.random((5, vocab)) < 0.6, mask_rows=g.integers(-1, 5, rows).tolist(), pad=pad, in_place=in_place,
            untouched=(rows // 2,), expect_status=binding.HOOK_ATTN_ERR_BOUNDS, **kw)
+
+
+@pytest.mark.gpu
+def test_offsets_into_an_empty_list_of_biases(eng):
+    x = torch.randn(2, 50, generator=torch.Generator().manual_seed(1)).cuda()
+    t = lambda a, dtype=torch.int32: torch.tensor(a, dtype=dtype, device="cuda")
+    kw = dict(bias_tokens=t([]), bias_values=t([], torch.float32))
+    for offsets, code in (([0, 0, 0], 0), ([0, 0, 3], binding.HOOK_ATTN_ERR_BOUNDS)):
+        status, out = t([0]), torch.full_like(x, 3.0)
+        eng.hook_adjust_logits(x, out=out, bias_offsets=t(offsets), status=status, **kw)
+        assert int(status.item()) == code and torch.equal(out[0], x[0]) and torch.equal(out[1], torch.full_like(x[1], 3.0) if code else x[1])

@@ -270,7 +270,8 @@ PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t n)
             check(prompt && total, "prompt_lens and total_lens with tokens");
             p.max_tokens = narrow(tokens->size(1));
             p.tokens_row_stride = tokens->stride(0);
-            p.tokens = Call::pointer<int32_t>(tokens);
+            // a buffer without room has no address, but lengths that are checked: any address stands for it, none of it is read
+            p.tokens = tokens->size(1) > 0 ? Call::pointer<int32_t>(tokens) : Call::pointer<int32_t>(total);
             p.prompt_lens = Call::pointer<int32_t>(prompt);
             p.total_lens = Call::pointer<int32_t>(total);
         }

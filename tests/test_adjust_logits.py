@@ -326,3 +326,17 @@ def test_offsets_into_an_empty_list_of_biases(eng):
         status, out = t([0]), torch.full_like(x, 3.0)
         eng.hook_adjust_logits(x, out=out, bias_offsets=t(offsets), status=status, **kw)
         assert int(status.item()) == code and torch.equal(out[0], x[0]) and torch.equal(out[1], torch.full_like(x[1], 3.0) if code else x[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab", [(2, 50), (100, 20000)])
+def test_histories_in_a_buffer_without_room(eng, rows, vocab):
+    x = torch.randn(rows, vocab, generator=torch.Generator().manual_seed(1)).cuda()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    tokens, total, status, out = torch.zeros((rows, 0), **i32), torch.zeros(rows, **i32), torch.zeros(1, **i32), torch.full_like(x, 3.0)
+    kw = dict(out=out, tokens=tokens, prompt_lens=torch.zeros(rows, **i32), total_lens=total, frequency=torch.ones(rows, device="cuda"), status=status)
+    assert torch.equal(eng.hook_adjust_logits(x, **kw), x) and int(status.item()) == 0
+    total[1] = 5
+    out.fill_(3.0)
+    eng.hook_adjust_logits(x, **kw)
+    assert int(status.item()) == binding.HOOK_ATTN_ERR_BOUNDS and (out[1] == 3.0).all() and torch.equal(out[0], x[0]) and torch.equal(out[2:], x[2:])

@@ -312,7 +312,7 @@ typedef struct {
 
 /* Edits of the logits before a token is chosen, in 32 bits with one rounding to out's type.  With c the number of
  * times token v was generated in the row, and `seen` whether it is in its prompt or generated:
- *   x = seen ? (x > 0 ? x / repetition : x * repetition) : x;   x -= frequency * c + presence * (c > 0);
+ *   x = seen ? (x > 0 ? x / repetition : x * repetition) : x;   x -= frequency * c + presence  if c > 0 (either may be infinite);
  *   x += bias[v];   x = -inf if the grammar forbids v (whatever x is; a mask may forbid all).
  * A row whose lengths, bias offsets or mask row are out of range sets status and its part of out is not written; a
  * bias for a token outside the vocabulary sets status and is passed over.  vocab_size <= 2^20, max_tokens < 2^20, num_rows < 2^16. */

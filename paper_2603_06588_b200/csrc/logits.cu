@@ -100,7 +100,7 @@ __device__ __forceinline__ float edit(float x, uint32_t word, const Stretch& r)
 {
     const uint32_t made = word & kCountMask;
     const float scale = word & (kSeen | kCountMask) ? (x > 0.f ? r.inv_rep : r.rep) : 1.f;
-    x = x * scale - (r.freq * (float)made + (made ? r.pres : 0.f));
+    x = x * scale - (made ? r.freq * (float)made + r.pres : 0.f);         // an infinite penalty is none for what was not generated
     if (word & kPlaceMask) x += r.bias[((word & kPlaceMask) >> kCountBits) - 1];
     return x;
 }

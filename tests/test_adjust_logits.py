@@ -340,3 +340,12 @@ def test_histories_in_a_buffer_without_room(eng, rows, vocab):
     out.fill_(3.0)
     eng.hook_adjust_logits(x, **kw)
     assert int(status.item()) == binding.HOOK_ATTN_ERR_BOUNDS and (out[1] == 3.0).all() and torch.equal(out[0], x[0]) and torch.equal(out[2:], x[2:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab", [(3, 777), (100, 20000)])
+def test_infinite_frequency_penalties(eng, rows, vocab):
+    """They rule out what was generated, and nothing else: a token of the prompt or the biases was generated no times."""
+    g, x, kw = _random(rows, vocab, torch.float32, 100, 17, bias=9)
+    _check(eng, x, **dict(kw, freq=[float("inf")] * rows))
+    _check(eng, x, **dict(kw, pres=[float("inf")] * rows))

@@ -349,3 +349,24 @@ def test_infinite_frequency_penalties(eng, rows, vocab):
     g, x, kw = _random(rows, vocab, torch.float32, 100, 17, bias=9)
     _check(eng, x, **dict(kw, freq=[float("inf")] * rows))
     _check(eng, x, **dict(kw, pres=[float("inf")] * rows))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rep", [2.0 ** -149, 1e-40, 2.0 ** -127, 2.0 ** -126, 1e-25, 2.0 ** -64, 1.0, 2.0 ** 64, 1e25, 2.0 ** 126, 2.0 ** 127, 3.4e38])
+@pytest.mark.parametrize("rows,vocab", [(2, 400), (100, 16400)])
+def test_repetition_penalties_over_the_whole_range(eng, rep, rows, vocab):
+    """The reciprocal and the product with it are rounded to 24 bits, powers of 2 aside: 2 x 2^-24, and a step of the numbers next to zero."""
+    g = np.random.default_rng(vocab)
+    x = (g.choice([-1.0, 1.0], (rows, vocab)) * np.exp2(g.uniform(-126, 127, (rows, vocab)))).astype(np.float32)
+    dev = torch.from_numpy(x).cuda()
+    tokens = torch.arange(vocab, dtype=torch.int32, device="cuda").expand(rows, vocab)
+    lens = torch.full((rows,), vocab, dtype=torch.int32, device="cuda")
+    got = eng.hook_adjust_logits(dev, out=torch.empty_like(dev), tokens=tokens, prompt_lens=lens, total_lens=lens,
+                                 repetition=torch.full((rows,), rep, device="cuda")).double().cpu().numpy()
+    r, x = float(np.float32(rep)), x.astype(np.float64)
+    want = np.where(x > 0, x / r, x * r)
+    top = float(np.finfo(np.float32).max)
+    near = np.abs(np.abs(want) / top - 1) <= 2.0 ** -22             # rounded to infinity or to the largest number
+    assert np.array_equal(got[(np.abs(want) > top) & ~near], np.copysign(np.inf, want[(np.abs(want) > top) & ~near]))
+    fine = (np.abs(want) <= top) & ~near
+    assert np.all(np.abs(got - want)[fine] <= np.abs(want[fine]) * 2.0 ** -23 + 2.0 ** -149)

@@ -371,7 +371,8 @@ typedef struct {
 
 /* Copies pages in the caches of all layers.  A source may have many destinations.  The pairs are independent of one
  * another: one whose destination is also another pair's destination or source, or whose source is another pair's
- * destination, is not carried out and sets status, like one outside the pool. */
+ * destination, is not carried out and sets status, like one outside the pool.  They are held against one another, which takes a time that
+ * grows with the square of their number (2^18 pairs: 30 ms): of more than 2^22 that count, none is carried out and status is set. */
 int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params* p, void* cuda_stream);
 
 /* Human-readable name of a return / status code. */

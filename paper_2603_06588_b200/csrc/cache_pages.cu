@@ -378,8 +378,14 @@ __global__ void __launch_bounds__(kListThreads) finish_kernel(const PoolArgs p, 
 // fixed number of CTAs goes through the units, slab after slab (page after page, all slabs of each: 62 -> 69 us for 256 pairs in 32
 // slabs).  32 CTAs for an SM: with one for each unit that there could be, 20 of 2048 pairs in 32 slabs take 36 us, with 64 10 us, with
 // 32 7 us; all 2048 take 1 % longer than with 64.  Bound by HBM (983 pages of 16 layers, 2.1 GB read and written: 320 us, the copy rate).
+//
+// The check's time grows with the square of the list, whose length the host does not know: lists of more than kMostPairs pairs are refused.
+// From kLong on there are units enough for all CTAs when each has all slabs, so that its pairs are checked once (2 KB pages: 2^18 pairs 30 ms, of which
+// the copies of a layer take 0.3; 2^20 pairs 0.5 s, 2^22 pairs 7.5 s).
 constexpr int kChecked = 8;                      // pairs of a unit at most
 constexpr int kMany = 2048;
+constexpr int kLong = 1 << 16;
+constexpr int kMostPairs = 1 << 22;
 constexpr int kCopyCtas = 32;
 
 // TIGHT: a page's tokens and heads follow one another without gaps, in either order.  CHECKED: 1 for lists that cannot be long (the
@@ -390,8 +396,12 @@ __global__ void __launch_bounds__(kListThreads, CHECKED == 1 ? 6 : 4) copy_pages
     __shared__ uint32_t refused;
     const int n = a.num_pairs ? min(max(*a.num_pairs, 0), a.max_pairs) : a.max_pairs, slabs = 2 * a.layers;
     if (n == 0) return;
+    if (CHECKED > 1 && n > kMostPairs) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        return;
+    }
     const bool many = CHECKED > 1 && n > kMany;
-    const uint32_t pairs = many ? CHECKED : 1, some = many ? min(slabs, 4) : 1;              // of a unit
+    const uint32_t pairs = many ? CHECKED : 1, some = !many ? 1 : n > kLong ? slabs : min(slabs, 4);              // of a unit
     const uint32_t groups = ((uint32_t)n + pairs - 1) / pairs, rows = (slabs + some - 1) / some;
     const uint32_t next_group = gridDim.x % groups, next_row = gridDim.x / groups;
     const int per_row = a.head_dim / 8, pieces = kPage * a.Hkv * per_row;

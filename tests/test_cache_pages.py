@@ -495,3 +495,38 @@ def test_pages_that_nobody_holds_are_not_forked(eng, count):
     both.fork([0, 1, 0, 2], [3, 4, 5, 6])
     assert both.want.lens == [20, 33, 5, 0, 33, 0, 0]
     both.extend([0, 1, 0, 0, 1, 0, 0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counted", [False, True])
+def test_lists_longer_than_can_be_checked(eng, counted):
+    """Refused as a whole: held against one another, 2^30 pairs would keep the device busy for days."""
+    n, i32 = 2 ** 22 + 1, dict(dtype=torch.int32, device="cuda")
+    cache = torch.ones((2, 4, 16, 1, 64), dtype=torch.bfloat16, device="cuda")
+    cache[:, 1] = 2.0
+    before, status = cache.clone(), torch.zeros(1, **i32)
+    pairs = torch.full((n, 2), -1, **i32)
+    pairs[0] = torch.tensor([0, 1], **i32)
+    eng.hook_cache_copy_pages([(cache[0], cache[1])], pairs, torch.tensor([n], **i32) if counted else None, status=status)
+    assert int(status.item()) == binding.HOOK_ATTN_ERR_BOUNDS and torch.equal(cache, before)
+    eng.hook_cache_copy_pages([(cache[0], cache[1])], pairs, torch.tensor([1], **i32), status=status.zero_())      # a long list of which little counts
+    assert int(status.item()) == 0 and (cache[:, 1] == 1.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [2 ** 16, 2 ** 16 + 1, 265001])
+def test_copy_of_long_lists(eng, count):
+    """On both sides of the length from which a unit has all slabs, with pairs that depend on one another."""
+    pages, g = 2 * 265001 + 3, torch.Generator(device="cuda").manual_seed(count)
+    pairs = torch.randperm(pages, generator=g, device="cuda")[:2 * 265001].reshape(-1, 2).int()
+    pairs[5000, 1] = pairs[60000, 1]
+    pairs[9, 0] = -1
+    cache = torch.randint(-2 ** 15, 2 ** 15, (3, 2, pages, 16, 1, 64), generator=g, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    want, status = cache.clone().view(torch.int16), torch.zeros(1, dtype=torch.int32, device="cuda")
+    eng.hook_cache_copy_pages([(c[0], c[1]) for c in cache], pairs, torch.tensor([count], dtype=torch.int32, device="cuda"), status=status)
+    live = torch.ones(count, dtype=torch.bool, device="cuda")
+    live[[9, 5000, 60000]] = False
+    src, dst = pairs[:count][live].long().T
+    for layer in want:
+        layer[:, dst] = layer[:, src]
+    assert torch.equal(cache.view(torch.int16), want) and int(status.item()) == binding.HOOK_ATTN_ERR_BOUNDS

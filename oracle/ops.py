@@ -5,7 +5,6 @@ Test infrastructure only; shares nothing with the CUDA code.
 from __future__ import annotations
 
 import collections
-import math
 
 import numpy as np
 
@@ -27,18 +26,18 @@ def axis_of_pair(axis_pairs, cyclic: bool):
 
 
 def rotate(x, pos, inv_freq, axis_pairs, cyclic, adjacent, factor):
-    """``x`` float64 ``[T, H, D]``, ``pos`` ``[axes, T]``.  Returns the rotated array and the sum of the magnitudes of the two
-    products that each element is the sum of (what its rounding errors scale with)."""
+    """``x`` float64 ``[T, H, D]``, ``pos`` ``[axes, T]``, ``inv_freq`` of 24 bits each.  Returns the rotated array and the sum of the
+    magnitudes of the two products that each element is the sum of (what its rounding errors scale with)."""
+    assert np.finfo(np.longdouble).nmant >= 63            # a position times a frequency has up to 32 + 24 bits: exact
     out, scale = x.copy(), np.abs(x)
     half = len(inv_freq)
     for p, axis in enumerate(axis_of_pair(axis_pairs, cyclic)):
         i, j = (2 * p, 2 * p + 1) if adjacent else (p, p + half)
-        for t in range(x.shape[0]):
-            angle = int(pos[axis][t]) * float(inv_freq[p])
-            c, s = factor * math.cos(angle), factor * math.sin(angle)
-            a, b = x[t, :, i].copy(), x[t, :, j].copy()
-            out[t, :, i], out[t, :, j] = a * c - b * s, b * c + a * s
-            scale[t, :, i] = scale[t, :, j] = abs(factor) * (np.abs(a) + np.abs(b))
+        angle = np.asarray(pos[axis], dtype=np.longdouble) * np.longdouble(inv_freq[p])
+        c, s = (factor * f(angle).astype(np.float64)[:, None] for f in (np.cos, np.sin))
+        a, b = x[:, :, i], x[:, :, j]
+        out[:, :, i], out[:, :, j] = a * c - b * s, b * c + a * s
+        scale[:, :, i] = scale[:, :, j] = abs(factor) * (np.abs(a) + np.abs(b))
     return out, scale
 
 

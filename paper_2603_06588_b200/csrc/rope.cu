@@ -3,8 +3,9 @@
 //   angle = position[axis of the pair][row] * inv_freq[pair],   (a, b) -> factor * (a cos - b sin, b cos + a sin);
 // q goes to a contiguous bf16 tensor, k and v to the page slots of the rows.
 //
-// Angles: position * inv_freq is exact in 64 bits (31 + 24 bits) and is brought to [-1/2, 1/2] turns there; in 32 bits a
-// position of a million would be off by 0.06 rad.  The rest is 32-bit, with one rounding to bf16 at the store.
+// Angles: position * inv_freq / (2 pi) is brought to [-1/2, 1/2] turns in 64 bits.  The two products and the constant are rounded to 53
+// bits each, so a turn is off by at most 3 x 2^-53 of the turns: by 1.1e-7 at 2^31 rad.  In 32 bits a position of a million would be off by
+// 0.06 rad.  The rest is 32-bit, with one rounding to bf16 at the store.
 #include "common.cuh"
 #include "ops.cuh"
 

@@ -311,3 +311,26 @@ def test_sequences_narrowed_down(eng, seqs):
     q_lens[seqs // 3:seqs // 2] = 0
     q_lens[-1] = g.integers(0, 2)
     _check(eng, _case(q_lens.tolist(), g.integers(0, 40, seqs).tolist(), 2, 1, 64, 32, torch.bfloat16), _freq(32), (32,))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_the_farthest_positions(eng, dtype, adjacent):
+    """Positions next to the last integers.  The product with the frequency, the one with 1 / (2 pi) and that constant are rounded to 53 bits
+    before the whole turns go: 3 x 2^-53 x 2^31 f = 3 f 2^-22 rad, for f <= 1/16 below 0.19 x 2^-22.  Beside it the reduced angle (2 pi 2^-26 =
+    0.4 x 2^-22), sine and cosine (a unit: 2^-24), the factor, a product and the sum (3 x 2^-24): 1.6 x 2^-22 together, below 2^-21."""
+    c = _case([40], [0], 2, 1, 64, 32, dtype)
+    g = np.random.default_rng(3)
+    pos = np.stack([2 ** 31 - 1 - g.integers(0, 100, 40), -2 ** 31 + g.integers(0, 100, 40), g.integers(-2 ** 31, 2 ** 31, 40)])
+    _check(eng, c, [f / 16 for f in _freq(32, 4.0)], (8, 12, 12), adjacent=adjacent, positions=torch.from_numpy(pos).int())
+
+
+def test_oracle_of_far_positions():
+    """Against angles reduced in whole numbers: 2 pi to 60 digits."""
+    tau = 6283185307179586476925286766559005768394338798750211641949889
+    x = np.array([[[1.0, 0.0]]])
+    for pos, freq in ((2 ** 31 - 1, 1 - 2.0 ** -24), (-2 ** 31, 0.75), (2 ** 31 - 12345, 2.0 ** -7 + 2.0 ** -30)):
+        angle = pos * int(freq * 2 ** 60) * 10 ** 60 % (tau * 2 ** 60) / (10 ** 60 * 2 ** 60)
+        out, _ = ops.rotate(x, [[pos]], [freq], [1], False, False, 1.0)
+        assert np.abs(out[0, 0] - [math.cos(angle), math.sin(angle)]).max() < 2.0 ** -50

@@ -334,3 +334,43 @@ def test_oracle_of_far_positions():
         angle = pos * int(freq * 2 ** 60) * 10 ** 60 % (tau * 2 ** 60) / (10 ** 60 * 2 ** 60)
         out, _ = ops.rotate(x, [[pos]], [freq], [1], False, False, 1.0)
         assert np.abs(out[0, 0] - [math.cos(angle), math.sin(angle)]).max() < 2.0 ** -50
+
+
+def _long_case(rows, pairs, dtype, seed, broken=True, **kw):
+    """Packed prompts of some ten rows each, two of them broken, five rows of padding at the end."""
+    g = np.random.default_rng(seed)
+    n = g.integers(0, 21, rows // 8)
+    n = n[:int(np.searchsorted(np.cumsum(n), rows - 50))].tolist()
+    n.append(rows - sum(n))
+    c = _case(n, g.integers(0, 40, len(n)).tolist(), 2, 1, 64, pairs, dtype, seed=seed, **kw)
+    if broken:
+        c["block_table"][len(n) // 3, 0] = -1
+        c["seq_lens"][len(n) // 2] = 16 * c["block_table"].shape[1] + 1
+        c["cu_q_lens"][-1] -= 5
+        c["seq_lens"][-1] -= 5
+    return c
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("axis_pairs", [(8, 12, 12), (3, 9), (5, 0, 1), (16, 15)])
+def test_several_rows_to_a_block(eng, dtype, adjacent, axis_pairs):
+    """Runs of eight, four, two and one elements, good and broken rows and padding side by side."""
+    c = _long_case(2531, sum(axis_pairs), dtype, sum(axis_pairs))
+    assert c["cu_q_lens"][-1] == 2526
+    _check(eng, c, _freq(sum(axis_pairs)), axis_pairs, True, adjacent, 0.75, _axes_positions(2531, len(axis_pairs), 3), expect_status=binding.HOOK_ATTN_ERR_BOUNDS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("axis_pairs,dtype", [((8, 12, 12), torch.bfloat16), ((5, 0, 1), torch.float32)])
+def test_as_many_rows_to_a_block_as_there_can_be(eng, axis_pairs, dtype):
+    c = _long_case(10007, sum(axis_pairs), dtype, 7)
+    _check(eng, c, _freq(sum(axis_pairs)), axis_pairs, positions=_axes_positions(10007, len(axis_pairs), 3), expect_status=binding.HOOK_ATTN_ERR_BOUNDS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_in_place_queries_of_several_rows_to_a_block(eng, adjacent):
+    c = _long_case(2503, 32, torch.bfloat16, 9, broken=False, fused=False)
+    _check(eng, c, _freq(32), (32,), adjacent=adjacent, in_place=True)

@@ -176,25 +176,23 @@ struct History {
     }
 };
 
-// Puts one of the row's biases into its word: of a token that is named twice the last entry counts.  Returns the place of the word
-// where it was zero, else -1.
-__device__ __forceinline__ int place_bias(const LogitsArgs& a, const Stretch& s, uint32_t* word, int i)
+// Puts one of the row's biases into its word: of a token that is named twice the last entry counts.
+__device__ __forceinline__ void place_bias(const LogitsArgs& a, const Stretch& s, uint32_t* word, int i)
 {
     const int t = a.bias_tokens[i];
     if (t < 0 || t >= a.vocab) {
         if (s.lo == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
-        return -1;
+        return;
     }
-    if ((unsigned)t - (unsigned)s.lo >= (unsigned)(s.hi - s.lo)) return -1;
+    if ((unsigned)t - (unsigned)s.lo >= (unsigned)(s.hi - s.lo)) return;
     uint32_t* w = &word[t - s.first];
     uint32_t old = *w;
     const uint32_t mine = (uint32_t)(i - s.b0 + 1) << kCountBits;
     while ((old & kPlaceMask) < mine) {
         const uint32_t was = atomicCAS(w, old, (old & ~kPlaceMask) | mine);
-        if (was == old) return old == 0 ? t - s.first : -1;
+        if (was == old) return;
         old = was;
     }
-    return -1;
 }
 
 // Eight values that begin at v, with the words of the stretch; `low` and `high` are the mask's words of the first and the last.

@@ -276,9 +276,10 @@ __global__ void __launch_bounds__(THREADS) adjust_logits_kernel(const __grid_con
 
 // Large calls: a CTA takes a long stretch, all of whose loads are under way while its words are filled; four CTAs of 256 threads on an
 // SM or one of 1024, with 64 registers each.  Without a history it is bound by HBM (256 rows of 160000 fp32 values with masks: 54 us, 6.1
-// TB/s).  With one, by the chain of loads before a stretch's edits and by the issue slots: each stretch of a row looks through the whole
-// history, and a warp runs the edit for each of the eight values of a lane that any of its lanes has a word for (the same with
-// histories of up to 4096 tokens: 71 us, 4.7 TB/s; 64 rows of 128000 bf16 to fp32 values with up to 32768 tokens: 27 us, 2.0 TB/s).
+// TB/s).  With one, by phases that do not cover one another, with half of the issue slots and of the bandwidth in use: each stretch of a row looks
+// through the whole history, and a warp runs the edit for each of the eight values of a lane that any of its lanes has a word for (the same with
+// histories of up to 4096 tokens: 72 us, 4.6 TB/s; 64 rows of 128000 bf16 to fp32 values with up to 32768 tokens: 27 us, 2.0 TB/s, in two
+// waves of CTAs: 37 rows, one wave, take 13 us).
 constexpr int kTogether = 4;
 
 template <int THREADS>
@@ -363,7 +364,8 @@ cudaError_t launch_large(const LogitsArgs& a, cudaStream_t st)
 template <typename TI, typename TO>
 cudaError_t launch(const LogitsArgs& a, int num_sms, cudaStream_t st)
 {
-    // Long stretches (8192 or 32768 values) for long rows once there are enough of them for all SMs.  Short and long ones take 4.9 and
+    // By the width of the token buffer, since the histories' lengths are on the device: shorter histories in a wide buffer take the times of the
+    // form for wide ones.  Long stretches (8192 or 32768 values) for long rows once there are enough of them for all SMs.  Short and long ones take 4.9 and
     // 5.5 us for 8 x 128000 with 4000 tokens a row, 6.9 and 6.4 us for 12 x 128000, 13.7 and 9.3 us for 32 x 128000; 10.0 and 11.3 us
     // for 12 x 128000 with 16000 tokens, 13.6 and 12.8 us with 32768.  Of the long ones, 32768 values look through long histories less
     // often: with 8192 and 32768, 64 x 128000 takes 14.5 and 16.2 us with 4000 tokens, 20.4 and 20.5 us with 12000, 26.9 and 23.1 us

@@ -102,7 +102,7 @@ __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&x)[V])
 // A CTA takes a few rows.  An item is two runs of V elements of one head: V pairs that turn, or 2 V elements that are only
 // moved; the thread that reads them writes them, so the queries may be rotated in place.  Bound by HBM: every element is read
 // once and written once, and a row's cosines and sines (R / 2 of them) are computed once for all its heads (65536 rows of 64/8
-// heads: 427 us, 6.3 TB/s; with the next item's loads under way during an item, 484 us: fewer CTAs fit an SM).  Small calls are
+// heads: 427 to 437 us, 6.1 to 6.3 TB/s; with the next item's loads under way during an item, 484 us: fewer CTAs fit an SM).  Small calls are
 // bound by the chain of loads before the first store (one row: 3.0 us).
 template <typename T, int V>
 __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_constant__ RopeArgs a)

@@ -113,9 +113,11 @@ class Pool:
         return 0 <= s < len(self.lens)
 
     def fork(self, parents, children):
-        before = list(self.lens)
-        for i, (a, b) in enumerate(zip(parents, children)):
-            if not (self._row(a) and self._row(b)) or b in parents or b in children[:i] or before[b] != 0 or not self._len_ok(self.lens[a]):
+        before, copied, named = list(self.lens), set(parents), set()
+        for a, b in zip(parents, children):
+            again = b in named
+            named.add(b)
+            if not (self._row(a) and self._row(b)) or b in copied or again or before[b] != 0 or not self._len_ok(self.lens[a]):
                 self.faults.append("bounds")
                 continue
             held = self.table[a][:self._pages(self.lens[a])]

@@ -370,3 +370,30 @@ def test_repetition_penalties_over_the_whole_range(eng, rep, rows, vocab):
     assert np.array_equal(got[(np.abs(want) > top) & ~near], np.copysign(np.inf, want[(np.abs(want) > top) & ~near]))
     fine = (np.abs(want) <= top) & ~near
     assert np.all(np.abs(got - want)[fine] <= np.abs(want[fine]) * 2.0 ** -23 + 2.0 ** -149)
+
+
+@pytest.mark.gpu
+def test_as_many_rows_as_there_can_be(eng):
+    g, x, kw = _random(65535, 37, torch.float32, 5, 19)
+    _check(eng, x, mask=g.random((3, 37)) < 0.6, mask_rows=g.integers(-1, 3, 65535).tolist(), **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab,hist", [(5, 1000, 20), (90, 20000, 20), (90, 20000, 13000)])
+def test_rows_behind_the_first_4_gigabytes(eng, rows, vocab, hist):
+    """Places of logits, tokens and mask words that do not fit 32 bits."""
+    g, x, kw = _random(rows, vocab, torch.bfloat16, hist, 23)
+    mask, i32 = g.random((rows, vocab)) < 0.6, dict(dtype=torch.int32, device="cuda")
+
+    def far(t):
+        """The same rows so far apart that the last one lies behind the first 2^32 elements."""
+        step = 2 ** 32 // (rows - 1) + 9
+        wide = torch.empty((rows - 1) * step + t.shape[1], dtype=t.dtype, device="cuda").as_strided(t.shape, (step, 1))
+        return wide.copy_(t)
+
+    total, prompt = (torch.tensor(kw[k], **i32) for k in ("total", "prompt"))
+    rep, pres, freq = (torch.tensor(kw[k], dtype=torch.float32, device="cuda") for k in ("rep", "pres", "freq"))
+    near = dict(tokens=torch.tensor(kw["tokens"], **i32), mask=_bits(mask).cuda())
+    rest = dict(prompt_lens=prompt, total_lens=total, repetition=rep, presence=pres, frequency=freq)
+    want = eng.hook_adjust_logits(x.cuda(), out=torch.empty(rows, vocab, device="cuda"), **near, **rest)
+    assert torch.equal(eng.hook_adjust_logits(far(x.cuda()), out=far(torch.empty_like(want)), **{k: far(t) for k, t in near.items()}, **rest), want)

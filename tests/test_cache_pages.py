@@ -530,3 +530,31 @@ def test_copy_of_long_lists(eng, count):
     for layer in want:
         layer[:, dst] = layer[:, src]
     assert torch.equal(cache.view(torch.int16), want) and int(status.item()) == binding.HOOK_ATTN_ERR_BOUNDS
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("num_blocks", [800, 3000, 16000, 40000])
+def test_as_many_sequences_as_a_pool_can_have(eng, num_blocks):
+    """Lists of 16384 entries, and every size of the kernel that hands pages out beside the largest tables."""
+    n, g = 16384, np.random.default_rng(num_blocks)
+    both = Both(eng, n, 3, num_blocks)
+    both.extend((g.integers(1, 33, n) * (np.arange(n) % 3 == 0)).tolist())
+    both.fork((np.arange(n) // 3 * 3).tolist(), g.permutation(n).tolist())
+    both.extend((g.random(n) < 0.3).astype(int).tolist())
+    both.free(g.permutation(n).tolist(), g.integers(0, 40, n).tolist())
+    both.extend(g.integers(0, 3, n).tolist())
+    both.compact()
+
+
+@pytest.mark.gpu
+def test_pages_behind_the_first_4_gigabytes(eng):
+    """Elements whose places do not fit 32 bits, in both caches of an interleaved pool."""
+    pages = 2 ** 32 // (2 * 16 * 8 * 128) + 5
+    cache = torch.zeros((pages, 2, 16, 8, 128), dtype=torch.bfloat16, device="cuda")
+    cache[1], cache[pages - 1] = torch.randn(cache.shape[1:], device="cuda").bfloat16(), torch.randn(cache.shape[1:], device="cuda").bfloat16()
+    first, last = cache[1].clone(), cache[pages - 1].clone()
+    eng.hook_cache_copy_pages([(cache[:, 0], cache[:, 1])], torch.tensor([[1, pages - 2], [pages - 1, 2]], dtype=torch.int32, device="cuda"))
+    for page, want in ((1, first), (2, last), (pages - 2, first), (pages - 1, last)):
+        assert torch.equal(cache[page], want)
+    cache[1:3], cache[pages - 2:] = 0, 0
+    assert not cache.any()

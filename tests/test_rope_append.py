@@ -374,3 +374,33 @@ def test_as_many_rows_to_a_block_as_there_can_be(eng, axis_pairs, dtype):
 def test_in_place_queries_of_several_rows_to_a_block(eng, adjacent):
     c = _long_case(2503, 32, torch.bfloat16, 9, broken=False, fused=False)
     _check(eng, c, _freq(32), (32,), adjacent=adjacent, in_place=True)
+
+
+@pytest.mark.gpu
+def test_as_many_sequences_as_there_can_be(eng):
+    """65535 of them, most without a row; and a cache whose last pages lie behind the first 2^32 elements."""
+    seqs, rows, pages, i32 = 65535, 3000, 2 ** 32 // (2 * 16 * 8 * 128) + 3000, dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    at = torch.randint(0, seqs, (rows,), generator=g, device="cuda").sort().values
+    n = torch.bincount(at, minlength=seqs)
+    cu = torch.zeros(seqs + 1, **i32)
+    cu[1:] = n.cumsum(0)
+    lens = (n + torch.randint(0, 30, (seqs,), generator=g, device="cuda")).int()
+    table = torch.full((seqs, 3), -1, **i32)
+    live = (torch.arange(3, device="cuda") * 16 < lens[:, None]) & (n > 0)[:, None]
+    table[live] = (pages - 1 - torch.randperm(int(live.sum()), generator=g, device="cuda")).int()
+    q, k, v = (torch.randn(rows, h, 128, generator=g, device="cuda").bfloat16() for h in (8, 8, 8))
+    cache = torch.empty((pages, 2, 16, 8, 128), dtype=torch.bfloat16, device="cuda")
+    status = torch.zeros(1, **i32)
+    freq = torch.tensor(_freq(64), device="cuda")
+    got = eng.hook_rope_append(q=q, k=k, v=v, k_cache=cache[:, 0], v_cache=cache[:, 1], block_table=table, seq_lens=lens, cu_q_lens=cu, inv_freq=freq, status=status)
+    pos = (lens[at] - cu[at + 1] + torch.arange(rows, device="cuda")).long()
+    page = table[at, pos // 16].long()
+    assert int(page.min()) * 2 * 16 * 8 * 128 > 2 ** 31 and int(page.max()) == pages - 1 and int(status.item()) == 0
+    assert torch.equal(cache[page, 1, pos % 16], v)
+    angle = pos[:, None].double() * freq.double()
+    turn = torch.polar(torch.ones_like(angle), angle)[:, None]
+    for res, x in ((got, q), (cache[page, 0, pos % 16], k)):
+        z = torch.complex(x[..., :64].double(), x[..., 64:].double()) * turn
+        want, scale = torch.cat([z.real, z.imag], -1), x[..., :64].double().abs() + x[..., 64:].double().abs()
+        assert ((res.double() - want).abs() <= want.abs() * BF16_HALF_STEP + torch.cat([scale, scale], -1) * ARITHMETIC).all()

@@ -395,7 +395,7 @@ class HookAttn:
 
     def hook_cache_copy_pages(self, caches, pairs, num_pairs=None, status=None, stream=None) -> None:
         """Copies pages ``pairs[i] = (source, destination)`` in the ``caches``, a list of ``(k_cache, v_cache)`` of the layers (one
-        shape, one set of strides).  ``num_pairs``: int32 ``[1]`` on the device, how many of the pairs count."""
+        shape, one set of strides).  ``num_pairs``: int32 ``[1]`` on the device, how many of the pairs count (2^22 at most)."""
         self._short("hook_cache_copy_pages", self._marshal.cache_copy_pages, stream, caches, pairs, num_pairs, status)
 
     # -- convenience ---------------------------------------------------------------------

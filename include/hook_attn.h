@@ -129,7 +129,7 @@ int hook_attn_destroy(hook_attn_handle* handle);
 
 /* Bytes of scratch the call described by `p` needs (only the shape fields and max_seq_len are read;
  * pass the same max_seq_len to the call).
- * is_decode = 1 sizes hook_attn_decode, 2 the decode half of hook_attn_mixed, 0 hook_attn_prefill.
+ * is_decode = 1 sizes hook_attn_decode, 2 the decode half of hook_attn_mixed, 3 hook_attn_decode_q4, 0 hook_attn_prefill.
  * Returns 0 when the call needs no scratch or when the shapes are invalid. */
 size_t hook_attn_workspace_bytes(const hook_attn_params* p, int is_decode);
 
@@ -374,6 +374,98 @@ typedef struct {
  * destination, is not carried out and sets status, like one outside the pool.  They are held against one another, which takes a time that
  * grows with the square of their number (2^18 pairs: 30 ms): of more than 2^22 that count, none is carried out and status is set. */
 int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params* p, void* cuda_stream);
+
+/* ---- a cache held in 4 bits ----------------------------------------------------------------------------------
+ * Where the cache and not the model bounds the number of sequences: keys and values of 16 tokens in 2.1 to 2.5 KB a
+ * head of 128 instead of 8 KB.  Block tables, lengths and the pool calls above are as for a bf16 cache; the pages are
+ * written by hook_rope_append_q4, read by hook_attn_decode_q4, and read back to bf16 pages for whatever else reads a
+ * cache (hook_attn_prefill of a prompt's next chunk, hook_capture_qk) by hook_cache_read_q4.
+ *
+ * A head's elements share a step and a lowest value in groups of `group` neighbours.  Of the group's elements, rounded
+ * to bf16 (what a bf16 cache holds), lowest is the least, step = (greatest - lowest) / 15 rounded to bf16 (0 if that is below
+ * 2^-100), and an element x has the code nearest to (x - lowest) / step, 0 .. 15, x - lowest rounded to 32 bits and halves to
+ * even (0 where the step is 0).  It reads as lowest + step * code.  A group that holds an infinity or a NaN, or whose step
+ * overflows, reads as NaN.
+ *
+ * A page's part for one KV head is a slab of hook_q4_slab_bytes(head_dim, group) bytes: 16 head_dim / 2 bytes of K codes, as
+ * many of V codes, then for K and for V the pairs (step, lowest) of bf16 [16][head_dim / group].  The codes of token t, element e:
+ *   K  nibble e % 8 (of a little-endian 32-bit word) of word (e / 8 % 4) * (head_dim / 32) + e / 32 of row t;
+ *   V  nibble e % 32 / 8 of the 16-bit word e / 32 of unit u of row (t / 2 % 4) + 4 (t % 2) + 8 (t / 8), a unit having head_dim / 16 bytes and
+ *      u being e % 8, with head_dim 128 and a row whose bit 1 is set e % 8 xor 4. */
+typedef struct {
+    void*   pages;               /* slab of block b, KV head h at b * block_stride + h * head_stride; 16-byte aligned */
+    int64_t block_stride, head_stride;  /* in BYTES, multiples of 16 */
+    int32_t group;               /* elements to a group: 32, 64 or 128, at most head_dim */
+} hook_q4_cache;
+
+/* Bytes of a slab; 0 for a head_dim or group that is not supported. */
+size_t hook_q4_slab_bytes(int32_t head_dim, int32_t group);
+
+/* hook_rope_append into a 4-bit cache: the same queries, keys rotated and rounded to bf16 in the same way, then keys and values
+ * quantised as they are written.  k_cache, v_cache and the kv strides of `p` are ignored; q_out must not overlap the pages. */
+int hook_rope_append_q4(hook_attn_handle* handle, const hook_rope_params* p, const hook_q4_cache* cache, void* cuda_stream);
+
+/* hook_attn_decode over a 4-bit cache: the same arguments, outputs, hooks and faults, k_cache, v_cache and the kv strides of `p` being
+ * ignored.  `workspace` holds hook_attn_workspace_bytes(p, 3) bytes.  Scores, softmax, span masses and the sums over the values
+ * are in 32 bits; a probability times a step is rounded to 11 bits. */
+int hook_attn_decode_q4(hook_attn_handle* handle, const hook_attn_params* p, const hook_q4_cache* cache, void* cuda_stream);
+
+typedef struct {
+    int32_t num_seqs, num_kv_heads, head_dim, page_size;
+    int32_t num_blocks, max_blocks_per_seq;         /* of the 4-bit cache and its block_table */
+    int32_t to_num_blocks, to_max_blocks_per_seq;   /* of the bf16 cache and to_table */
+    const int32_t* block_table;  /* [num_seqs][max_blocks_per_seq] */
+    const int32_t* seq_lens;     /* [num_seqs]; 0: nothing is read */
+    const int32_t* first;        /* [num_seqs] first position that is read; NULL: 0 */
+    void*          k_cache;      /* bf16, written: as in hook_attn_params */
+    void*          v_cache;
+    int64_t        kv_block_stride, kv_token_stride, kv_head_stride;
+    const int32_t* to_table;     /* [num_seqs][to_max_blocks_per_seq] pages of the bf16 cache */
+    int32_t*       status;
+} hook_q4_read_params;
+
+/* Positions first[s] .. seq_lens[s] - 1 of every sequence, each lowest + step * code computed in 32 bits and rounded to bf16, go to the
+ * same positions of to_table's pages; nothing else is written.  The pages that are written belong to one sequence
+ * alone.  A sequence whose length is negative or beyond one of the tables, or whose first is negative, is passed over and sets status, like
+ * a page outside its pool. */
+int hook_cache_read_q4(hook_attn_handle* handle, const hook_q4_read_params* p, const hook_q4_cache* cache, void* cuda_stream);
+
+typedef struct {
+    int32_t num_layers, num_blocks, page_size, num_kv_heads, head_dim, group, max_pairs;
+    int64_t block_stride, head_stride;   /* of every layer's pages, in bytes */
+    void* const*   pages;        /* HOST array [num_layers] of device pointers */
+    const int32_t* pairs;        /* as in hook_cache_copy_params */
+    const int32_t* num_pairs;
+    int32_t*       status;
+} hook_q4_copy_params;
+
+/* hook_cache_copy_pages for 4-bit caches. */
+int hook_cache_copy_pages_q4(hook_attn_handle* handle, const hook_q4_copy_params* p, void* cuda_stream);
+
+/* ---- the choice of a token ------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t num_rows, vocab_size;
+    int32_t dtype;               /* HOOK_DTYPE_* of logits */
+    const void*    logits;       /* [num_rows][vocab_size], rows logits_row_stride elements apart */
+    int64_t        logits_row_stride;
+    const float*   uniform;      /* [num_rows] random numbers in [0, 1) */
+    const float*   temperature;  /* [num_rows] T >= 0; 0: the token with the largest logit; NULL: 1 */
+    const int32_t* top_k;        /* [num_rows]; 0 or less, or vocab_size and more: all; NULL: all */
+    const float*   top_p;        /* [num_rows] >= 0; 1 and more: all; NULL: all */
+    const float*   min_p;        /* [num_rows] 0 .. 1; NULL: 0 */
+    int32_t*       tokens;       /* [num_rows] */
+    int32_t*       status;
+} hook_sample_params;
+
+/* One token for every row, from its logits (of hook_adjust_logits, say) and one random number.  Token v weighs w_v = exp((x_v - max x) / T).  In the
+ * order of falling logits, equal ones in that of their indices, the first top_k tokens stay, of these those with
+ * w_v >= min_p, and of these each before which less than top_p of their weight lies; the first one always stays.  The token is the first, in the
+ * order of the indices, up to and with which the weights of those that stayed exceed `uniform` times their sum.
+ * The weights are computed in 64 bits and summed as whole multiples of 2^-42: the order of the sums has no say in the result, and a
+ * token below 2^-43 of the most likely one is never drawn.  A NaN counts as -infinity; infinite logits weigh the same.
+ * A row without a logit above -infinity, or with a parameter outside the ranges above (NaN among them), gets -1 and sets status to
+ * HOOK_ATTN_ERR_INVALID_ARG.  vocab_size <= 2^20, num_rows < 2^16. */
+int hook_sample_tokens(hook_attn_handle* handle, const hook_sample_params* p, void* cuda_stream);
 
 /* Human-readable name of a return / status code. */
 const char* hook_attn_strerror(int code);

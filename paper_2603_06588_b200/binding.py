@@ -31,7 +31,8 @@ EXPORTS = ("hook_attn_create", "hook_attn_destroy", "hook_attn_workspace_bytes",
            "hook_attn_prefill", "hook_attn_decode", "hook_attn_mixed", "hook_attn_decode_static_scratch",
            "hook_attn_score", "hook_steer_residual", "hook_capture_qk", "hook_rope_append", "hook_adjust_logits",
            "hook_cache_fork", "hook_cache_extend", "hook_cache_free", "hook_cache_compact", "hook_cache_copy_pages",
-           "hook_attn_selftest_wait_limit", "hook_attn_strerror")
+           "hook_q4_slab_bytes", "hook_rope_append_q4", "hook_attn_decode_q4", "hook_cache_read_q4", "hook_cache_copy_pages_q4",
+           "hook_sample_tokens", "hook_attn_selftest_wait_limit", "hook_attn_strerror")
 HOOK_SCORE_MEAN = 0
 HOOK_SCORE_SUM_NORMALIZE = 1
 STATIC_SCRATCH_BYTES = 16 << 20   # HOOK_ATTN_STATIC_SCRATCH_BYTES
@@ -41,7 +42,8 @@ HOOK_ROPE_PAIR_HALVES, HOOK_ROPE_PAIR_ADJACENT = 0, 1
 HOOK_ROPE_MAX_AXES = 4
 # Arguments between the handle and the stream: p an address, i an int32.
 _AROUND = {"hook_rope_append": "p", "hook_adjust_logits": "p", "hook_cache_fork": "pppi", "hook_cache_extend": "ppp",
-           "hook_cache_free": "pppi", "hook_cache_compact": "pppppp", "hook_cache_copy_pages": "p"}
+           "hook_cache_free": "pppi", "hook_cache_compact": "pppppp", "hook_cache_copy_pages": "p", "hook_rope_append_q4": "pp",
+           "hook_attn_decode_q4": "pp", "hook_cache_read_q4": "pp", "hook_cache_copy_pages_q4": "p", "hook_sample_tokens": "p"}
 
 
 class HookAttnParams(ctypes.Structure):
@@ -107,6 +109,30 @@ class HookCacheCopyParams(ctypes.Structure):
                 + _fields("k_caches v_caches pairs num_pairs status", ctypes.c_void_p))
 
 
+class HookQ4Cache(ctypes.Structure):
+    """Mirror of ``hook_q4_cache``."""
+    _fields_ = [("pages", ctypes.c_void_p)] + _fields("block_stride head_stride", ctypes.c_int64) + [("group", ctypes.c_int32)]
+
+
+class HookQ4ReadParams(ctypes.Structure):
+    """Mirror of ``hook_q4_read_params``."""
+    _fields_ = (_fields("num_seqs num_kv_heads head_dim page_size num_blocks max_blocks_per_seq to_num_blocks to_max_blocks_per_seq", ctypes.c_int32)
+                + _fields("block_table seq_lens first k_cache v_cache", ctypes.c_void_p)
+                + _fields("kv_block_stride kv_token_stride kv_head_stride", ctypes.c_int64) + _fields("to_table status", ctypes.c_void_p))
+
+
+class HookQ4CopyParams(ctypes.Structure):
+    """Mirror of ``hook_q4_copy_params``."""
+    _fields_ = (_fields("num_layers num_blocks page_size num_kv_heads head_dim group max_pairs", ctypes.c_int32)
+                + _fields("block_stride head_stride", ctypes.c_int64) + _fields("pages pairs num_pairs status", ctypes.c_void_p))
+
+
+class HookSampleParams(ctypes.Structure):
+    """Mirror of ``hook_sample_params``."""
+    _fields_ = (_fields("num_rows vocab_size dtype", ctypes.c_int32) + [("logits", ctypes.c_void_p), ("logits_row_stride", ctypes.c_int64)]
+                + _fields("uniform temperature top_k top_p min_p tokens status", ctypes.c_void_p))
+
+
 class HookAttnError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -164,6 +190,8 @@ def load_library() -> ctypes.CDLL:
             fn = getattr(lib, name)
             fn.restype = ctypes.c_int
             fn.argtypes = [void_p] + [i32 if a == "i" else void_p for a in args] + [void_p]
+        lib.hook_q4_slab_bytes.restype = ctypes.c_size_t
+        lib.hook_q4_slab_bytes.argtypes = [i32, i32]
         lib.hook_attn_selftest_wait_limit.restype = ctypes.c_int
         lib.hook_attn_selftest_wait_limit.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p,
                                                       ctypes.c_void_p]
@@ -179,6 +207,15 @@ def load_library() -> ctypes.CDLL:
 
 def strerror(code: int) -> str:
     return load_library().hook_attn_strerror(int(code)).decode()
+
+
+def q4_slab_bytes(head_dim: int, group: int) -> int:
+    """Bytes that a page of a 4-bit cache takes for one KV head: the last dimension of its uint8 ``pages [num_blocks, Hkv, bytes]``, from which
+    the calls tell the group.  A fresh cache may hold anything."""
+    nbytes = int(load_library().hook_q4_slab_bytes(int(head_dim), int(group)))
+    if nbytes == 0:
+        raise HookAttnError(HOOK_ATTN_ERR_UNSUPPORTED, "hook_q4_slab_bytes")
+    return nbytes
 
 
 def _dptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -245,6 +282,7 @@ class HookAttn:
         self._index = int(device)
         self._marshal = _compiled
         self._calls = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _AROUND}
+        self._workspace_bytes = ctypes.cast(lib.hook_attn_workspace_bytes, ctypes.c_void_p).value
         self.device = torch.device("cuda", int(device))
 
     def close(self):
@@ -260,7 +298,7 @@ class HookAttn:
 
     # -- raw calls -----------------------------------------------------------------------
     def workspace_bytes(self, params: HookAttnParams, is_decode) -> int:
-        """``is_decode``: False / True, or 2 for the decode half of a mixed step."""
+        """``is_decode``: False / True, 2 for the decode half of a mixed step, or 3 for the decode over a 4-bit cache."""
         return int(self._lib.hook_attn_workspace_bytes(ctypes.byref(params), int(is_decode)))
 
     def call(self, params: HookAttnParams, is_decode: bool, stream: Optional[int] = None) -> int:
@@ -397,6 +435,40 @@ class HookAttn:
         """Copies pages ``pairs[i] = (source, destination)`` in the ``caches``, a list of ``(k_cache, v_cache)`` of the layers (one
         shape, one set of strides).  ``num_pairs``: int32 ``[1]`` on the device, how many of the pairs count (2^22 at most)."""
         self._short("hook_cache_copy_pages", self._marshal.cache_copy_pages, stream, caches, pairs, num_pairs, status)
+
+    # -- a cache held in 4 bits --------------------------------------------------------------
+    def hook_rope_append_q4(self, *, q, k, v, pages, block_table, seq_lens, inv_freq, cu_q_lens=None, positions=None, axis_pairs=None,
+                            axis_order: int = HOOK_ROPE_AXES_BLOCKED, pairing: int = HOOK_ROPE_PAIR_HALVES, factor: float = 1.0, q_out=None,
+                            status=None, stream=None) -> torch.Tensor:
+        """:meth:`hook_rope_append` into a 4-bit cache, ``pages`` uint8 ``[num_blocks, Hkv, q4_slab_bytes(D, group)]``: keys and values are
+        quantised as they are written.  Returns the rotated queries."""
+        return self._short("hook_rope_append_q4", self._marshal.rope_append_q4, stream, q, k, v, pages, block_table, seq_lens, inv_freq,
+                           cu_q_lens, positions, axis_pairs, axis_order, pairing, factor, q_out, status)
+
+    def hook_attn_decode_q4(self, *, q, pages, block_table, seq_lens, spans=None, head_mask=None, alpha=None, steer_vec=None, scale: float = 0.0,
+                            out=None, span_mass=None, workspace=None, status=None, max_seq_len: int = 0, stream=None):
+        """:meth:`hook_attn_decode` over a 4-bit cache: ``q`` bf16 ``[seqs, Hq, D]``, ``head_mask`` and ``alpha`` on the host.  Returns
+        ``(out, span_mass)``; ``span_mass`` is None without probes.  ``workspace``: uint8 of
+        ``workspace_bytes(params, 3)``, 256-byte aligned; allocated if not given."""
+        return self._short("hook_attn_decode_q4", self._marshal.attn_decode_q4, stream, q, pages, block_table, seq_lens, spans, head_mask, alpha,
+                           steer_vec, scale, out, span_mass, workspace, status, max_seq_len, self._workspace_bytes)
+
+    def hook_cache_read_q4(self, pages, block_table, seq_lens, *, k_cache, v_cache, to_table, first=None, status=None, stream=None) -> None:
+        """Reads positions ``first[s]`` (default 0) to ``seq_lens[s]`` of every sequence back to the pages ``to_table`` of a bf16 cache, where
+        :meth:`hook_attn_prefill` and :meth:`hook_capture_qk` find them."""
+        self._short("hook_cache_read_q4", self._marshal.cache_read_q4, stream, pages, block_table, seq_lens, k_cache, v_cache, to_table, first, status)
+
+    def hook_cache_copy_pages_q4(self, caches, pairs, num_pairs=None, status=None, stream=None) -> None:
+        """:meth:`hook_cache_copy_pages` for 4-bit caches, a list of the layers' ``pages``."""
+        self._short("hook_cache_copy_pages_q4", self._marshal.cache_copy_pages_q4, stream, caches, pairs, num_pairs, status)
+
+    # -- the choice of a token ---------------------------------------------------------------
+    def hook_sample_tokens(self, logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, status=None,
+                           stream=None) -> torch.Tensor:
+        """A token for each row of ``logits [rows, vocab]`` (bf16, fp16 or fp32; rows may be strided) from one random number in [0, 1) each:
+        ``uniform``, ``temperature``, ``top_p``, ``min_p`` fp32 and ``top_k`` int32, all ``[rows]``.  Temperature 0 takes the largest logit.
+        Returns int32 ``[rows]``; -1 for a row that has nothing to choose from or a parameter out of range."""
+        return self._short("hook_sample_tokens", self._marshal.sample_tokens, stream, logits, uniform, temperature, top_k, top_p, min_p, tokens, status)
 
     # -- convenience ---------------------------------------------------------------------
     def plan(self, is_decode: bool, *, q, k_cache, v_cache, block_table, seq_lens, cu_q_lens=None,

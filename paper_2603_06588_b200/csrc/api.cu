@@ -7,6 +7,7 @@
 
 #include "common.cuh"
 #include "ops.cuh"
+#include "q4.cuh"
 
 namespace hook_attn {
 // decode.cu
@@ -49,6 +50,14 @@ cudaError_t launch_extend(const PoolArgs& p, const int32_t* new_rows, int32_t* p
 cudaError_t launch_compact(const PoolArgs& p, int32_t* table_out, int32_t* refs_out, int32_t* page_map, int32_t* pairs,
                            int32_t* num_pairs, cudaStream_t st);
 cudaError_t launch_copy_pages(const CopyArgs& a, int num_sms, cudaStream_t st);
+// decode_q4.cu, cache_q4.cu, sample.cu
+cudaError_t configure_decode_q4();
+size_t decode_q4_workspace_bytes(int num_seqs, int Hkv, int G, int head_dim, int max_keys);
+cudaError_t launch_decode_q4(const KernelArgs& a, const HeadCfg& hc, int head_dim, int group, int num_sms, cudaStream_t st);
+cudaError_t launch_rope_append_q4(RopeArgs& a, int dtype, int group, int num_sms, cudaStream_t st);
+cudaError_t launch_q4_read(const Q4ReadArgs& a, int head_dim, int group, int num_sms, cudaStream_t st);
+cudaError_t configure_sample();
+cudaError_t launch_sample(const SampleArgs& a, int dtype, int num_sms, cudaStream_t st);
 }  // namespace hook_attn
 
 using namespace hook_attn;
@@ -106,6 +115,14 @@ int check_handle(const hook_attn_handle* handle)
 bool dtype_ok(int dtype) { return dtype == HOOK_DTYPE_BF16 || dtype == HOOK_DTYPE_F16 || dtype == HOOK_DTYPE_F32; }
 
 int64_t min64(int64_t x, int64_t y) { return x < y ? x : y; }
+
+// The pages of a 4-bit cache.
+int check_q4(const hook_q4_cache* c, int head_dim)
+{
+    if (!c || !c->pages || c->block_stride <= 0 || c->head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (hook_q4_slab_bytes(head_dim, c->group) == 0 || ((c->block_stride | c->head_stride) & 15) || !aligned16(c->pages)) return HOOK_ATTN_ERR_UNSUPPORTED;
+    return HOOK_ATTN_OK;
+}
 
 int prepare_pool(const hook_cache_pool* p, PoolArgs& a)
 {
@@ -196,6 +213,8 @@ int hook_attn_create(hook_attn_handle** handle, int device)
     if (e == cudaSuccess) e = configure_mixed();
     if (e == cudaSuccess) e = configure_logits();
     if (e == cudaSuccess) e = configure_cache_pages();
+    if (e == cudaSuccess) e = configure_decode_q4();
+    if (e == cudaSuccess) e = configure_sample();
     cudaSetDevice(prev);
     if (e != cudaSuccess) return HOOK_ATTN_ERR_CUDA;
     hook_attn_handle* h = new hook_attn_handle;
@@ -224,6 +243,7 @@ size_t hook_attn_workspace_bytes(const hook_attn_params* p, int is_decode)
     if (validate_common(p, is_decode != 0) != HOOK_ATTN_OK) return 0;
     if (!is_decode) return 0;
     const int G = p->num_q_heads / p->num_kv_heads;
+    if (is_decode == 3) return decode_q4_workspace_bytes(p->num_seqs, p->num_kv_heads, G, p->head_dim, max_keys_of(p));
     const size_t alone = decode_workspace_bytes(p->num_seqs, p->num_kv_heads, G, p->head_dim, max_keys_of(p));
     if (is_decode != 2) return alone;
     // the decode half of hook_attn_mixed: the one-launch path cuts by page shares whatever the unit count,
@@ -405,7 +425,8 @@ int hook_capture_qk(hook_attn_handle* handle, const hook_attn_params* p, int is_
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
 }
 
-int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* cuda_stream)
+// What both rotary appends check and fill; `q4` replaces the bf16 cache.
+static int prepare_rope(const hook_attn_handle* handle, const hook_rope_params* p, const hook_q4_cache* q4, RopeArgs& a)
 {
     if (!p || p->num_seqs < 0 || p->total_q < 0 || p->num_q_heads <= 0 || p->num_kv_heads <= 0 || p->head_dim <= 0 ||
         p->page_size <= 0 || p->num_blocks < 0 || p->max_blocks_per_seq < 0)
@@ -427,12 +448,17 @@ int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* 
     if (p->head_dim != 64 && p->head_dim != 128) return HOOK_ATTN_ERR_UNSUPPORTED;
     if (p->page_size != kPage || p->num_q_heads > kMaxHeads || p->num_seqs > 65535) return HOOK_ATTN_ERR_UNSUPPORTED;
     if (p->num_seqs > 0 && p->total_q > 0) {
-        if (!p->q || !p->k || !p->v || !p->q_out || !p->k_cache || !p->v_cache || !p->block_table || !p->seq_lens)
+        if (!p->q || !p->k || !p->v || !p->q_out || (!q4 && (!p->k_cache || !p->v_cache)) || !p->block_table || !p->seq_lens)
             return HOOK_ATTN_ERR_INVALID_ARG;
         if (pairs > 0 && !p->inv_freq) return HOOK_ATTN_ERR_INVALID_ARG;
-        if (p->kv_block_stride <= 0 || p->kv_token_stride <= 0 || p->kv_head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
-        if ((p->kv_block_stride | p->kv_token_stride | p->kv_head_stride) & 7) return HOOK_ATTN_ERR_UNSUPPORTED;
-        if (!aligned16(p->q_out) || !aligned16(p->k_cache) || !aligned16(p->v_cache)) return HOOK_ATTN_ERR_UNSUPPORTED;
+        if (!q4) {
+            if (p->kv_block_stride <= 0 || p->kv_token_stride <= 0 || p->kv_head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
+            if ((p->kv_block_stride | p->kv_token_stride | p->kv_head_stride) & 7) return HOOK_ATTN_ERR_UNSUPPORTED;
+            if (!aligned16(p->k_cache) || !aligned16(p->v_cache)) return HOOK_ATTN_ERR_UNSUPPORTED;
+        } else if (const int bad = check_q4(q4, p->head_dim)) {
+            return bad;
+        }
+        if (!aligned16(p->q_out)) return HOOK_ATTN_ERR_UNSUPPORTED;
         const uintptr_t size = p->dtype == HOOK_DTYPE_F32 ? 4 : 2;
         if ((reinterpret_cast<uintptr_t>(p->q) | reinterpret_cast<uintptr_t>(p->k) | reinterpret_cast<uintptr_t>(p->v)) & (size - 1))
             return HOOK_ATTN_ERR_UNSUPPORTED;
@@ -444,16 +470,20 @@ int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* 
     int rc = check_handle(handle);
     if (rc != HOOK_ATTN_OK || p->num_seqs == 0 || p->total_q == 0) return rc;
 
-    RopeArgs a;
     memset(&a, 0, sizeof a);
     a.q = p->q; a.k = p->k; a.v = p->v;
     a.q_row = p->q_row_stride; a.q_head = p->q_head_stride;
     a.k_row = p->k_row_stride; a.k_head = p->k_head_stride;
     a.v_row = p->v_row_stride; a.v_head = p->v_head_stride;
     a.q_out = static_cast<__nv_bfloat16*>(p->q_out);
-    a.k_cache = static_cast<__nv_bfloat16*>(p->k_cache);
-    a.v_cache = static_cast<__nv_bfloat16*>(p->v_cache);
-    a.bs = p->kv_block_stride; a.ts = p->kv_token_stride; a.hs = p->kv_head_stride;
+    if (q4) {
+        a.k_cache = static_cast<__nv_bfloat16*>(q4->pages);
+        a.bs = q4->block_stride; a.hs = q4->head_stride;
+    } else {
+        a.k_cache = static_cast<__nv_bfloat16*>(p->k_cache);
+        a.v_cache = static_cast<__nv_bfloat16*>(p->v_cache);
+        a.bs = p->kv_block_stride; a.ts = p->kv_token_stride; a.hs = p->kv_head_stride;
+    }
     a.block_table = p->block_table; a.seq_lens = p->seq_lens; a.cu_q_lens = p->cu_q_lens;
     a.positions = p->positions; a.axis_stride = p->position_axis_stride;
     a.inv_freq = p->inv_freq;
@@ -469,6 +499,14 @@ int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* 
         --left[axis];
         if (p->axis_order == HOOK_ROPE_AXES_CYCLIC) axis = (axis + 1) % p->num_axes;
     }
+    return HOOK_ATTN_OK;
+}
+
+int hook_rope_append(hook_attn_handle* handle, const hook_rope_params* p, void* cuda_stream)
+{
+    RopeArgs a;
+    int rc = prepare_rope(handle, p, nullptr, a);
+    if (rc != HOOK_ATTN_OK || p->num_seqs == 0 || p->total_q == 0) return rc;
     cudaError_t e = launch_rope_append(a, p->dtype, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
 }
@@ -585,15 +623,141 @@ int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params
     a.pairs = p->pairs; a.num_pairs = p->num_pairs;
     a.status = p->status;
     a.num_blocks = p->num_blocks; a.Hkv = p->num_kv_heads; a.head_dim = p->head_dim; a.max_pairs = p->max_pairs;
+    a.tokens = kPage;
     for (int l0 = 0; l0 < p->num_layers; l0 += kCopyLayers) {
-        a.layers = p->num_layers - l0 < kCopyLayers ? p->num_layers - l0 : kCopyLayers;
-        for (int l = 0; l < a.layers; ++l) {
+        const int layers = p->num_layers - l0 < kCopyLayers ? p->num_layers - l0 : kCopyLayers;
+        a.slabs = 2 * layers;
+        for (int l = 0; l < layers; ++l) {
             a.k[l] = static_cast<__nv_bfloat16*>(p->k_caches[l0 + l]);
             a.v[l] = static_cast<__nv_bfloat16*>(p->v_caches[l0 + l]);
         }
         if (launch_copy_pages(a, handle->num_sms, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return HOOK_ATTN_ERR_CUDA;
     }
     return HOOK_ATTN_OK;
+}
+
+size_t hook_q4_slab_bytes(int32_t head_dim, int32_t group)
+{
+    if ((head_dim != 64 && head_dim != 128) || (group != 32 && group != 64 && group != 128) || group > head_dim) return 0;
+    return (size_t)q4_slab_bytes(head_dim, head_dim / group);
+}
+
+int hook_rope_append_q4(hook_attn_handle* handle, const hook_rope_params* p, const hook_q4_cache* cache, void* cuda_stream)
+{
+    RopeArgs a;
+    if (!cache) return HOOK_ATTN_ERR_INVALID_ARG;
+    int rc = prepare_rope(handle, p, cache, a);
+    if (rc != HOOK_ATTN_OK || p->num_seqs == 0 || p->total_q == 0) return rc;
+    cudaError_t e = launch_rope_append_q4(a, p->dtype, cache->group, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_attn_decode_q4(hook_attn_handle* handle, const hook_attn_params* p, const hook_q4_cache* cache, void* cuda_stream)
+{
+    if (!p || !cache) return HOOK_ATTN_ERR_INVALID_ARG;
+    int rc = validate_common(p, true);
+    if (rc != HOOK_ATTN_OK) return rc;
+    if (p->num_seqs > 0 && (rc = check_q4(cache, p->head_dim)) != HOOK_ATTN_OK) return rc;
+    hook_attn_params q = *p;               // the pages in the place of the bf16 cache, strides in bytes
+    q.k_cache = q.v_cache = cache->pages;
+    q.kv_block_stride = cache->block_stride; q.kv_token_stride = 16; q.kv_head_stride = cache->head_stride;
+    KernelArgs a;
+    HeadCfg hc;
+    if ((rc = prepare(&q, true, a, hc)) != HOOK_ATTN_OK) return rc;
+    if (p->num_seqs > 0 && p->max_blocks_per_seq == 0) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->num_seqs > 0) {
+        const size_t need = decode_q4_workspace_bytes(p->num_seqs, p->num_kv_heads, a.G, p->head_dim, a.max_keys);
+        if (!p->workspace || p->workspace_bytes < need || (reinterpret_cast<uintptr_t>(p->workspace) & 255u)) return HOOK_ATTN_ERR_WORKSPACE;
+    }
+    if ((rc = check_handle(handle)) != HOOK_ATTN_OK || p->num_seqs == 0) return rc;
+    cudaError_t e = launch_decode_q4(a, hc, p->head_dim, cache->group, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_cache_read_q4(hook_attn_handle* handle, const hook_q4_read_params* p, const hook_q4_cache* cache, void* cuda_stream)
+{
+    if (!p || !cache || p->num_seqs < 0 || p->num_kv_heads <= 0 || p->head_dim <= 0 || p->page_size <= 0 || p->num_blocks < 0 ||
+        p->max_blocks_per_seq < 0 || p->to_num_blocks < 0 || p->to_max_blocks_per_seq < 0)
+        return HOOK_ATTN_ERR_INVALID_ARG;
+    if ((p->head_dim != 64 && p->head_dim != 128) || p->page_size != kPage || p->num_kv_heads > kMaxHeads || p->num_seqs > 65535)
+        return HOOK_ATTN_ERR_UNSUPPORTED;
+    int rc;
+    if (p->num_seqs > 0) {
+        if ((rc = check_q4(cache, p->head_dim)) != HOOK_ATTN_OK) return rc;
+        if (!p->seq_lens || !p->k_cache || !p->v_cache || (p->max_blocks_per_seq > 0 && !p->block_table) || (p->to_max_blocks_per_seq > 0 && !p->to_table))
+            return HOOK_ATTN_ERR_INVALID_ARG;
+        if (p->kv_block_stride <= 0 || p->kv_token_stride <= 0 || p->kv_head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
+        if ((p->kv_block_stride | p->kv_token_stride | p->kv_head_stride) & 7) return HOOK_ATTN_ERR_UNSUPPORTED;
+        if (!aligned16(p->k_cache) || !aligned16(p->v_cache)) return HOOK_ATTN_ERR_UNSUPPORTED;
+    }
+    if ((rc = check_handle(handle)) != HOOK_ATTN_OK || p->num_seqs == 0) return rc;
+    Q4ReadArgs a;
+    memset(&a, 0, sizeof a);
+    a.pages = static_cast<const uint8_t*>(cache->pages);
+    a.page_block = cache->block_stride; a.page_head = cache->head_stride;
+    a.k_cache = static_cast<__nv_bfloat16*>(p->k_cache); a.v_cache = static_cast<__nv_bfloat16*>(p->v_cache);
+    a.bs = p->kv_block_stride; a.ts = p->kv_token_stride; a.hs = p->kv_head_stride;
+    a.block_table = p->block_table; a.seq_lens = p->seq_lens; a.first = p->first; a.to_table = p->to_table;
+    a.status = p->status;
+    a.num_seqs = p->num_seqs; a.Hkv = p->num_kv_heads;
+    a.num_blocks = p->num_blocks; a.max_blocks = p->max_blocks_per_seq;
+    a.to_num_blocks = p->to_num_blocks; a.to_max_blocks = p->to_max_blocks_per_seq;
+    const int64_t shorter = min64(p->max_blocks_per_seq, p->to_max_blocks_per_seq);
+    a.max_keys = (int32_t)min64(shorter * kPage, INT32_MAX);
+    cudaError_t e = launch_q4_read(a, p->head_dim, cache->group, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
+}
+
+int hook_cache_copy_pages_q4(hook_attn_handle* handle, const hook_q4_copy_params* p, void* cuda_stream)
+{
+    if (!p || p->num_layers < 0 || p->num_blocks < 0 || p->page_size <= 0 || p->num_kv_heads <= 0 || p->head_dim <= 0 || p->max_pairs < 0)
+        return HOOK_ATTN_ERR_INVALID_ARG;
+    const size_t slab = hook_q4_slab_bytes(p->head_dim, p->group);
+    if (slab == 0 || p->page_size != kPage || p->num_kv_heads > kMaxHeads || p->max_pairs > 1 << 30) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->num_layers > 0 && p->max_pairs > 0) {
+        if (!p->pages || !p->pairs || p->block_stride <= 0 || p->head_stride <= 0) return HOOK_ATTN_ERR_INVALID_ARG;
+        if ((p->block_stride | p->head_stride) & 15) return HOOK_ATTN_ERR_UNSUPPORTED;
+        for (int l = 0; l < p->num_layers; ++l) {
+            if (!p->pages[l]) return HOOK_ATTN_ERR_INVALID_ARG;
+            if (!aligned16(p->pages[l])) return HOOK_ATTN_ERR_UNSUPPORTED;
+        }
+    }
+    int rc = check_handle(handle);
+    if (rc != HOOK_ATTN_OK) return rc;
+    if (p->num_layers == 0 || p->max_pairs == 0) return HOOK_ATTN_OK;
+    CopyArgs a;                            // a page is one row of a slab for every head, in units of two bytes
+    memset(&a, 0, sizeof a);
+    a.head_dim = (int32_t)(slab / 2); a.tokens = 1; a.Hkv = p->num_kv_heads;
+    a.bs = p->block_stride / 2; a.hs = p->head_stride / 2; a.ts = (int64_t)a.Hkv * a.head_dim;
+    a.pairs = p->pairs; a.num_pairs = p->num_pairs;
+    a.status = p->status;
+    a.num_blocks = p->num_blocks; a.max_pairs = p->max_pairs;
+    for (int l0 = 0; l0 < p->num_layers; l0 += 2 * kCopyLayers) {
+        a.slabs = p->num_layers - l0 < 2 * kCopyLayers ? p->num_layers - l0 : 2 * kCopyLayers;
+        for (int l = 0; l < a.slabs; ++l) (l & 1 ? a.v : a.k)[l / 2] = static_cast<__nv_bfloat16*>(p->pages[l0 + l]);
+        if (launch_copy_pages(a, handle->num_sms, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return HOOK_ATTN_ERR_CUDA;
+    }
+    return HOOK_ATTN_OK;
+}
+
+int hook_sample_tokens(hook_attn_handle* handle, const hook_sample_params* p, void* cuda_stream)
+{
+    if (!p || p->num_rows < 0 || p->vocab_size <= 0 || !dtype_ok(p->dtype)) return HOOK_ATTN_ERR_INVALID_ARG;
+    if (p->vocab_size > kMaxVocab || p->num_rows > 65535) return HOOK_ATTN_ERR_UNSUPPORTED;
+    if (p->num_rows > 0) {
+        if (!p->logits || !p->uniform || !p->tokens || p->logits_row_stride < 0) return HOOK_ATTN_ERR_INVALID_ARG;
+        if (reinterpret_cast<uintptr_t>(p->logits) & (p->dtype == HOOK_DTYPE_F32 ? 3 : 1)) return HOOK_ATTN_ERR_UNSUPPORTED;
+    }
+    int rc = check_handle(handle);
+    if (rc != HOOK_ATTN_OK || p->num_rows == 0) return rc;
+    SampleArgs a;
+    memset(&a, 0, sizeof a);
+    a.logits = p->logits; a.row = p->logits_row_stride;
+    a.uniform = p->uniform; a.temperature = p->temperature; a.top_k = p->top_k; a.top_p = p->top_p; a.min_p = p->min_p;
+    a.tokens = p->tokens; a.status = p->status;
+    a.rows = p->num_rows; a.vocab = p->vocab_size;
+    cudaError_t e = launch_sample(a, p->dtype, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
 }
 
 int hook_attn_selftest_wait_limit(hook_attn_handle* handle, int32_t* status, uint64_t limit_ns, uint64_t* waited_ns,

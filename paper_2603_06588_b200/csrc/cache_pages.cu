@@ -394,7 +394,7 @@ template <bool TIGHT, int CHECKED>
 __global__ void __launch_bounds__(kListThreads, CHECKED == 1 ? 6 : 4) copy_pages_kernel(const __grid_constant__ CopyArgs a)
 {
     __shared__ uint32_t refused;
-    const int n = a.num_pairs ? min(max(*a.num_pairs, 0), a.max_pairs) : a.max_pairs, slabs = 2 * a.layers;
+    const int n = a.num_pairs ? min(max(*a.num_pairs, 0), a.max_pairs) : a.max_pairs, slabs = a.slabs;
     if (n == 0) return;
     if (CHECKED > 1 && n > kMostPairs) {
         if (blockIdx.x == 0 && threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kListThreads, CHECKED == 1 ? 6 : 4) copy_pages
     const uint32_t pairs = many ? CHECKED : 1, some = !many ? 1 : n > kLong ? slabs : min(slabs, 4);              // of a unit
     const uint32_t groups = ((uint32_t)n + pairs - 1) / pairs, rows = (slabs + some - 1) / some;
     const uint32_t next_group = gridDim.x % groups, next_row = gridDim.x / groups;
-    const int per_row = a.head_dim / 8, pieces = kPage * a.Hkv * per_row;
+    const int per_row = a.head_dim / 8, pieces = a.tokens * a.Hkv * per_row;
     auto place = [&](int e) {
         if (TIGHT) return (int64_t)e * 8;
         const int c = e % per_row, h = e / per_row % a.Hkv, t = e / per_row / a.Hkv;
@@ -558,9 +558,9 @@ cudaError_t launch_compact(const PoolArgs& p, int32_t* table_out, int32_t* refs_
 
 cudaError_t launch_copy_pages(const CopyArgs& a, int num_sms, cudaStream_t st)
 {
-    const int64_t units = (int64_t)a.max_pairs * 2 * a.layers, most = (int64_t)num_sms * kCopyCtas;
+    const int64_t units = (int64_t)a.max_pairs * a.slabs, most = (int64_t)num_sms * kCopyCtas;
     const int grid = (int)(units < most ? units : most);
-    const bool tight = (a.hs == a.head_dim && a.ts == (int64_t)a.Hkv * a.head_dim) || (a.ts == a.head_dim && a.hs == (int64_t)kPage * a.head_dim);
+    const bool tight = (a.hs == a.head_dim && a.ts == (int64_t)a.Hkv * a.head_dim) || (a.ts == a.head_dim && a.hs == (int64_t)a.tokens * a.head_dim);
     const bool few = a.max_pairs <= kMany;
     const auto kernel = tight ? (few ? copy_pages_kernel<true, 1> : copy_pages_kernel<true, kChecked>)
                               : (few ? copy_pages_kernel<false, 1> : copy_pages_kernel<false, kChecked>);

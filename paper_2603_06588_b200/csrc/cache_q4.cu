@@ -1,0 +1,278 @@
+// What fills and empties a cache held in 4 bits (its layout is in q4.cuh): the rotary append that quantises as it writes, and the read-back
+// to the pages of a bf16 cache, which is what hook_attn_prefill and hook_capture_qk read.
+//
+// Quantising: the D / NG elements of a group, rounded to bf16, are lowest + step c with
+//   lowest = min x,  step = (max x - min x) / 15 in bf16 (0 below 2^-100),  t = x - lowest in 32 bits,  c = t / step rounded to nearest,
+// halves to even, 0 .. 15 -- of the quotient itself and not of a rounded one, so that a code can be told from the inputs.  An element is off
+// by half a step at most (and by 15/512 of one more where the step was rounded down).
+#include "q4.cuh"
+#include "rope_device.cuh"
+
+namespace hook_attn {
+
+namespace {
+
+constexpr int kAppendThreads = 256;
+constexpr int kAppendRows = 8;             // rows per CTA at most: one warp looks each of them up
+constexpr int kAppendStage = 40 * 1024;    // bytes of keys and values of its rows that a CTA holds
+
+// c with |t - c step| at most half a step, halves to even.  t / step is estimated with the step's reciprocal (off by 2^-22 of it), and what is
+// left over is exact where it decides: t and c step lie within a step of one another.
+__device__ __forceinline__ uint32_t q4_code(float t, float step, float inv)
+{
+    float c = rintf(t * inv);
+    const float left = fmaf(-c, step, t), half = 0.5f * step;
+    const bool odd = ((int)c & 1) != 0;
+    if (left > half || (left == half && odd)) c += 1.f;
+    else if (left < -half || (left == -half && odd)) c -= 1.f;
+    return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
+}
+
+// A CTA takes a few rows.  Queries are turned and stored as in hook_rope_append; keys (turned) and values go to shared memory as bf16, then
+// a thread takes eight neighbouring elements of a head: the lanes of a group agree on its lowest and highest value, a thread's codes are a
+// word of K as they are, and four lanes exchange theirs for V.
+template <typename T, int V, int HD, int NG>
+__global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __grid_constant__ RopeArgs a)
+{
+    using Slab = Q4Slab<HD, NG>;
+    __shared__ __align__(16) float2 turn[kAppendRows][kMaxPairs];
+    __shared__ RowPlace places[kAppendRows];
+    extern __shared__ __align__(16) __nv_bfloat16 held[];            // [rows][K, V][Hkv][HD]
+    const int row0 = blockIdx.x * a.rows_per_cta, warp = threadIdx.x >> 5;
+    if (warp < a.rows_per_cta) {
+        const RowPlace r = find_row(a, row0 + warp);
+        if ((threadIdx.x & 31) == 0) {
+            places[warp] = r;
+            if (r.state == kBroken) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        }
+    }
+    if (!a.positions) __syncthreads();             // the angles go by the places
+    for (int i = threadIdx.x; i < a.rows_per_cta * kMaxPairs; i += kAppendThreads) {
+        const int r = i / kMaxPairs, pair = i % kMaxPairs, row = row0 + r;
+        if (pair < a.pairs && row < a.total_q)
+            turn[r][pair] = turn_of(a, a.positions ? a.positions[a.axis_of_pair[pair] * a.axis_stride + row] : places[r].pos, pair);
+    }
+    __syncthreads();
+
+    constexpr int PER_HEAD = HD / (2 * V);
+    const int heads = a.Hq + 2 * a.Hkv, turning = a.pairs / V, total = a.rows_per_cta * heads * PER_HEAD;
+    for (int i = threadIdx.x; i < total; i += kAppendThreads) {
+        const int j = i % PER_HEAD, rh = i / PER_HEAD, r = rh / heads;
+        int h = rh - r * heads;
+        const int state = places[r].state;
+        if (state == kBehind || (state == kBroken && h >= a.Hq)) continue;
+        const int64_t row = row0 + r;
+        const T* src;
+        __nv_bfloat16* dst;
+        bool turns = j < turning;
+        if (h < a.Hq) {
+            src = static_cast<const T*>(a.q) + row * a.q_row + h * a.q_head;
+            dst = a.q_out + (row * a.Hq + h) * HD;
+        } else {
+            h -= a.Hq;
+            dst = held + (r * 2 * a.Hkv + h) * HD;
+            if (h < a.Hkv) {
+                src = static_cast<const T*>(a.k) + row * a.k_row + h * a.k_head;
+            } else {
+                src = static_cast<const T*>(a.v) + row * a.v_row + (h - a.Hkv) * a.v_head;
+                turns = false;
+            }
+        }
+        int e0 = j * 2 * V, e1 = e0 + V;
+        if (a.halves && j < turning) {             // v takes the same runs as k: which they are is of no account there
+            e0 = j * V;
+            e1 = a.pairs + j * V;
+        }
+        float x[V], y[V];
+        load(x, src + e0);
+        load(y, src + e1);
+        if (turns) turn_item<V>(x, y, &turn[r][j * V], a.halves);
+        if (state == kBroken) {
+#pragma unroll
+            for (int m = 0; m < V; ++m) x[m] = y[m] = 0.f;
+        }
+        store(dst + e0, x);
+        store(dst + e1, y);
+    }
+    __syncthreads();
+
+    constexpr int CHUNKS = HD / 8, LANES = CHUNKS / NG;              // threads to a head and to a group
+    const int work = a.rows_per_cta * 2 * a.Hkv * CHUNKS, rounded = (work + kAppendThreads - 1) / kAppendThreads * kAppendThreads;
+    for (int i = threadIdx.x; i < rounded; i += kAppendThreads) {    // all lanes of a warp stay: they exchange values
+        const int c = i % CHUNKS, rh = i / CHUNKS, r = rh / (2 * a.Hkv);
+        int h = rh - r * 2 * a.Hkv;
+        const bool live = i < work && places[r].state == kGood;
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (live) raw = *reinterpret_cast<const uint4*>(held + (size_t)rh * HD + 8 * c);
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        float x[8], bad = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = q4_step(w[e]);              // a bf16 in the low half, and one in the high half
+            x[2 * e + 1] = q4_lowest(w[e]);
+        }
+        float lo = x[0], hi = x[0];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            lo = fminf(lo, x[e]);
+            hi = fmaxf(hi, x[e]);
+            bad = fmaf(x[e], 0.f, bad);            // NaN when an element is not finite
+        }
+#pragma unroll
+        for (int d = 1; d < LANES; d <<= 1) {
+            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+            bad += __shfl_xor_sync(0xffffffffu, bad, d);
+        }
+        float step = __bfloat162float(__float2bfloat16((hi - lo) / 15.f));
+        if (step < 7.88860905e-31f) step = 0.f;    // 2^-100
+        if (bad != 0.f || !(step <= 3.3895314e38f)) step = __int_as_float(0x7fc00000);
+        const float inv = step > 0.f ? 1.f / step : 0.f;
+        uint32_t codes = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (step > 0.f) codes |= q4_code(x[e] - lo, step, inv) << (4 * e);
+        const bool value = h >= a.Hkv;
+        uint32_t others[4];                        // of the four chunks of 32 elements, in their order
+#pragma unroll
+        for (int k = 0; k < 4; ++k) others[k] = __shfl_sync(0xffffffffu, codes, (threadIdx.x & 28) + k);
+        if (!live) continue;
+        if (value) h -= a.Hkv;
+        const int t = places[r].pos % kPage;
+        uint8_t* slab = reinterpret_cast<uint8_t*>(a.k_cache) + places[r].slot + h * a.hs;
+        if (!value) {
+            *reinterpret_cast<uint32_t*>(slab + t * Slab::kRow + (c % 4 * (HD / 32) + c / 4) * 4) = codes;
+        } else {
+            const int n = c % 4, row = q4_row(t);
+            uint32_t even = 0, odd = 0;            // nibbles of elements 2 n and 2 n + 1 of the four chunks
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t byte = others[k] >> (8 * n);
+                even |= (byte & 15u) << (4 * k);
+                odd |= ((byte >> 4) & 15u) << (4 * k);
+            }
+            uint8_t* at = slab + Slab::kCodes + row * Slab::kRow + c / 4 * 2;
+            *reinterpret_cast<uint16_t*>(at + q4_unit<HD>(row, 2 * n) * (HD / 16)) = (uint16_t)even;
+            *reinterpret_cast<uint16_t*>(at + q4_unit<HD>(row, 2 * n + 1) * (HD / 16)) = (uint16_t)odd;
+        }
+        if (c % LANES == 0) {
+            const uint32_t pair = (__float_as_uint(step) >> 16) | (__float_as_uint(lo) & 0xffff0000u);
+            *reinterpret_cast<uint32_t*>(slab + 2 * Slab::kCodes + value * Slab::kParams + (t * NG + c / LANES) * 4) = pair;
+        }
+    }
+}
+
+template <typename T, int V, int HD, int NG>
+cudaError_t issue(RopeArgs& a, int num_sms, cudaStream_t st)
+{
+    // as many rows per CTA as let all CTAs be resident at once, within the shared memory that holds their keys and values
+    const int row_bytes = 2 * a.Hkv * HD * 2, resident = num_sms * 4;
+    int rows = (a.total_q + resident - 1) / resident;
+    if (rows > kAppendRows) rows = kAppendRows;
+    if (rows > kAppendStage / row_bytes) rows = kAppendStage / row_bytes > 0 ? kAppendStage / row_bytes : 1;
+    a.rows_per_cta = rows;
+    rope_append_q4_kernel<T, V, HD, NG><<<(a.total_q + rows - 1) / rows, kAppendThreads, rows * row_bytes, st>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T, int V>
+cudaError_t for_group(RopeArgs& a, int group, int num_sms, cudaStream_t st)
+{
+    const int ng = a.head_dim / group;
+    if (a.head_dim == 64) return ng == 1 ? issue<T, V, 64, 1>(a, num_sms, st) : issue<T, V, 64, 2>(a, num_sms, st);
+    if (ng == 1) return issue<T, V, 128, 1>(a, num_sms, st);
+    return ng == 2 ? issue<T, V, 128, 2>(a, num_sms, st) : issue<T, V, 128, 4>(a, num_sms, st);
+}
+
+template <typename T>
+cudaError_t launch(RopeArgs& a, int group, int num_sms, cudaStream_t st)
+{
+    // the widest run that divides the rotated half and the strides and on whose multiples the tensors start, as in hook_rope_append
+    const int64_t strides = a.q_row | a.q_head | a.k_row | a.k_head | a.v_row | a.v_head | a.pairs;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v);
+    if (((strides & 7) == 0) && (from & 15) == 0) return for_group<T, 8>(a, group, num_sms, st);
+    if (((strides | (int64_t)(from / sizeof(T))) & 1) == 0) return for_group<T, 2>(a, group, num_sms, st);
+    return for_group<T, 1>(a, group, num_sms, st);
+}
+
+// ---- read-back ----------------------------------------------------------------------------------------------------------------------
+constexpr int kReadThreads = 256;
+
+// A warp takes a (page, KV head) of a sequence: the slab comes to shared memory with wide loads, then a lane writes 16 bytes of a token's
+// row at a time.
+template <int HD, int NG>
+__global__ void __launch_bounds__(kReadThreads) q4_read_kernel(const __grid_constant__ Q4ReadArgs a)
+{
+    using Slab = Q4Slab<HD, NG>;
+    constexpr int WARPS = kReadThreads / 32, CHUNKS = HD / 8;
+    __shared__ __align__(16) uint8_t slabs[WARPS][Slab::kBytes];
+    const int s = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int L = a.seq_lens[s];
+    int from = a.first ? a.first[s] : 0;
+    if (L < 0 || L > a.max_keys || from < 0) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+        return;
+    }
+    const int page0 = from / kPage;
+    const int64_t units = (int64_t)max(0, (L + kPage - 1) / kPage - page0) * a.Hkv;
+    uint8_t* mine = slabs[warp];
+    for (int64_t u = (int64_t)blockIdx.x * WARPS + warp; u < units; u += (int64_t)gridDim.x * WARPS) {
+        const int j = page0 + (int)(u / a.Hkv), h = (int)(u % a.Hkv);
+        const int page = a.block_table[(int64_t)s * a.max_blocks + j], to = a.to_table[(int64_t)s * a.to_max_blocks + j];
+        if (page < 0 || page >= a.num_blocks || to < 0 || to >= a.to_num_blocks) {
+            if (lane == 0) report(a.status, HOOK_ATTN_ERR_BOUNDS);
+            continue;
+        }
+        const uint4* src = reinterpret_cast<const uint4*>(a.pages + (int64_t)page * a.page_block + (int64_t)h * a.page_head);
+        __syncwarp();
+        for (int i = lane; i < Slab::kBytes / 16; i += 32) reinterpret_cast<uint4*>(mine)[i] = src[i];
+        __syncwarp();
+        const int t_from = max(0, from - j * kPage), t_to = min(kPage, L - j * kPage);
+        const int64_t out = (int64_t)to * a.bs + (int64_t)h * a.hs;
+        const uint32_t* params = reinterpret_cast<const uint32_t*>(mine + 2 * Slab::kCodes);
+        for (int i = lane; i < kPage * CHUNKS; i += 32) {
+            const int t = i / CHUNKS, c = i % CHUNKS;
+            if (t < t_from || t >= t_to) continue;
+            const uint32_t kp = params[t * NG + c / (CHUNKS / NG)], vp = params[(kPage + t) * NG + c / (CHUNKS / NG)];
+            const uint32_t codes = *reinterpret_cast<const uint32_t*>(mine + t * Slab::kRow + (c % 4 * (HD / 32) + c / 4) * 4);
+            const int row = q4_row(t);
+            const uint8_t* vrow = mine + Slab::kCodes + row * Slab::kRow + c / 4 * 2;
+            float k[8], v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                k[e] = fmaf(q4_step(kp), (float)((codes >> (4 * e)) & 15u), q4_lowest(kp));
+                const uint32_t half = *reinterpret_cast<const uint16_t*>(vrow + q4_unit<HD>(row, e) * (HD / 16));
+                v[e] = fmaf(q4_step(vp), (float)((half >> (4 * (c % 4))) & 15u), q4_lowest(vp));
+            }
+            store(a.k_cache + out + (int64_t)t * a.ts + 8 * c, k);
+            store(a.v_cache + out + (int64_t)t * a.ts + 8 * c, v);
+        }
+    }
+}
+
+}  // namespace
+
+// `a.k_cache` is the pages, `a.bs` and `a.hs` their strides in bytes, `a.ts` 0.
+cudaError_t launch_rope_append_q4(RopeArgs& a, int dtype, int group, int num_sms, cudaStream_t st)
+{
+    if (dtype == HOOK_DTYPE_BF16) return launch<__nv_bfloat16>(a, group, num_sms, st);
+    if (dtype == HOOK_DTYPE_F16) return launch<__half>(a, group, num_sms, st);
+    return launch<float>(a, group, num_sms, st);
+}
+
+cudaError_t launch_q4_read(const Q4ReadArgs& a, int head_dim, int group, int num_sms, cudaStream_t st)
+{
+    // CTAs for the longest sequence that the table allows, and no more in all than fill the device a few times
+    const int64_t most = ((int64_t)a.max_keys / kPage + 1) * a.Hkv / (kReadThreads / 32) + 1, share = (int64_t)num_sms * 32 / a.num_seqs + 1;
+    const dim3 grid((unsigned)(most < share ? most : share), a.num_seqs);
+    const int ng = head_dim / group;
+    if (head_dim == 64) {
+        if (ng == 1) q4_read_kernel<64, 1><<<grid, kReadThreads, 0, st>>>(a);
+        else q4_read_kernel<64, 2><<<grid, kReadThreads, 0, st>>>(a);
+    } else if (ng == 1) q4_read_kernel<128, 1><<<grid, kReadThreads, 0, st>>>(a);
+    else if (ng == 2) q4_read_kernel<128, 2><<<grid, kReadThreads, 0, st>>>(a);
+    else q4_read_kernel<128, 4><<<grid, kReadThreads, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace hook_attn

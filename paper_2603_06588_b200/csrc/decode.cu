@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kMergeMaxWarps * 32) decode_merge_kernel(const
     }
     const float inv = 1.f / ltot;
     if (d < HD) {
-        val = val * inv + steer_d;
+        val = Mg == kBrokenMax ? 0.f : val * inv + steer_d;
         orow[d] = __float2bfloat16(val);
     }
     if (mrow && d < a.S) mrow[d] = mm * inv;
@@ -253,7 +253,7 @@ static cudaError_t launch_merge(const KernelArgs& a, const HeadCfg& hc, bool str
 
 // Partials per unit when `ctas` streaming CTAs of `warps` warps share the pages of the call (half-full
 // sequences assumed): whole groups of four warps inside a long unit, plus the warps of its two shared groups.
-static long stream_parts_estimate(const KernelArgs& a, int ctas, int warps)
+long stream_parts_estimate(const KernelArgs& a, int ctas, int warps)
 {
     const long max_pages = ((long)a.max_keys + kPage - 1) / kPage;
     const long groups = (long)ctas * warps / kDecWarps;
@@ -335,6 +335,12 @@ size_t decode_stream_workspace_bytes(int num_seqs, int Hkv, int G, int head_dim)
 {
     const size_t per_part = (size_t)G * decode_partial_stride(head_dim) * sizeof(float);
     return decode_prefix_bytes(num_seqs) + ((size_t)num_seqs * Hkv + kDecMaxWorkers) * per_part;
+}
+
+// For the decode over 4-bit pages, whose first-stage kernels leave the same partials.
+cudaError_t launch_decode_merge(const KernelArgs& a, const HeadCfg& hc, int head_dim, bool stream, long parts, cudaStream_t st)
+{
+    return head_dim == 128 ? launch_merge<128>(a, hc, stream, parts, st) : launch_merge<64>(a, hc, stream, parts, st);
 }
 
 cudaError_t launch_decode_stream_merge(const KernelArgs& a, const HeadCfg& hc, int ctas, int warps, cudaStream_t st)

@@ -18,6 +18,7 @@ constexpr int kDecMaxSMs = 148;                       // SMs of a B200; a device
 constexpr int kDecStreamUnits = 2 * kDecMaxSMs;       // the streaming kernel is picked for fewer units than this
 constexpr int kDecMaxWorkers = kDecCtasPerSM * kDecMaxSMs * kDecWarps;   // most warps that share the flat page list
 constexpr int kScanSeqs = 512;                        // most sequences the streaming kernel is picked for (a power of two)
+constexpr float kBrokenMax = 3.402823466e38f;          // the maximum of a partial that ran into a page out of range: its row becomes zeros
 constexpr int kPartPad = 16;   // floats after o[D] in a partial: m, l, s[0..7], padding
 static_assert(kDecStreamUnits <= kScanSeqs, "the streaming kernel scans all sequences in one pass");
 
@@ -344,13 +345,25 @@ struct DecStreamShared {
     DecFold fold[NW / kDecWarps];
 };
 
-// The work of streaming CTA `cta` (of a grid whose warps add up to a.workers): NW warps, each with
-// kDecStages * 2 page buffers in `smem`.  Every thread of the CTA calls it.
-template <int HD, int NS, int NW>
+// A warp that reduces runs of bf16 pages, with kDecStages * 2 page buffers of its own in shared memory.
+template <int HD>
+struct Bf16Walk {
+    static constexpr int kBytes = kDecStages * 2 * kPage * HD * 2;   // of one warp
+    uint32_t base;
+    __device__ __forceinline__ Bf16Walk(uint8_t* smem, int warp) : base(smem_u32(smem) + warp * kBytes) {}
+    template <int NS, typename... Rest>
+    __device__ __forceinline__ void segment(const KernelArgs& a, const HeadCfg& hc, int s, int kvh, int pg, int seg, int L, Rest&&... rest)
+    {
+        decode_segment<HD, NS>(a, hc, s, kvh, pg, seg, L, base, rest...);
+    }
+};
+
+// The work of streaming CTA `cta` (of a grid whose warps add up to a.workers): NW warps, each a Walk
+// with its buffers in `smem`.  Every thread of the CTA calls it.
+template <int HD, int NS, int NW, typename Walk = Bf16Walk<HD>>
 __device__ __forceinline__ void decode_stream_cta(const KernelArgs& a, const HeadCfg& hc, uint8_t* smem, int cta,
                                                   DecStreamShared<NW>& sh)
 {
-    constexpr int TILEB = kPage * HD * 2;   // bytes per 16-key tile
     constexpr int KS = HD / 16;
     constexpr int EPT = DecStreamShared<NW>::kEPT;
     constexpr int NT = NW * 32;
@@ -430,7 +443,7 @@ __device__ __forceinline__ void decode_stream_cta(const KernelArgs& a, const Hea
         pg = (int)(r % np);
     };
 
-    const uint32_t wbase = smem_u32(smem) + warp * (kDecStages * 2 * TILEB);
+    Walk walk(smem, warp);
     const size_t pstride = decode_partial_stride(HD);
     float* parts = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + decode_prefix_bytes(a.num_seqs));
 
@@ -441,9 +454,9 @@ __device__ __forceinline__ void decode_stream_cta(const KernelArgs& a, const Hea
     locate(c_begin, s, kvh, pg, np, L);
     if (c_end - c_begin <= (long long)(np - pg)) {        // uniform over the group
         const int seg = (int)(f_end - f_begin);
-        decode_segment<HD, NS>(a, hc, s, kvh, pg + (int)(f_begin - c_begin), seg, L, wbase, sh.span[warp], m0, m1, l0, l1, o, sm);
+        walk.template segment<NS>(a, hc, s, kvh, pg + (int)(f_begin - c_begin), seg, L, sh.span[warp], m0, m1, l0, l1, o, sm);
         float* part = parts + ((size_t)s * a.Hkv + kvh + (W - (warp & (kDecWarps - 1)))) * G * pstride;
-        float* red = reinterpret_cast<float*>(smem + (size_t)quad * kDecWarps * kDecStages * 2 * TILEB);
+        float* red = reinterpret_cast<float*>(smem + (size_t)quad * kDecWarps * Walk::kBytes);
         decode_fold_cta<HD, NS>(part, G, red, sh.fold[quad], 1 + quad, m0, m1, l0, l1, o, sm);
         return;
     }
@@ -454,7 +467,7 @@ __device__ __forceinline__ void decode_stream_cta(const KernelArgs& a, const Hea
     long long rem = f_end - f_begin;
     while (rem > 0) {
         const int seg = (int)min((long long)(np - pg), rem);   // pages of unit (s, kvh) this warp handles
-        decode_segment<HD, NS>(a, hc, s, kvh, pg, seg, L, wbase, sh.span[warp], m0, m1, l0, l1, o, sm);
+        walk.template segment<NS>(a, hc, s, kvh, pg, seg, L, sh.span[warp], m0, m1, l0, l1, o, sm);
         decode_store_warp_partial<HD, NS>(parts + ((size_t)s * a.Hkv + kvh + W) * G * pstride, G, m0, m1, l0, l1, o, sm);
 
         // ---- next unit ----

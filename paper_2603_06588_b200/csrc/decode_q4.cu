@@ -1,0 +1,502 @@
+// The hooked attention of single query rows over a cache held in 4 bits: scores, softmax, span masses, P V and steering as in decode.cu,
+// whose cuts, folds and merge it shares.  Only the walk over a run of pages is its own.
+//
+// A warp takes a page of one KV head at a time: one bulk copy brings its slab (2.1 to 2.5 KB) into one of the warp's stages.  The codes
+// go into the matrix instructions as they are: a nibble of a masked word, read as a half, is the number code * 2^-24 (or 2^-20 for the nibble
+// above it), exactly, and products with subnormal halves are exact too.  So no code is converted; a word of eight costs four ANDs and a
+// shift, and the powers of two go into the queries and out of the sums.  With k = lowest + step c for the tokens' groups,
+//   x_t = scale * sum_g (step_tg * (q_g . c_tg) + lowest_tg * sum(q_g)),    o = sum_t sum_g p_t step_tg c_tg + sum_t p_t lowest_tg:
+// the steps of K multiply the partial products of a group, those of V the probabilities before their one rounding to halves (off by
+// 2^-12 of a probability times its group's range), and the lowest values are summed in 32 bits.
+//
+// Halves reach from 2^-24 to 2^16, so the softmax's reference is that of p * step: it is raised when a score exceeds it by 2^8 or a step
+// exceeds 2^7 times the power of two that stands for the steps.  It cancels in o / l and s / l, as in decode.cu.
+#include "decode_device.cuh"
+#include "q4.cuh"
+
+namespace hook_attn {
+
+// decode.cu
+cudaError_t launch_decode_merge(const KernelArgs& a, const HeadCfg& hc, int head_dim, bool stream, long parts, cudaStream_t st);
+long stream_parts_estimate(const KernelArgs& a, int ctas, int warps);
+
+namespace {
+
+constexpr int kQ4Stages = 4;          // slabs in flight or in use per warp
+constexpr int kQ4CtasPerSM = 4;
+constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
+constexpr float kLeastLog = -80.f;    // steps below 2^-80 count as 2^-80 in the reference
+
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 t = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+// N words (1, 2 or 4) from shared memory, N * 4 bytes aligned.
+template <int N>
+__device__ __forceinline__ void lds(uint32_t (&r)[N], uint32_t addr)
+{
+    if constexpr (N == 1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[0]) : "r"(addr));
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+    else asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// A warp that reduces runs of 4-bit pages.  Its stages and their barriers are its own; `turn` counts the pages it has taken, so stages and
+// phases go on from one run to the next.
+template <int HD, int NG>
+struct Q4Walk {
+    using Slab = Q4Slab<HD, NG>;
+    static constexpr int kBytes = kQ4Stages * Slab::kBytes;           // of one warp's stages
+    // of a CTA: the stages, where its warps' sums are folded in the end, then the barriers, which nothing else may touch
+    static constexpr int kCtaBytes = kDecWarps * (kBytes + kQ4Stages * 8);
+    static_assert(kDecWarps * 8 * (HD + 4) * 4 <= kDecWarps * kBytes, "the fold's buffer fits the stages");
+    uint32_t base, bars, turn = 0;
+
+    __device__ __forceinline__ Q4Walk(uint8_t* smem, int warp)
+        : base(smem_u32(smem) + warp * kBytes), bars(smem_u32(smem) + kDecWarps * kBytes + warp * kQ4Stages * 8)
+    {
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+            for (int i = 0; i < kQ4Stages; ++i) mbar_init(bars + 8 * i, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+    }
+
+    template <int NS>
+    __device__ __forceinline__ void segment(const KernelArgs& a, const HeadCfg& hc, int s, int kvh, int pg, int seg, int L, int* span,
+                                            float& m0, float& m1, float& l0, float& l1, float (&o)[HD / 16][4], float (&sm)[NS > 0 ? NS : 1][2])
+    {
+        constexpr int KS = HD / 16, W = HD / 32, PER = W / NG;        // W: words of a lane's K codes; PER: words to a group
+        constexpr int NSX = NS > 0 ? NS : 1;
+        const int lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3, G = a.G;
+
+        m0 = m1 = -INFINITY;
+        l0 = l1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NSX; ++j) sm[j][0] = sm[j][1] = 0.f;
+        if (seg <= 0) return;
+
+        const int32_t* bt = a.block_table + (int64_t)s * a.max_blocks + pg;
+        const int key_base = pg * kPage;
+        const char* pages = reinterpret_cast<const char*>(a.k) + (int64_t)kvh * a.hs;     // strides in bytes
+
+        bool probe = false, broken = false;
+        if constexpr (NS > 0) {
+            for (int i = 0; i < G; ++i) probe |= (hc.slot[kvh * G + i] >= 0);
+            __syncwarp();
+            if (lane < 2 * NS) {
+                const int j = lane >> 1;
+                span[lane] = (probe && j < a.S) ? a.spans[((int64_t)s * a.S + j) * 2 + (lane & 1)] : 0;
+            }
+            __syncwarp();
+        }
+
+        // block ids of 32 consecutive pages, one per lane; the next 32 are fetched a window ahead
+        int btw = 0, btw_next = (lane < seg) ? bt[lane] : 0;
+        auto issue = [&](int it) {
+            if (it >= seg) return;
+            if ((it & 31) == 0) {
+                btw = btw_next;
+                btw_next = (it + 32 + lane < seg) ? bt[it + 32 + lane] : 0;
+            }
+            const int page = __shfl_sync(0xffffffffu, btw, it & 31);
+            const bool ok = page >= 0 && page < a.num_blocks;
+            broken |= !ok;
+            if (lane == 0) {
+                const uint32_t st = (turn + it) % kQ4Stages, bar = bars + 8 * st;
+                if (ok) {
+                    mbar_expect_tx(bar, Slab::kBytes);
+                    bulk_load(base + st * Slab::kBytes, pages + (int64_t)page * a.bs, Slab::kBytes, bar);
+                } else {
+                    report(a.status, HOOK_ATTN_ERR_BOUNDS);
+                    mbar_arrive(bar);
+                }
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kQ4Stages - 1; ++i) issue(i);
+
+        // The queries of head g of the group as halves, times a power of two that brings the largest to [2^14, 2^15): what is below 2^-27 of
+        // that loses bits.  In a word's pairs (element n, n + 4) the odd nibbles stand for 16 times their code.
+        uint32_t qb[KS][2];
+        float qs0, qs1, qsum[NG][2];
+        {
+            float x[W][8], most = 0.f, sum[NG];
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                uint4 raw = make_uint4(0, 0, 0, 0);
+                if (g < G) raw = *reinterpret_cast<const uint4*>(a.q + ((int64_t)s * a.Hq + kvh * G + g) * HD + 32 * i + 8 * tq);
+                const uint32_t r[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[i][2 * e] = __uint_as_float(r[e] << 16);
+                    x[i][2 * e + 1] = __uint_as_float(r[e] & 0xffff0000u);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[i][e]));
+            }
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                sum[j] = 0.f;
+#pragma unroll
+                for (int i = j * PER; i < (j + 1) * PER; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[j] += x[i][e];
+            }
+#pragma unroll
+            for (int d = 1; d <= 2; d <<= 1) {
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+#pragma unroll
+                for (int j = 0; j < NG; ++j) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], d);
+            }
+            int up = 141 - (int)(__float_as_uint(most) >> 23);        // 14 less the exponent
+            up = most > 0.f ? min(max(up, -100), 100) : 0;
+            const float raise = __uint_as_float((uint32_t)(127 + up) << 23), odd = raise * 0.0625f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                qb[2 * i][0] = pack_f16(x[i][0] * raise, x[i][4] * raise);
+                qb[2 * i][1] = pack_f16(x[i][1] * odd, x[i][5] * odd);
+                qb[2 * i + 1][0] = pack_f16(x[i][2] * raise, x[i][6] * raise);
+                qb[2 * i + 1][1] = pack_f16(x[i][3] * odd, x[i][7] * odd);
+            }
+            const float back = __uint_as_float((uint32_t)(127 + min(24 - up, 127)) << 23) * a.scale_log2;   // 2^24: a code as a half
+            qs0 = __shfl_sync(0xffffffffu, back, 8 * tq);             // of heads 2 tq and 2 tq + 1
+            qs1 = __shfl_sync(0xffffffffu, back, 8 * tq + 4);
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                qsum[j][0] = __shfl_sync(0xffffffffu, sum[j], 8 * tq) * a.scale_log2;
+                qsum[j][1] = __shfl_sync(0xffffffffu, sum[j], 8 * tq + 4) * a.scale_log2;
+            }
+        }
+
+        // Scores so far at most m; the accumulators hold p 2^(x - f) with f = m + steps, where 2^steps stands for the steps of V.
+        float f0 = -INFINITY, f1 = -INFINITY, steps = kLeastLog, step_limit = 0.f, zl[NG][2];
+#pragma unroll
+        for (int j = 0; j < NG; ++j) zl[j][0] = zl[j][1] = 0.f;
+
+        uint64_t limit_ns = 2000000000ull;
+        for (int it = 0; it < seg; ++it) {
+            issue(it + kQ4Stages - 1);
+            const uint32_t st = (turn + it) % kQ4Stages;
+            if (!__all_sync(0xffffffffu, mbar_wait(bars + 8 * st, ((turn + it) / kQ4Stages) & 1u, nullptr, limit_ns))) {
+                if (lane == 0) report(a.status, HOOK_ATTN_ERR_TIMEOUT);
+                broken = true;
+                limit_ns = 1000000;                           // the others in flight are waited for, but not for long
+            }
+            const uint32_t kt = base + st * Slab::kBytes, vt = kt + Slab::kCodes, kp = vt + Slab::kCodes, vp = kp + Slab::kParams;
+            const int key0 = key_base + it * kPage;
+
+            // ---- scores: keys g and g + 8 of the page for the heads 2 tq and 2 tq + 1 ----
+            float acc[NG][4];
+            {
+                uint32_t wa[W], wb[W];
+                lds<W>(wa, kt + g * Slab::kRow + tq * (W * 4));
+                lds<W>(wb, kt + (g + 8) * Slab::kRow + tq * (W * 4));
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+#pragma unroll
+                    for (int i = j * PER; i < (j + 1) * PER; ++i) {
+                        mma_f16_16816(acc[j], wa[i] & 0x000f000fu, wb[i] & 0x000f000fu, wa[i] & 0x00f000f0u, wb[i] & 0x00f000f0u, qb[2 * i][0], qb[2 * i][1]);
+                        const uint32_t ua = wa[i] >> 8, ub = wb[i] >> 8;
+                        mma_f16_16816(acc[j], ua & 0x000f000fu, ub & 0x000f000fu, ua & 0x00f000f0u, ub & 0x00f000f0u, qb[2 * i + 1][0], qb[2 * i + 1][1]);
+                    }
+                }
+            }
+            float x0 = 0.f, x1 = 0.f, x2 = 0.f, x3 = 0.f;
+            {
+                uint32_t pa[NG], pb[NG];
+                lds<NG>(pa, kp + g * (NG * 4));
+                lds<NG>(pb, kp + (g + 8) * (NG * 4));
+                float w0 = 0.f, w1 = 0.f, w2 = 0.f, w3 = 0.f;
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    x0 += q4_step(pa[j]) * acc[j][0]; x1 += q4_step(pa[j]) * acc[j][1];
+                    x2 += q4_step(pb[j]) * acc[j][2]; x3 += q4_step(pb[j]) * acc[j][3];
+                    w0 += q4_lowest(pa[j]) * qsum[j][0]; w1 += q4_lowest(pa[j]) * qsum[j][1];
+                    w2 += q4_lowest(pb[j]) * qsum[j][0]; w3 += q4_lowest(pb[j]) * qsum[j][1];
+                }
+                x0 = x0 * qs0 + w0; x1 = x1 * qs1 + w1;
+                x2 = x2 * qs0 + w2; x3 = x3 * qs1 + w3;
+            }
+            uint32_t va[NG], vb[NG];                          // steps and lowest values of V
+            lds<NG>(va, vp + g * (NG * 4));
+            lds<NG>(vb, vp + (g + 8) * (NG * 4));
+            const int t0 = key0 + g, t1 = t0 + 8;
+            if (key0 + kPage > L) {                           // what lies behind the sequence may be anything
+                if (t0 >= L) {
+                    x0 = x1 = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) va[j] = 0;
+                }
+                if (t1 >= L) {
+                    x2 = x3 = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) vb[j] = 0;
+                }
+            }
+            float mx0 = fmaxf(x0, x2), mx1 = fmaxf(x1, x3), top = 0.f;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) top = fmaxf(top, fmaxf(q4_step(va[j]), q4_step(vb[j])));
+            // ---- the reference: m = f - steps ----
+            if (__any_sync(0xffffffffu, mx0 > f0 + (kDecRaise - steps) || mx1 > f1 + (kDecRaise - steps) || top > step_limit)) {
+#pragma unroll
+                for (int d = 4; d <= 16; d <<= 1) {
+                    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
+                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                }
+                const float e = fmaxf((float)((int)(__float_as_uint(top) >> 23) - 127), steps);
+                const float n0 = fmaxf(f0 - steps, mx0) + e, n1 = fmaxf(f1 - steps, mx1) + e;
+                const float c0 = fast_exp2(f0 - n0), c1 = fast_exp2(f1 - n1);
+                f0 = n0; f1 = n1;
+                steps = e;
+                step_limit = fast_exp2(e + 7.f);
+                l0 *= c0; l1 *= c1;
+#pragma unroll
+                for (int i = 0; i < KS; ++i) { o[i][0] *= c0; o[i][1] *= c1; o[i][2] *= c0; o[i][3] *= c1; }
+#pragma unroll
+                for (int j = 0; j < NG; ++j) { zl[j][0] *= c0; zl[j][1] *= c1; }
+                if (NS > 0) {
+#pragma unroll
+                    for (int j = 0; j < NSX; ++j) { sm[j][0] *= c0; sm[j][1] *= c1; }
+                }
+            }
+            const float p0 = fast_exp2(x0 - f0), p1 = fast_exp2(x1 - f1);
+            const float p2 = fast_exp2(x2 - f0), p3 = fast_exp2(x3 - f1);
+            l0 += p0 + p2;
+            l1 += p1 + p3;
+            if (NS > 0 && probe) {
+#pragma unroll
+                for (int j = 0; j < NSX; ++j) {
+                    const int sa = span[2 * j], sb = span[2 * j + 1];
+                    if (sb > key0 && sa < key0 + kPage) {
+                        const bool in0 = (t0 >= sa) && (t0 < sb), in1 = (t1 >= sa) && (t1 < sb);
+                        sm[j][0] += (in0 ? p0 : 0.f) + (in1 ? p2 : 0.f);
+                        sm[j][1] += (in0 ? p1 : 0.f) + (in1 ? p3 : 0.f);
+                    }
+                }
+            }
+            // ---- P V: for each group the probabilities times the steps, as the B operand (k = key, n = head) ----
+            uint32_t pb[NG][2];
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                const float sa = q4_step(va[j]), sb = q4_step(vb[j]);
+                pb[j][0] = movmatrix_trans(pack_f16(p0 * sa, p1 * sa));
+                pb[j][1] = movmatrix_trans(pack_f16(p2 * sb, p3 * sb));
+                zl[j][0] += p0 * q4_lowest(va[j]) + p2 * q4_lowest(vb[j]);
+                zl[j][1] += p1 * q4_lowest(va[j]) + p3 * q4_lowest(vb[j]);
+            }
+            constexpr int U = HD / 64;                        // words of a unit: keys 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9 of the page
+            uint32_t v0[U], v1[U], v2[U], v3[U];
+            const uint32_t unit = vt + tq * Slab::kRow + q4_unit<HD>(tq, g) * (U * 4);
+            lds<U>(v0, unit);
+            lds<U>(v1, unit + 4 * Slab::kRow);
+            lds<U>(v2, unit + 8 * Slab::kRow);
+            lds<U>(v3, unit + 12 * Slab::kRow);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {                     // 32 elements: two blocks of 16 of the output
+                const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+                uint32_t lo = __byte_perm(v0[j / 2], v1[j / 2], sel), hi = __byte_perm(v2[j / 2], v3[j / 2], sel);
+                const int grp = j / PER;
+                mma_f16_16816(o[2 * j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, pb[grp][0], pb[grp][1]);
+                lo >>= 8;
+                hi >>= 8;
+                mma_f16_16816(o[2 * j + 1], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, pb[grp][0], pb[grp][1]);
+            }
+            __syncwarp();                                     // the stage may be filled again
+        }
+        turn += seg;
+
+        // per-thread partial sums -> per-warp sums (lanes with the same tq hold the same heads)
+#pragma unroll
+        for (int d = 4; d <= 16; d <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, d);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, d);
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                zl[j][0] += __shfl_xor_sync(0xffffffffu, zl[j][0], d);
+                zl[j][1] += __shfl_xor_sync(0xffffffffu, zl[j][1], d);
+            }
+            if (NS > 0) {
+#pragma unroll
+                for (int j = 0; j < NS; ++j) {
+                    sm[j][0] += __shfl_xor_sync(0xffffffffu, sm[j][0], d);
+                    sm[j][1] += __shfl_xor_sync(0xffffffffu, sm[j][1], d);
+                }
+            }
+        }
+        m0 = f0;
+        m1 = f1;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const int j = i / 2 / PER;
+            o[i][0] = o[i][0] * 16777216.f + zl[j][0]; o[i][1] = o[i][1] * 16777216.f + zl[j][1];   // rows g: codes times 2^-24
+            o[i][2] = o[i][2] * 1048576.f + zl[j][0]; o[i][3] = o[i][3] * 1048576.f + zl[j][1];     // rows g + 8: times 2^-20
+        }
+        if (broken) {                                         // a page out of range: the row becomes zeros
+            m0 = m1 = kBrokenMax;
+            l0 = l1 = 1.f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < NSX; ++j) sm[j][0] = sm[j][1] = 0.f;
+        }
+    }
+};
+
+template <int HD, int NG>
+constexpr int q4_smem_bytes() { return Q4Walk<HD, NG>::kCtaBytes; }
+
+template <int HD, int NG, int NS>
+__global__ void __launch_bounds__(kDecWarps * 32, kQ4CtasPerSM) decode_q4_stream_kernel(const KernelArgs a, const HeadCfg hc)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ DecStreamShared<kDecWarps> sh;
+    decode_stream_cta<HD, NS, kDecWarps, Q4Walk<HD, NG>>(a, hc, smem, blockIdx.x, sh);
+}
+
+template <int HD, int NG, int NS>
+__global__ void __launch_bounds__(kDecWarps * 32, kQ4CtasPerSM) decode_q4_splitk_kernel(const KernelArgs a, const HeadCfg hc)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ int sh_span[kDecWarps][2 * kMaxSpans];
+    __shared__ DecFold sh_fold;
+
+    const int s = blockIdx.z, kvh = blockIdx.y, c = blockIdx.x;
+    const int warp = threadIdx.x >> 5;
+    asm volatile("griddepcontrol.wait;" ::: "memory");        // as in decode.cu: the merge of the call before may still be running
+    const int L = a.seq_lens[s];
+    if (L <= 0 || L > a.max_keys) return;                     // reported and zero-filled by the merge kernel
+    const int start = c * a.chunk;
+    if (start >= L) return;
+    const int ntiles = (min(L, start + a.chunk) - start + kPage - 1) / kPage;
+    const int per = (ntiles + kDecWarps - 1) / kDecWarps;     // the four warps take contiguous quarters of the chunk's pages
+    const int first = min(warp * per, ntiles);
+    Q4Walk<HD, NG> walk(smem, warp);
+    float m0, m1, l0, l1, o[HD / 16][4], sm[NS > 0 ? NS : 1][2];
+    walk.template segment<NS>(a, hc, s, kvh, start / kPage + first, min(per, ntiles - first), L, sh_span[warp], m0, m1, l0, l1, o, sm);
+    float* part = a.ws + (((size_t)s * a.Hkv + kvh) * a.max_chunks + c) * a.G * decode_partial_stride(HD);
+    decode_fold_cta<HD, NS>(part, a.G, reinterpret_cast<float*>(smem), sh_fold, 1, m0, m1, l0, l1, o, sm);
+}
+
+// How a call is cut, from host-known bounds only, as in decode.cu: few units share their pages out evenly; many are cut into chunks.
+struct Q4Plan {
+    bool stream;
+    int chunk, max_chunks;
+};
+
+Q4Plan q4_plan(int num_seqs, int Hkv, int max_keys)
+{
+    Q4Plan p = {};
+    p.stream = (long)num_seqs * Hkv < kDecStreamUnits;
+    p.chunk = 2048;
+    while (p.chunk > 256) {
+        const long ctas = (long)num_seqs * Hkv * (((long)max_keys + p.chunk - 1) / p.chunk);
+        if (ctas >= 8L * kDecMaxSMs) break;
+        p.chunk >>= 1;
+    }
+    p.max_chunks = (int)(((long)max_keys + p.chunk - 1) / p.chunk);
+    if (p.max_chunks < 1) p.max_chunks = 1;
+    return p;
+}
+
+template <int HD, int NG, int NS>
+cudaError_t launch_t(KernelArgs a, const HeadCfg& hc, int num_sms, cudaStream_t st)
+{
+    const Q4Plan plan = q4_plan(a.num_seqs, a.Hkv, a.max_keys);
+    a.chunk = plan.chunk;
+    a.max_chunks = plan.max_chunks;
+    long parts;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kDecWarps * 32);
+    cfg.dynamicSmemBytes = q4_smem_bytes<HD, NG>();
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = plan.stream ? 0 : 1;
+    cudaError_t e;
+    if (plan.stream) {
+        const int ctas = kQ4CtasPerSM * (num_sms < kDecMaxSMs ? (num_sms > 0 ? num_sms : 1) : kDecMaxSMs);
+        a.workers = ctas * kDecWarps;
+        cfg.gridDim = dim3(ctas);
+        e = cudaLaunchKernelEx(&cfg, decode_q4_stream_kernel<HD, NG, NS>, a, hc);
+        parts = stream_parts_estimate(a, ctas, kDecWarps);
+    } else {
+        cfg.gridDim = dim3(plan.max_chunks, a.Hkv, a.num_seqs);
+        e = cudaLaunchKernelEx(&cfg, decode_q4_splitk_kernel<HD, NG, NS>, a, hc);
+        parts = plan.max_chunks;
+    }
+    if (e != cudaSuccess) return e;
+    return launch_decode_merge(a, hc, HD, plan.stream, parts, st);
+}
+
+template <int HD, int NG>
+cudaError_t launch_ng(const KernelArgs& a, const HeadCfg& hc, int num_sms, cudaStream_t st)
+{
+    if (!a.any_probe) return launch_t<HD, NG, 0>(a, hc, num_sms, st);
+    return a.S <= 4 ? launch_t<HD, NG, 4>(a, hc, num_sms, st) : launch_t<HD, NG, 8>(a, hc, num_sms, st);
+}
+
+template <int HD, int NG>
+cudaError_t configure_one()
+{
+    const auto allow = [](auto* kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, q4_smem_bytes<HD, NG>()); };
+    cudaError_t e;
+#define HOOK_CFG(NS) if ((e = allow(decode_q4_splitk_kernel<HD, NG, NS>)) != cudaSuccess || (e = allow(decode_q4_stream_kernel<HD, NG, NS>)) != cudaSuccess) return e;
+    HOOK_CFG(0) HOOK_CFG(4) HOOK_CFG(8)
+#undef HOOK_CFG
+    return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t configure_decode_q4()
+{
+    cudaError_t e = configure_one<64, 1>();
+    if (e == cudaSuccess) e = configure_one<64, 2>();
+    if (e == cudaSuccess) e = configure_one<128, 1>();
+    if (e == cudaSuccess) e = configure_one<128, 2>();
+    if (e == cudaSuccess) e = configure_one<128, 4>();
+    return e;
+}
+
+// As decode_workspace_bytes: one partial per (unit, chunk), or the page-count prefix and one per (unit, warp) that meet.
+size_t decode_q4_workspace_bytes(int num_seqs, int Hkv, int G, int head_dim, int max_keys)
+{
+    const Q4Plan plan = q4_plan(num_seqs, Hkv, max_keys);
+    const size_t per_part = (size_t)G * decode_partial_stride(head_dim) * sizeof(float);
+    if (plan.stream) return decode_prefix_bytes(num_seqs) + ((size_t)num_seqs * Hkv + kQ4MaxWorkers) * per_part;
+    return (size_t)num_seqs * Hkv * plan.max_chunks * per_part;
+}
+
+// `a.k` is the pages, `a.bs` and `a.hs` their strides in bytes.
+cudaError_t launch_decode_q4(const KernelArgs& a, const HeadCfg& hc, int head_dim, int group, int num_sms, cudaStream_t st)
+{
+    const int ng = head_dim / group;
+    if (head_dim == 64) return ng == 1 ? launch_ng<64, 1>(a, hc, num_sms, st) : launch_ng<64, 2>(a, hc, num_sms, st);
+    if (ng == 1) return launch_ng<128, 1>(a, hc, num_sms, st);
+    return ng == 2 ? launch_ng<128, 2>(a, hc, num_sms, st) : launch_ng<128, 4>(a, hc, num_sms, st);
+}
+
+}  // namespace hook_attn

@@ -153,13 +153,30 @@ int32_t dtype_of(const at::Tensor& t)
     }
 }
 
-PyObject* rope_append(PyObject*, PyObject* const* args, Py_ssize_t n)
+// The pages of a 4-bit cache, [blocks, Hkv, slab]: the slab's bytes tell the group.
+hook_q4_cache q4_of(const at::Tensor& pages, int64_t head_dim)
+{
+    check(pages.scalar_type() == at::kByte && (pages.size(2) <= 1 || pages.stride(2) == 1), "pages: uint8 [blocks, Hkv, slab bytes]");
+    hook_q4_cache q = {};
+    for (int group = 32; group <= 128; group *= 2)
+        if (group <= head_dim && pages.size(2) == kPage * head_dim + 8 * kPage * (head_dim / group)) q.group = group;
+    check(q.group > 0 || (head_dim != 64 && head_dim != 128), "pages: a slab of hook_q4_slab_bytes(head_dim, group)");
+    q.pages = pages.data_ptr();
+    q.block_stride = pages.stride(0);
+    q.head_stride = pages.stride(1);
+    return q;
+}
+
+// Both rotary appends; Q4: into `pages` in the place of k_cache and v_cache.
+template <bool Q4>
+PyObject* append(PyObject* const* args, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject* {
-        Call c(args, n, 4 + 16);
+        Call c(args, n, 4 + (Q4 ? 15 : 16));
         hook_rope_params p = {};
         const at::Tensor &q = c.tensor("q [T, Hq, D]", 3), &k = c.tensor("k [T, Hkv, D]", 3), &v = c.tensor("v [T, Hkv, D]", 3);
-        const at::Tensor &kc = c.tensor("k_cache [pages, 16, Hkv, D]", 4), &vc = c.tensor("v_cache [pages, 16, Hkv, D]", 4);
+        const at::Tensor &kc = Q4 ? c.tensor("pages [blocks, Hkv, slab bytes]", 3) : c.tensor("k_cache [pages, 16, Hkv, D]", 4);
+        const at::Tensor& vc = Q4 ? kc : c.tensor("v_cache [pages, 16, Hkv, D]", 4);
         const at::Tensor &table = c.tensor("block_table [seqs, pages]", 2), &lens = c.list("seq_lens: int32 [seqs]", at::kInt, table.size(0));
         const at::Tensor& freq = c.list("inv_freq: fp32 [R / 2]", at::kFloat, -1);
         const int64_t rows = q.size(0), pairs = freq.size(0);
@@ -175,9 +192,15 @@ PyObject* rope_append(PyObject*, PyObject* const* args, Py_ssize_t n)
         check(k.sizes() == v.sizes() && k.size(0) == rows && k.size(2) == q.size(2), "k and v [T, Hkv, D]");
         check(k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type(), "q, k and v of one type");
         check(rows == 0 || (q.stride(2) == 1 && k.stride(2) == 1 && v.stride(2) == 1), "q, k and v: neighbouring elements of a head");
-        check(kc.sizes() == vc.sizes() && kc.strides() == vc.strides() && kc.stride(3) == 1 && kc.size(3) == q.size(2) && kc.size(2) == k.size(1),
-              "k_cache and v_cache [pages, 16, Hkv, D] with the same strides");
-        check(kc.scalar_type() == at::kBFloat16 && vc.scalar_type() == at::kBFloat16, "a bf16 cache");
+        hook_q4_cache q4 = {};
+        if constexpr (Q4) {
+            q4 = q4_of(kc, q.size(2));
+            check(kc.size(1) == k.size(1), "pages of as many heads as k");
+        } else {
+            check(kc.sizes() == vc.sizes() && kc.strides() == vc.strides() && kc.stride(3) == 1 && kc.size(3) == q.size(2) && kc.size(2) == k.size(1),
+                  "k_cache and v_cache [pages, 16, Hkv, D] with the same strides");
+            check(kc.scalar_type() == at::kBFloat16 && vc.scalar_type() == at::kBFloat16, "a bf16 cache");
+        }
         check(table.scalar_type() == at::kInt && table.is_contiguous(), "block_table: int32, contiguous");
         p.num_axes = 1;
         p.axis_pairs[0] = narrow(pairs);
@@ -206,7 +229,7 @@ PyObject* rope_append(PyObject*, PyObject* const* args, Py_ssize_t n)
         p.num_q_heads = narrow(q.size(1));
         p.num_kv_heads = narrow(k.size(1));
         p.head_dim = narrow(q.size(2));
-        p.page_size = narrow(kc.size(1));
+        p.page_size = Q4 ? kPage : narrow(kc.size(1));
         p.num_blocks = narrow(kc.size(0));
         p.max_blocks_per_seq = narrow(table.size(1));
         p.dtype = dtype_of(q);
@@ -223,17 +246,23 @@ PyObject* rope_append(PyObject*, PyObject* const* args, Py_ssize_t n)
         p.inv_freq = Call::pointer<float>(&freq);
         p.positions = Call::pointer<int32_t>(positions);
         p.q_out = out.data_ptr();
-        p.k_cache = kc.data_ptr();
-        p.v_cache = vc.data_ptr();
-        p.kv_block_stride = kc.stride(0);
-        p.kv_token_stride = kc.stride(1);
-        p.kv_head_stride = kc.stride(2);
+        if constexpr (!Q4) {
+            p.k_cache = kc.data_ptr();
+            p.v_cache = vc.data_ptr();
+            p.kv_block_stride = kc.stride(0);
+            p.kv_token_stride = kc.stride(1);
+            p.kv_head_stride = kc.stride(2);
+        }
         p.block_table = Call::pointer<int32_t>(&table);
         p.seq_lens = Call::pointer<int32_t>(&lens);
         p.cu_q_lens = Call::pointer<int32_t>(cu);
-        return result(c.issue<decltype(hook_rope_append)>(&p), std::move(out));
+        if constexpr (Q4) return result(c.issue<decltype(hook_rope_append_q4)>(&p, &q4), std::move(out));
+        else return result(c.issue<decltype(hook_rope_append)>(&p), std::move(out));
     });
 }
+
+PyObject* rope_append(PyObject*, PyObject* const* args, Py_ssize_t n) { return append<false>(args, n); }
+PyObject* rope_append_q4(PyObject*, PyObject* const* args, Py_ssize_t n) { return append<true>(args, n); }
 
 PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -431,9 +460,224 @@ PyObject* cache_copy_pages(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
+PyObject* cache_copy_pages_q4(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        Call c(args, n, 4 + 4);
+        hook_q4_copy_params p = {};
+        PyObject* caches = PySequence_Fast(c.other(), "a list of pages");
+        if (!caches) throw Raised{};
+        struct Held {
+            PyObject* x;
+            ~Held() { Py_DECREF(x); }
+        } held{caches};
+        const Py_ssize_t layers = PySequence_Fast_GET_SIZE(caches);
+        std::vector<void*> at;
+        const at::Tensor* first = nullptr;
+        for (Py_ssize_t l = 0; l < layers; ++l) {
+            PyObject* x = PySequence_Fast_GET_ITEM(caches, l);
+            check(THPVariable_Check(x), "a list of pages");
+            const at::Tensor& t = THPVariable_Unpack(x);
+            if (!first) first = &t;
+            check(t.dim() == 3 && t.sizes() == first->sizes() && t.strides() == first->strides() && t.stride(2) == 1 && t.scalar_type() == at::kByte,
+                  "pages of one shape and one set of strides, uint8 [blocks, Hkv, slab bytes]");
+            check(t.is_cuda() && t.get_device() == c.device, "a tensor is not on the handle's device");
+            at.push_back(t.data_ptr());
+        }
+        const at::Tensor& pairs = c.tensor("pairs [n, 2]", 2);
+        const at::Tensor* count = c.maybe("num_pairs");
+        p.status = c.status();
+        check(pairs.scalar_type() == at::kInt && pairs.size(1) == 2 && pairs.is_contiguous(), "pairs: int32 [n, 2], contiguous");
+        if (count) check(count->scalar_type() == at::kInt && count->numel() == 1, "num_pairs: int32 [1]");
+        if (!first) return PyLong_FromLong(HOOK_ATTN_OK);
+        for (int d = 64; d <= 128; d *= 2)             // no two of the supported slabs are alike
+            for (int group = 32; group <= d; group *= 2)
+                if (first->size(2) == kPage * d + 8 * kPage * (d / group)) {
+                    p.head_dim = d;
+                    p.group = group;
+                }
+        check(p.group > 0, "pages: a slab of hook_q4_slab_bytes(head_dim, group)");
+        p.num_layers = narrow(layers);
+        p.num_blocks = narrow(first->size(0));
+        p.page_size = kPage;
+        p.num_kv_heads = narrow(first->size(1));
+        p.max_pairs = narrow(pairs.size(0));
+        p.block_stride = first->stride(0);
+        p.head_stride = first->stride(1);
+        p.pages = at.data();
+        p.pairs = Call::pointer<int32_t>(&pairs);
+        p.num_pairs = Call::pointer<int32_t>(count);
+        return PyLong_FromLong(c.issue<decltype(hook_cache_copy_pages_q4)>(&p));
+    });
+}
+
+PyObject* cache_read_q4(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        Call c(args, n, 4 + 8);
+        hook_q4_read_params p = {};
+        const at::Tensor& pages = c.tensor("pages [blocks, Hkv, slab bytes]", 3);
+        const at::Tensor &table = c.tensor("block_table [seqs, pages]", 2), &lens = c.list("seq_lens: int32 [seqs]", at::kInt, table.size(0));
+        const at::Tensor &kc = c.tensor("k_cache [pages, 16, Hkv, D]", 4), &vc = c.tensor("v_cache [pages, 16, Hkv, D]", 4);
+        const at::Tensor& to = c.tensor("to_table [seqs, pages]", 2);
+        const at::Tensor* first = c.maybe_list("first: int32 [seqs]", at::kInt, table.size(0));
+        p.status = c.status();
+        check(kc.sizes() == vc.sizes() && kc.strides() == vc.strides() && kc.stride(3) == 1 && kc.size(2) == pages.size(1) &&
+                  kc.scalar_type() == at::kBFloat16 && vc.scalar_type() == at::kBFloat16,
+              "k_cache and v_cache: bf16 [pages, 16, Hkv, D] with the same strides");
+        check(table.scalar_type() == at::kInt && table.is_contiguous(), "block_table: int32, contiguous");
+        check(to.scalar_type() == at::kInt && to.is_contiguous() && to.size(0) == table.size(0), "to_table: int32 [seqs, pages], contiguous");
+        const hook_q4_cache q4 = q4_of(pages, kc.size(3));
+        p.num_seqs = narrow(table.size(0));
+        p.num_kv_heads = narrow(kc.size(2));
+        p.head_dim = narrow(kc.size(3));
+        p.page_size = narrow(kc.size(1));
+        p.num_blocks = narrow(pages.size(0));
+        p.max_blocks_per_seq = narrow(table.size(1));
+        p.to_num_blocks = narrow(kc.size(0));
+        p.to_max_blocks_per_seq = narrow(to.size(1));
+        p.block_table = Call::pointer<int32_t>(&table);
+        p.seq_lens = Call::pointer<int32_t>(&lens);
+        p.first = Call::pointer<int32_t>(first);
+        p.k_cache = kc.data_ptr();
+        p.v_cache = vc.data_ptr();
+        p.kv_block_stride = kc.stride(0);
+        p.kv_token_stride = kc.stride(1);
+        p.kv_head_stride = kc.stride(2);
+        p.to_table = Call::pointer<int32_t>(&to);
+        return PyLong_FromLong(c.issue<decltype(hook_cache_read_q4)>(&p, &q4));
+    });
+}
+
+// A tensor that stays on the host, one value for each query head.
+const at::Tensor* host_list(PyObject* x, at::ScalarType type, int64_t length, const char* what)
+{
+    if (x == Py_None) return nullptr;
+    check(THPVariable_Check(x), what);
+    const at::Tensor& t = THPVariable_Unpack(x);
+    check(t.is_cpu() && t.scalar_type() == type && t.dim() == 1 && t.is_contiguous() && t.size(0) == length, what);
+    return &t;
+}
+
+PyObject* attn_decode_q4(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        Call c(args, n, 4 + 15);
+        hook_attn_params p = {};
+        const at::Tensor &q = c.tensor("q [seqs, Hq, D]", 3), &pages = c.tensor("pages [blocks, Hkv, slab bytes]", 3);
+        const at::Tensor &table = c.tensor("block_table [seqs, pages]", 2), &lens = c.list("seq_lens: int32 [seqs]", at::kInt, table.size(0));
+        const int64_t seqs = q.size(0), heads = q.size(1);
+        const at::Tensor* spans = c.maybe("spans");
+        const at::Tensor* mask = host_list(c.other(), at::kByte, heads, "head_mask: uint8 [Hq] on the host");
+        const at::Tensor* alpha = host_list(c.other(), at::kFloat, heads, "alpha: fp32 [Hq] on the host");
+        const at::Tensor* steer = c.maybe("steer_vec");
+        p.scale = (float)PyFloat_AsDouble(c.other());
+        if (PyErr_Occurred()) throw Raised{};
+        const at::Tensor *given_out = c.maybe("out"), *given_mass = c.maybe("span_mass"), *given_ws = c.maybe("workspace");
+        p.status = c.status();
+        p.max_seq_len = narrow(integer(c.other()));
+        const auto workspace_bytes = reinterpret_cast<decltype(&hook_attn_workspace_bytes)>(integer(c.other()));
+
+        check(q.scalar_type() == at::kBFloat16 && q.is_contiguous(), "q: bf16, contiguous");
+        check(table.scalar_type() == at::kInt && table.is_contiguous() && table.size(0) == seqs, "block_table: int32 [seqs, pages], contiguous");
+        if (spans) check(spans->scalar_type() == at::kInt && spans->is_contiguous() && spans->dim() == 3 && spans->size(0) == seqs && spans->size(2) == 2,
+                         "spans: int32 [seqs, S, 2], contiguous");
+        if (steer) check(steer->scalar_type() == at::kFloat && steer->is_contiguous() && steer->dim() == 2 && steer->size(0) == heads && steer->size(1) == q.size(2),
+                         "steer_vec: fp32 [Hq, D], contiguous");
+        if (given_out) check(given_out->scalar_type() == at::kBFloat16 && given_out->is_contiguous() && given_out->sizes() == q.sizes(), "out: bf16, contiguous, like q");
+        const hook_q4_cache q4 = q4_of(pages, q.size(2));
+        int64_t probed = 0;
+        if (mask && spans) {
+            const uint8_t* m = static_cast<const uint8_t*>(mask->data_ptr());
+            for (int64_t h = 0; h < heads; ++h) probed += m[h] != 0;
+        }
+        p.num_seqs = p.total_q = narrow(seqs);
+        p.num_q_heads = narrow(heads);
+        p.num_kv_heads = narrow(pages.size(1));
+        p.head_dim = narrow(q.size(2));
+        p.page_size = kPage;
+        p.num_blocks = narrow(pages.size(0));
+        p.max_blocks_per_seq = narrow(table.size(1));
+        p.num_spans = spans ? narrow(spans->size(1)) : 0;
+        p.q = q.data_ptr();
+        p.block_table = Call::pointer<int32_t>(&table);
+        p.seq_lens = Call::pointer<int32_t>(&lens);
+        p.spans = Call::pointer<int32_t>(spans);
+        p.steer_vec = Call::pointer<float>(steer);
+        p.head_mask = Call::pointer<uint8_t>(mask);
+        p.alpha = Call::pointer<float>(alpha);
+        at::Tensor out = given_out ? *given_out : c.make(q.sizes(), at::kBFloat16), mass, ws;
+        p.out = out.data_ptr();
+        if (probed > 0 && p.num_spans > 0) {
+            if (given_mass) {
+                check(given_mass->scalar_type() == at::kFloat && given_mass->is_contiguous() && given_mass->numel() == seqs * probed * p.num_spans,
+                      "span_mass: fp32 [seqs, probed heads, S], contiguous");
+                mass = *given_mass;
+            } else {
+                mass = c.make({seqs, probed, p.num_spans}, at::kFloat);
+            }
+            p.span_mass = Call::pointer<float>(&mass);
+        }
+        if (given_ws) {
+            check(given_ws->is_contiguous(), "workspace: contiguous");
+            p.workspace = given_ws->data_ptr();
+            p.workspace_bytes = given_ws->nbytes();
+        } else if (const size_t need = workspace_bytes(&p, 3)) {
+            ws = c.make({(int64_t)need}, at::kByte);
+            p.workspace = ws.data_ptr();
+            p.workspace_bytes = need;
+        }
+        const int rc = c.issue<decltype(hook_attn_decode_q4)>(&p, &q4);
+        if (rc != HOOK_ATTN_OK) return PyLong_FromLong(rc);
+        PyObject* both = PyTuple_New(2);
+        if (!both) return nullptr;
+        PyObject* x = THPVariable_Wrap(std::move(out));
+        PyObject* y = Py_None;
+        if (mass.defined()) y = THPVariable_Wrap(std::move(mass));
+        else Py_INCREF(y);
+        PyTuple_SET_ITEM(both, 0, x);
+        PyTuple_SET_ITEM(both, 1, y);
+        if (!x || !y) {
+            Py_DECREF(both);
+            return nullptr;
+        }
+        return both;
+    });
+}
+
+PyObject* sample_tokens(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        Call c(args, n, 4 + 8);
+        hook_sample_params p = {};
+        const at::Tensor& logits = c.tensor("logits [rows, vocab]", 2);
+        const int64_t rows = logits.size(0), vocab = logits.size(1);
+        const at::Tensor& uniform = c.list("uniform: fp32 [rows]", at::kFloat, rows);
+        const at::Tensor* heat = c.maybe_list("temperature: fp32 [rows]", at::kFloat, rows);
+        const at::Tensor* k = c.maybe_list("top_k: int32 [rows]", at::kInt, rows);
+        const at::Tensor *top = c.maybe_list("top_p: fp32 [rows]", at::kFloat, rows), *least = c.maybe_list("min_p: fp32 [rows]", at::kFloat, rows);
+        const at::Tensor* given = c.maybe_list("tokens: int32 [rows]", at::kInt, rows);
+        p.status = c.status();
+        check(vocab <= 1 || rows == 0 || logits.stride(1) == 1, "logits [rows, vocab]: neighbouring values of a row");
+        p.num_rows = narrow(rows);
+        p.vocab_size = narrow(vocab);
+        p.dtype = dtype_of(logits);
+        p.logits = logits.data_ptr();
+        p.logits_row_stride = rows > 1 ? logits.stride(0) : vocab;
+        p.uniform = Call::pointer<float>(&uniform);
+        p.temperature = Call::pointer<float>(heat);
+        p.top_k = Call::pointer<int32_t>(k);
+        p.top_p = Call::pointer<float>(top);
+        p.min_p = Call::pointer<float>(least);
+        at::Tensor tokens = given ? *given : c.make({rows}, at::kInt);
+        p.tokens = Call::pointer<int32_t>(&tokens);
+        return result(c.issue<decltype(hook_sample_tokens)>(&p), std::move(tokens));
+    });
+}
+
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CALL(rope_append), CALL(adjust_logits), CALL(cache_fork), CALL(cache_extend), CALL(cache_free), CALL(cache_compact),
-                         CALL(cache_copy_pages), {nullptr, nullptr, 0, nullptr}};
+                         CALL(cache_copy_pages), CALL(rope_append_q4), CALL(attn_decode_q4), CALL(cache_read_q4), CALL(cache_copy_pages_q4), CALL(sample_tokens), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the short calls of libhook_attn.so.", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 

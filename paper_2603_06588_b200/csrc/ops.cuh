@@ -53,7 +53,27 @@ struct CopyArgs {
     int64_t bs, ts, hs;
     const int32_t *pairs, *num_pairs;
     int32_t* status;
-    int32_t layers, num_blocks, Hkv, head_dim, max_pairs;
+    int32_t slabs;                         // arrays whose pages are copied: k[0], v[0], k[1], ...
+    int32_t tokens, num_blocks, Hkv, head_dim, max_pairs;   // a page: tokens x Hkv rows of head_dim elements
+};
+
+struct Q4ReadArgs {
+    const uint8_t* pages;
+    int64_t page_block, page_head;         // strides in bytes
+    __nv_bfloat16 *k_cache, *v_cache;
+    int64_t bs, ts, hs;                    // strides in elements
+    const int32_t *block_table, *seq_lens, *first, *to_table;
+    int32_t* status;
+    int32_t num_seqs, Hkv, num_blocks, max_blocks, max_keys, to_num_blocks, to_max_blocks;
+};
+
+struct SampleArgs {
+    const void* logits;
+    int64_t row;                           // in elements
+    const float *uniform, *temperature, *top_p, *min_p;
+    const int32_t* top_k;
+    int32_t *tokens, *status;
+    int32_t rows, vocab, slice;            // slice: tokens of a row that one CTA holds
 };
 
 // Exclusive prefix sum over the CTA; `total` is the sum.  `sh` holds 33 ints.

@@ -6,98 +6,16 @@
 // Angles: position * inv_freq / (2 pi) is brought to [-1/2, 1/2] turns in 64 bits.  The two products and the constant are rounded to 53
 // bits each, so a turn is off by at most 3 x 2^-53 of the turns: by 1.1e-7 at 2^31 rad.  In 32 bits a position of a million would be off by
 // 0.06 rad.  The rest is 32-bit, with one rounding to bf16 at the store.
-#include "common.cuh"
-#include "ops.cuh"
-
-#include <cuda_fp16.h>
+#include "rope_device.cuh"
 
 namespace hook_attn {
 
 namespace {
 
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_f32(float x) { return x; }
-
 constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = 8;       // rows per CTA at most: one warp looks each of them up
 template <int V>
 constexpr int kResident = V == 8 ? 6 : 8;      // CTAs on an SM: 40 registers with runs of eight (held to 32, 65536 rows take 443 us)
-
-// Where a row of the call goes.
-struct RowPlace {
-    int64_t slot;  // element offset of its slot in the cache (block and token part)
-    int pos;       // its position in the sequence
-    int state;     // kGood; kBroken: zero its queries; kBehind: behind the last sequence, leave it alone
-};
-enum { kGood = 0, kBroken = 1, kBehind = 2 };
-
-// A warp looks a row up: its sequence is the number of sequences that end at or before the row.  Of many, the lanes narrow them down to
-// 128 first (4096 rows of as many sequences: 20.8 us, and 33.6 us counting through all).
-__device__ __forceinline__ RowPlace find_row(const RopeArgs& a, int row)
-{
-    const int lane = threadIdx.x & 31;
-    RowPlace r = {0, 0, kBehind};
-    int seq = row, lo = row, n = 1;
-    if (row >= a.total_q) return r;
-    if (a.cu_q_lens) {
-        int from = 0, to = a.num_seqs;
-        while (to - from > 128) {
-            const int step = (to - from + 31) / 32, s = from + (lane + 1) * step;         // where the lane's part ends
-            from += step * __popc(__ballot_sync(0xffffffffu, s <= to && a.cu_q_lens[s] <= row));
-            to = min(from + step, to);
-        }
-        seq = 0;
-#pragma unroll 4
-        for (int s = from + lane; s < to; s += 32) seq += a.cu_q_lens[s + 1] <= row;
-        seq = from + __reduce_add_sync(0xffffffffu, seq);
-        if (seq >= a.num_seqs) return r;
-        lo = a.cu_q_lens[seq];
-        n = a.cu_q_lens[seq + 1] - lo;
-    }
-    r.state = kBroken;
-    const int L = a.seq_lens[seq], at = row - lo;
-    if (L <= 0 || L > a.max_keys || at < 0 || at >= n || n > L) return r;
-    r.pos = L - n + at;
-    const int page = a.block_table[(int64_t)seq * a.max_blocks + r.pos / kPage];
-    if (page < 0 || page >= a.num_blocks) return r;
-    r.slot = (int64_t)page * a.bs + (int64_t)(r.pos % kPage) * a.ts;
-    r.state = kGood;
-    return r;
-}
-
-// Cosine and sine of one pair at one position, times the factor.
-__device__ __forceinline__ float2 turn_of(const RopeArgs& a, int p, int pair)
-{
-    double turns = (double)p * (double)a.inv_freq[pair] * 0.15915494309189535;   // 1 / (2 pi)
-    turns -= rint(turns);
-    float s, c;
-    sincospif(2.0f * (float)turns, &s, &c);
-    return make_float2(c * a.factor, s * a.factor);
-}
-
-// V values in a row of memory: the widest accesses that V allows, then 32 bits each.
-template <typename T, int V>
-struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Pack {
-    T x[V];
-};
-
-template <typename T, int V>
-__device__ __forceinline__ void load(float (&x)[V], const T* p)
-{
-    const Pack<T, V> raw = *reinterpret_cast<const Pack<T, V>*>(p);
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = to_f32(raw.x[i]);
-}
-
-template <int V>
-__device__ __forceinline__ void store(__nv_bfloat16* p, const float (&x)[V])
-{
-    Pack<__nv_bfloat16, V> raw;
-#pragma unroll
-    for (int i = 0; i < V; ++i) raw.x[i] = __float2bfloat16(x[i]);
-    *reinterpret_cast<Pack<__nv_bfloat16, V>*>(p) = raw;
-}
 
 // A CTA takes a few rows.  An item is two runs of V elements of one head: V pairs that turn, or 2 V elements that are only
 // moved; the thread that reads them writes them, so the queries may be rotated in place.  Bound by HBM: every element is read
@@ -156,27 +74,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
         float x[V], y[V];
         load(x, src + e0);
         load(y, src + e1);
-        if (turns) {
-#pragma unroll
-            for (int m = 0; m < V; ++m) {
-                const float2 t = turn[r][j * V + m];
-                if (a.halves) {
-                    const float u = x[m], w = y[m];
-                    x[m] = u * t.x - w * t.y;
-                    y[m] = w * t.x + u * t.y;
-                } else if (V == 1) {
-                    const float u = x[0], w = y[0];
-                    x[0] = u * t.x - w * t.y;
-                    y[0] = w * t.x + u * t.y;
-                } else {                           // pair m: elements 2 m and 2 m + 1 of x, then of y
-                    float& u = m < V / 2 ? x[2 * m % V] : y[2 * m % V];
-                    float& w = m < V / 2 ? x[(2 * m + 1) % V] : y[(2 * m + 1) % V];
-                    const float u0 = u, w0 = w;
-                    u = u0 * t.x - w0 * t.y;
-                    w = w0 * t.x + u0 * t.y;
-                }
-            }
-        }
+        if (turns) turn_item<V>(x, y, &turn[r][j * V], a.halves);
         if (state == kBroken) {
 #pragma unroll
             for (int m = 0; m < V; ++m) x[m] = y[m] = 0.f;

@@ -4,9 +4,10 @@
 // little the others need through distributed shared memory.  All three filters keep the first tokens in the order of falling logits
 // (equal ones by index), so what stays is a least key K and how many of the tokens at K itself: tokens are never sorted.
 //
-// K is found by narrowing down: a histogram of the tokens' counts (top-k) or weights (top-p) over 1024 bins, the bin in which the wanted count
-// or weight is reached, a histogram of that bin, until a bin is one key: bins of equal width below the largest logit first, which spread
-// what a row holds evenly, then bins of the keys' bits.
+// K is found by narrowing down: a histogram of the tokens' counts (top-k) or weights (top-p) over bins of equal width below the largest logit,
+// then the few tokens of the bin in which the wanted count or weight is reached are listed, and each is held against all others; where they
+// are many, histograms of that bin by the keys' bits, until a bin is one key.  On the way each warp lists, in order, those of its tokens that may
+// stay, and what follows goes by the lists.
 //
 // Weights are exp((x - max) / T) in 64 bits, off by 2^-44 of them, and are summed as whole multiples of 2^-42: whatever the order, the
 // sums are the same, and a random number that falls next to a border is on the same side in every run and for every cluster size.
@@ -24,22 +25,18 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBins = 2 * kThreads;
+constexpr int kBins = kThreads;            // what is read from the other CTAs limits them: 64 KB took 2 us
 constexpr int kMostCtas = 8;               // of a cluster
-constexpr int kTable = 64;                 // 2^(i / 64)
+constexpr int kTable = 16;                 // 2^(i / 16): as wide as the banks of shared memory, so that lanes read any of it at once
+constexpr int kList = kThreads;            // tokens of a bin that are held against one another
+constexpr int kShare = kList / kMostCtas;  // of one CTA
+constexpr int kMayStay = 128;              // tokens in a warp's list
 constexpr double kUnit = 4398046511104.0;  // 2^42 units to a weight of 1
+constexpr float kLargest = 3.402823466e38f;
 
 __device__ __forceinline__ float as_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float as_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float as_f32(float x) { return x; }
-
-// A logit as the kernel holds it: NaN is -infinity, and there is one zero.
-template <typename T>
-__device__ __forceinline__ float logit(T raw)
-{
-    const float x = as_f32(raw) + 0.f;
-    return x == x ? x : -INFINITY;
-}
 
 // Integers in the order of the floats.
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -52,172 +49,351 @@ __device__ __forceinline__ float value_of(uint32_t key)
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
-struct SampleShared {
+struct alignas(16) SampleShared {
+    alignas(16) float may_stay[kWarps][kMayStay];      // the warps' lists: logits, and where they are
+    unsigned int place[kWarps][kMayStay];
     unsigned long long hist[2][kBins];     // levels take turns: a CTA may still read the one before
-    double table[kTable];
-    unsigned long long seg_sum[kMostCtas * kWarps];
-    unsigned int seg_ties[kMostCtas * kWarps];
-    float peer_max[kMostCtas], peer_sum[kMostCtas];
-    unsigned int peer_count[kMostCtas], peer_first[kMostCtas];
-    float warp_max[kWarps], warp_sum[kWarps];
-    unsigned int warp_count[kWarps];
-    unsigned long long warp_scan[kWarps];
-    unsigned long long found_before;
-    int found_bin, found_seg;
-    double found_target;
-    unsigned int found_ties;
-    unsigned long long found_total;
+    double table[kTable], wide_top;
+    float peer_max[kMostCtas * kWarps], peer_sum[kMostCtas * kWarps];
+    unsigned int peer_count[kMostCtas * kWarps];
+    unsigned long long peer_weight[kMostCtas], peer_ties[kMostCtas];
+    unsigned long long warp_scan[2][kWarps], draw[2][kWarps];
+    double per_logit, below;               // log2(e) / T; how far below the largest logit min_p's border lies
+    unsigned long long found_before, found_ties;
+    int found_bin, found_from, found_to, too_many;
+    unsigned int listed_count, listed[kShare], all[kList], all_count[kMostCtas], keys[kList], pick;
+    unsigned long long amounts[kList];
 };
 
-// exp2(y), y <= 0, in units of 2^-42: y is brought to a multiple of 1/64, whose power is in the table, and a rest r of at most 1/128, for which
-// four terms of the series of exp(r ln 2) leave out less than 4e-14.
-__device__ __forceinline__ unsigned long long weight_of(double y, const double* table)
+// 2^(i / 16)
+__device__ const double kPowers[kTable] = {
+    0x1.0000000000000p+0, 0x1.0b5586cf9890fp+0, 0x1.172b83c7d517bp+0, 0x1.2387a6e756238p+0,
+    0x1.306fe0a31b715p+0, 0x1.3dea64c123422p+0, 0x1.4bfdad5362a27p+0, 0x1.5ab07dd485429p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.7a11473eb0187p+0, 0x1.8ace5422aa0dbp+0, 0x1.9c49182a3f090p+0,
+    0x1.ae89f995ad3adp+0, 0x1.c199bdd85529cp+0, 0x1.d5818dcfba487p+0, 0x1.ea4afa2a490dap+0,
+};
+
+// A float as a double, by its bits: the conversion instruction takes four times as long as arithmetic, and a branch for the rare cases would keep
+// the chains of several logits from running side by side.  A zero becomes 2^-151, an infinity 2^128.
+__device__ __forceinline__ double widened(float x)
 {
-    if (!(y > -43.5)) return 0;
-    const double shifter = 6755399441055744.0 / kTable;                    // 1.5 * 2^52 / 64: adding it rounds to a multiple of 1/64
-    const double rounded = y + shifter;
-    const int n = __double2loint(rounded);                                 // 64 times the multiple
-    const double r = (y - (rounded - shifter)) * 0.6931471805599453;
-    double p = fma(r, 1.0 / 24, 1.0 / 6);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    p *= table[n & (kTable - 1)];
-    p = __hiloint2double(__double2hiint(p) + ((n >> 6) << 20), __double2loint(p));
-    const double fixed = p + 6755399441055744.0 / kUnit;                   // the mantissa's low bits are the multiple of 2^-42
-    return (unsigned long long)(__double_as_longlong(fixed) - __double_as_longlong(6755399441055744.0 / kUnit));
+    const bool tiny = fabsf(x) < 1.17549435e-38f;
+    const uint32_t b = __float_as_uint(tiny ? x * 16777216.f : x);
+    return __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + (tiny ? 0x36800000u : 0x38000000u))), (int)(b << 29));
 }
 
-// Sum over the CTA's threads of those before this one; `total` over all.
-__device__ __forceinline__ unsigned long long scan_cta(unsigned long long x, unsigned long long* warps, unsigned long long& total)
+// The weights of four logits in units of 2^-42: 2^y with y = (x - top) * per_logit.  y is brought to a multiple of 1/16, whose power is in the table,
+// and a rest r of at most 1/32, for which six terms of the series of exp(r ln 2) leave out less than 1e-15.  Next to an infinite logit
+// everything else weighs nothing.
+__device__ __forceinline__ void weights_of(unsigned long long (&w)[4], const float4& x4, float top, const SampleShared& sh)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned long long incl = x;
+    constexpr double kShifter = 6755399441055744.0 / kTable;               // 1.5 * 2^52 / 16: adding it rounds to a multiple of 1/16
+    constexpr double kFixed = 6755399441055744.0 / kUnit;                  // and this one to a multiple of 2^-42
+    const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const double y = x[e] == top ? 0.0 : (widened(x[e]) - sh.wide_top) * sh.per_logit;
+        const double rounded = y + kShifter;
+        const int n = __double2loint(rounded);                             // 16 times the multiple
+        const double r = (y - (rounded - kShifter)) * 0.6931471805599453;
+        double p = fma(r, 1.0 / 720, 1.0 / 120);
+        p = fma(p, r, 1.0 / 24);
+        p = fma(p, r, 1.0 / 6);
+        p = fma(p, r, 0.5);
+        p = fma(p, r, 1.0);
+        p = fma(p, r, 1.0);
+        p *= sh.table[n & (kTable - 1)];
+        p = __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p));
+        w[e] = y > -43.5 ? (unsigned long long)(__double_as_longlong(p + kFixed) - __double_as_longlong(kFixed)) : 0ull;
+    }
+}
+
+__device__ __forceinline__ unsigned long long weight_of(float x, float top, const SampleShared& sh)
+{
+    unsigned long long w[4];
+    weights_of(w, make_float4(x, top, top, top), top, sh);
+    return w[0];
+}
+
+// Adds to a 64-bit sum in shared memory by its words: there the hardware adds 32 bits at a time, and the carry is known from the old value.
+__device__ __forceinline__ void add_words(unsigned long long* sum, unsigned long long amount)
+{
+    unsigned int* words = reinterpret_cast<unsigned int*>(sum);
+    const unsigned int low = (unsigned int)amount, old = atomicAdd(words, low);
+    const unsigned int high = (unsigned int)(amount >> 32) + (old + low < low);
+    if (high) atomicAdd(words + 1, high);
+}
+
+// Sum over a warp's lanes, below 2^63: in limbs of 22 bits, which the reduction instruction adds (five exchanges of 64 bits took 450 cycles).
+__device__ __forceinline__ unsigned long long sum_warp(unsigned long long x)
+{
+    const unsigned int a = __reduce_add_sync(0xffffffffu, (unsigned int)x & 0x3fffffu), b = __reduce_add_sync(0xffffffffu, (unsigned int)(x >> 22) & 0x3fffffu);
+    const unsigned int c = __reduce_add_sync(0xffffffffu, (unsigned int)(x >> 44));
+    return ((unsigned long long)c << 44) + ((unsigned long long)b << 22) + a;
+}
+
+// Inclusive, over a warp.
+__device__ __forceinline__ unsigned long long scan_warp(unsigned long long x)
+{
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long y = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += y;
+        const unsigned long long y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
     }
-    __syncthreads();
-    if (lane == 31) warps[warp] = incl;
-    __syncthreads();
-    unsigned long long before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) before += warps[w];
-        total += warps[w];
-    }
-    return before + incl - x;
+    return x;
 }
 
+// Sum over the CTA's threads of those before this one, and over all.  `sums` is not in use by anything before the last barrier.
+__device__ __forceinline__ unsigned long long scan_cta(unsigned long long x, unsigned long long& total, unsigned long long (&sums)[kWarps])
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned long long incl = scan_warp(x);
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    const unsigned long long w = lane < kWarps ? sums[lane] : 0;
+    total = sum_warp(w);
+    return sum_warp(lane < warp ? w : 0) + incl - x;
+}
+
+// Four logits at a time of what a warp goes through: its part of the CTA's stretch, held as floats in shared memory or read again from
+// the row, or its list.
 template <typename T, bool HELD>
-struct Row {
+struct Walk {
+    const float4* held;
     const T* global;
-    const float* held;
-    int n;                                 // tokens of this CTA's stretch
-    __device__ __forceinline__ float at(int i) const { return HELD ? held[i] : logit(global[i]); }
+    int n;                                 // of the stretch, where it is not held
+    int from, to;
+    bool listed;
+    __device__ __forceinline__ float4 get(int v) const
+    {
+        if (HELD || listed) return held[v];
+        float x[4] = {};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = 4 * v + e < n ? as_f32(global[4 * v + e]) + 0.f : -INFINITY;
+            if (x[e] != x[e]) x[e] = -INFINITY;
+        }
+        return make_float4(x[0], x[1], x[2], x[3]);
+    }
 };
 
-// Bins of equal width below the largest logit; what lies beyond them is in the last.
+// Bins of equal width below the largest logit: (top - x) * scale to the nearest whole number, which an addition of 2^23 leaves in the low bits;
+// what lies beyond them (and an infinity's difference to itself) is in the last.
 __device__ __forceinline__ int linear_bin(float x, float top, float scale)
 {
-    const float f = (top - x) * scale;     // 0 for x = top, also where both are infinite (scale 0 then, and NaN below compares false)
-    return f < (float)(kBins - 1) ? (int)f : (f == f ? kBins - 1 : 0);
+    return (int)min(__float_as_uint(fmaf(top - x, scale, 8388608.f)) - 0x4b000000u, (uint32_t)(kBins - 1));
 }
 
-// The key at which the wanted number or weight of eligible tokens is reached, and how much lies above it.  WEIGHTS: `want` is the share of the
-// total; otherwise it is a number of tokens.  Tokens at `tie_key` count `tie_count` times in all, in no token's own turn.  All CTAs of
-// the cluster come to the same result.  `level` says which histogram is free.
+// The key at which the wanted number or weight of the logits from `floor` on is reached, and how much lies above it.  weighted: `want` is the share
+// of the total; otherwise it is a number of tokens.  Tokens at `tie_key`, below floor, count `tie_amount` in all.  All CTAs of the cluster
+// come to the same result.  `level` says which histogram is free.  Warps without a list get one of what is in play, from `base` on, and not
+// below the key.
 struct Reached {
     uint32_t key;
     unsigned long long above, total;       // above: of the tokens with larger keys
     bool all;                              // counts: there are no more than wanted
 };
 
-template <bool WEIGHTS, typename R, typename Ok, typename Weight>
-__device__ Reached reach(const R& row, SampleShared& sh, cg::cluster_group& cluster, int& level, double want, float top, float scale,
-                         Ok eligible, Weight weight, uint32_t tie_key, unsigned long long tie_amount)
+template <typename R>
+__device__ __forceinline__ Reached reach(const bool weighted, R& row, SampleShared& sh, int& level, double want, float top, float scale, float base,
+                                      float floor, uint32_t tie_key, unsigned long long tie_amount)
 {
-    const int ctas = (int)cluster.num_blocks();
-    const bool first_cta = cluster.block_rank() == 0;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Reached out = {0, 0, 0, false};
     int linear = -1, shift = 0;
     uint32_t key_lo = 0, key_hi = 0;
     double goal = want;
+#pragma unroll 1
     for (int pass = 0;; ++pass) {
         unsigned long long* hist = sh.hist[level & 1];
         ++level;
-        for (int i = threadIdx.x; i < kBins; i += kThreads) hist[i] = 0;
+        hist[threadIdx.x] = 0;
+        if (threadIdx.x == 0) sh.listed_count = 0;
         __syncthreads();
-        auto bin_of = [&](float x, uint32_t key) {
+        auto bin_of = [&](float x) {
             const int l = linear_bin(x, top, scale);
             if (pass == 0) return l;
+            const uint32_t key = key_of(x);
             return l == linear && key >= key_lo && key <= key_hi ? (int)((key_hi - key) >> shift) : -1;
         };
         unsigned long long rest = 0;       // of the last linear bin: most of a row, added once
-        for (int i = threadIdx.x; i < row.n; i += kThreads) {
-            const float x = row.at(i);
-            const uint32_t key = key_of(x);
-            if (!eligible(x, key)) continue;
-            const int b = bin_of(x, key);
-            if (b < 0) continue;
-            const unsigned long long amount = WEIGHTS ? weight(x) : 1ull;
-            if (pass == 0 && b == kBins - 1) rest += amount;
-            else if (amount) atomicAdd(&hist[b], amount);
+#pragma unroll 2
+        for (int v = row.from + lane; v < row.to; v += 32) {
+            const float4 x4 = row.get(v);
+            if (!(fmaxf(fmaxf(x4.x, x4.y), fmaxf(x4.z, x4.w)) >= floor)) continue;
+            unsigned long long w[4] = {1, 1, 1, 1};
+            if (weighted) weights_of(w, x4, top, sh);
+            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+            int bin[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                bin[e] = x[e] >= floor ? bin_of(x[e]) : -1;
+                if (pass == 0 && bin[e] == kBins - 1) {
+                    rest += w[e];
+                    bin[e] = -1;
+                }
+            }
+            unsigned int old[4];           // the four side by side: what they wait for is the old values
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (bin[e] >= 0) old[e] = atomicAdd(reinterpret_cast<unsigned int*>(&hist[bin[e]]), (unsigned int)w[e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!weighted || bin[e] < 0) continue;
+                const unsigned int high = (unsigned int)(w[e] >> 32) + (old[e] + (unsigned int)w[e] < old[e]);
+                if (high) atomicAdd(reinterpret_cast<unsigned int*>(&hist[bin[e]]) + 1, high);
+            }
         }
-        if (rest) atomicAdd(&hist[kBins - 1], rest);
-        if (WEIGHTS && first_cta && threadIdx.x == 0 && tie_amount) {
-            const int b = bin_of(value_of(tie_key), tie_key);
-            if (b >= 0) atomicAdd(&hist[b], tie_amount);
+        if (__any_sync(0xffffffffu, rest != 0)) {
+            rest = sum_warp(rest);
+            if (lane == 0) add_words(&hist[kBins - 1], rest);
+        }
+        if (rank == 0 && threadIdx.x == 0 && tie_amount) {
+            const int b = bin_of(value_of(tie_key));
+            if (b >= 0) add_words(&hist[b], tie_amount);
         }
         cluster.sync();
-        unsigned long long mine[2] = {0, 0};
-        for (int c = 0; c < ctas; ++c) {
-            const unsigned long long* other = cluster.map_shared_rank(hist, c);
-            mine[0] += other[2 * threadIdx.x];
-            mine[1] += other[2 * threadIdx.x + 1];
-        }
+        unsigned long long mine = 0, theirs[kMostCtas];        // all under way at once
+#pragma unroll
+        for (int c = 0; c < kMostCtas; ++c) theirs[c] = c < ctas ? cluster.map_shared_rank(hist, c)[threadIdx.x] : 0;
+#pragma unroll
+        for (int c = 0; c < kMostCtas; ++c) mine += theirs[c];
         unsigned long long total;
-        const unsigned long long before = scan_cta(mine[0] + mine[1], sh.warp_scan, total) + out.above;
+        const unsigned long long before = scan_cta(mine, total, sh.warp_scan[level & 1]) + out.above;
         if (pass == 0) {
             out.total = total;
-            if (WEIGHTS) {
+            if (weighted) {
                 goal = want * (double)total;
             } else if ((double)total <= want) {
                 out.all = true;
                 return out;
             }
-            if (threadIdx.x == 0) sh.found_bin = -1;
-            __syncthreads();
         }
         // the first bin with which the goal is reached
-        const unsigned long long after0 = before + mine[0], after1 = after0 + mine[1];
-        const bool start = threadIdx.x == 0;
-        if ((double)after0 >= goal && ((double)before < goal || start)) {
-            sh.found_bin = 2 * threadIdx.x;
+        if ((double)(before + mine) >= goal && ((double)before < goal || threadIdx.x == 0)) {
+            sh.found_bin = threadIdx.x;
             sh.found_before = before;
-        } else if ((double)after1 >= goal && (double)after0 < goal) {
-            sh.found_bin = 2 * threadIdx.x + 1;
-            sh.found_before = after0;
         }
+        if (threadIdx.x == 0) sh.pick = 0xffffffffu;
         __syncthreads();
         const int b = sh.found_bin;
         out.above = sh.found_before;
-        if (pass == 0) {
-            linear = b;
-            key_hi = key_of(top);
-            key_lo = key_of(-3.402823466e38f);
-            if (scale > 0.f) {             // what rounds into bin b, with a margin for the rounding of (top - x) * scale
-                key_hi = min(key_hi, key_of(__double2float_ru((double)top - b * (1 - 0x1p-22) / (double)scale)));
-                if (b < kBins - 1) key_lo = max(key_lo, key_of(__double2float_rd((double)top - (b + 1) * (1 + 0x1p-22) / (double)scale)));
-            }
-        } else {
+        if (pass > 0) {
             key_hi -= (uint32_t)b << shift;
             if (key_hi - key_lo >= 1u << shift) key_lo = key_hi - ((1u << shift) - 1);
             if (shift == 0) {
                 out.key = key_hi;
                 return out;
+            }
+        } else {
+            linear = b;
+            // The tokens of bin b, for all CTAs; and for the warp's own list those up to it: none lies below `near`, with a margin for what rounds into b.
+            const float near = fmaxf(base, scale > 0.f && b < kBins - 1 ? top - (b + 0.51f) / scale - fabsf(top) * 4e-7f : -kLargest);
+            int n = 0;
+#pragma unroll 1
+            for (int v0 = row.from; v0 < row.to; v0 += 32) {
+                const int v = v0 + lane;
+                const float4 x4 = v < row.to ? row.get(v) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                if (!__any_sync(0xffffffffu, fmaxf(fmaxf(x4.x, x4.y), fmaxf(x4.z, x4.w)) >= near)) continue;
+                const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+                uint32_t mine_in = 0, who[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int l = x[e] >= near ? linear_bin(x[e], top, scale) : kBins;
+                    if (l == b && x[e] >= floor) {
+                        const unsigned int at = atomicAdd(&sh.listed_count, 1u);
+                        if (at < kShare) sh.listed[at] = key_of(x[e]);
+                    }
+                    mine_in |= (uint32_t)(l <= b) << e;
+                    who[e] = __ballot_sync(0xffffffffu, l <= b);
+                }
+                if (row.listed) continue;
+                const uint32_t before_me = (1u << lane) - 1;
+                int at = n + __popc(who[0] & before_me) + __popc(who[1] & before_me) + __popc(who[2] & before_me) + __popc(who[3] & before_me);
+                n += __popc(who[0]) + __popc(who[1]) + __popc(who[2]) + __popc(who[3]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (mine_in >> e & 1) {
+                        if (at < kMayStay) {
+                            sh.may_stay[warp][at] = x[e];
+                            sh.place[warp][at] = 4 * v + e;
+                        }
+                        ++at;
+                    }
+            }
+            if (!row.listed && n <= kMayStay) {
+                if (lane < (-n & 3)) sh.may_stay[warp][n + lane] = -INFINITY;
+                row.held = reinterpret_cast<const float4*>(sh.may_stay[warp]);
+                row.from = 0;
+                row.to = (n + 3) / 4;
+                row.listed = true;
+            }
+            __syncthreads();
+            if ((int)threadIdx.x / kShare < ctas) {        // a group of threads for every CTA
+                SampleShared* other = cluster.map_shared_rank(&sh, threadIdx.x / kShare);
+                const int j = threadIdx.x % kShare;
+                if (j < (int)sh.listed_count) other->all[rank * kShare + j] = sh.listed[j];
+                if (j == 0) other->all_count[rank] = sh.listed_count;
+            }
+            cluster.sync();
+            bool few = true;
+#pragma unroll
+            for (int c = 0; c < kMostCtas; ++c) few &= c >= ctas || sh.all_count[c] <= kShare;
+            if (few) {
+                // each is held against all, by as many threads as there are for it
+                const int from_cta = threadIdx.x / kShare, from_at = threadIdx.x % kShare;
+                int n = 0, at = 0;
+#pragma unroll
+                for (int c = 0; c < kMostCtas; ++c) {
+                    if (c == from_cta) at = n + from_at;
+                    if (c < ctas) n += sh.all_count[c];
+                }
+                if (from_cta < ctas && from_at < (int)sh.all_count[from_cta]) {
+                    sh.keys[at] = sh.all[threadIdx.x];
+                    sh.amounts[at] = weighted ? weight_of(value_of(sh.all[threadIdx.x]), top, sh) : 1;
+                }
+                __syncthreads();
+                const int split = n <= kThreads / 4 ? 4 : 1, mine_at = threadIdx.x / split;
+                const bool live = mine_at < n;
+                const uint32_t key = live ? sh.keys[mine_at] : 0;                  // no token in play has key 0
+                unsigned long long larger = 0, whole = 0;
+                if (live)
+#pragma unroll 4
+                    for (int j = threadIdx.x % split; j < n; j += split) {
+                        const unsigned long long amount = sh.amounts[j];
+                        whole += amount;
+                        larger += sh.keys[j] > key ? amount : 0;
+                    }
+                if (split > 1)
+#pragma unroll
+                    for (int d = 1; d < 4; d <<= 1) {
+                        whole += __shfl_xor_sync(0xffffffffu, whole, d);
+                        larger += __shfl_xor_sync(0xffffffffu, larger, d);
+                    }
+                if (live && ((double)(out.above + larger) < goal || key == key_of(top))) atomicMin(&sh.pick, key);
+                __syncthreads();
+                const uint32_t pick = sh.pick;
+                const bool none = pick == 0xffffffffu;                             // the bin holds nothing but those that have no turn
+                if (none ? threadIdx.x == 0 : live && key == pick) {
+                    const bool ties = tie_amount && (double)(out.above + whole) < goal;                // or the goal lies among them
+                    sh.found_before = out.above + (ties ? whole : larger);
+                    sh.found_bin = none || ties;
+                }
+                __syncthreads();
+                out.key = sh.found_bin ? tie_key : pick;
+                out.above = sh.found_before;
+                return out;
+            }
+        }
+        if (pass == 0) {                   // what rounds into bin b, with a margin for the rounding of top - x
+            key_hi = key_of(top);
+            key_lo = key_of(-kLargest);
+            if (scale > 0.f) {
+                const double width = 1.0 / (double)scale;
+                if (b > 0) key_hi = min(key_hi, key_of(__double2float_ru((double)top - (b - 0.5) * (1 - 0x1p-22) * width)));
+                if (b < kBins - 1) key_lo = max(key_lo, key_of(__double2float_rd((double)top - (b + 0.5) * (1 + 0x1p-22) * width)));
             }
         }
         shift = 0;
@@ -226,10 +402,10 @@ __device__ Reached reach(const R& row, SampleShared& sh, cg::cluster_group& clus
 }
 
 template <typename T, bool HELD>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a)
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 {
     __shared__ SampleShared sh;
-    extern __shared__ __align__(16) float stretch[];
+    extern __shared__ __align__(16) float4 stretch[];
     cg::cluster_group cluster = cg::this_cluster();
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), r = blockIdx.x / ctas;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -238,77 +414,96 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a)
     const float share = a.top_p ? a.top_p[r] : 1.f, least = a.min_p ? a.min_p[r] : 0.f;
     const int k = a.top_k ? a.top_k[r] : 0;
     const bool valid = u >= 0.f && u < 1.f && heat >= 0.f && heat < INFINITY && share >= 0.f && least >= 0.f && least <= 1.f;
-    if (!valid) {                          // of the whole cluster
-        if (rank == 0 && threadIdx.x == 0) {
-            a.tokens[r] = -1;
-            report(a.status, HOOK_ATTN_ERR_INVALID_ARG);
-        }
-        return;
+    const bool greedy = heat == 0.f;
+    if (threadIdx.x == kThreads - 32) {    // while the others fetch
+        sh.per_logit = greedy ? 0.0 : 1.4426950408889634 / (double)heat;
+        sh.below = least > 0.f && !greedy ? log2((double)least) / sh.per_logit : -INFINITY;
     }
-
     // ---- the stretch, its largest logit, the sum and number of the finite ones ----
-    const int start = rank * a.slice;
-    Row<T, HELD> row;
-    row.n = max(0, min(a.slice, a.vocab - start));
-    row.global = static_cast<const T*>(a.logits) + (int64_t)r * a.row + start;
+    const int start = rank * a.slice, n = max(0, min(a.slice, a.vocab - start));
+    const T* const global = static_cast<const T*>(a.logits) + (int64_t)r * a.row + start;
+    // Read in vectors of 16 bytes where they are aligned; element i is then held at place i + lead, the first vector's alignment.
+    constexpr int E = 16 / sizeof(T);
+    const int lead = HELD ? (int)(reinterpret_cast<uintptr_t>(global) & 15) / (int)sizeof(T) : 0;
+    Walk<T, HELD> row;
+    row.held = stretch;
+    row.global = global;
+    row.n = n;
+    row.listed = false;
+    {
+        const int fours = (lead + n + 3) / 4, per = (fours + kWarps - 1) / kWarps;
+        row.from = min(warp * per, fours);
+        row.to = min(row.from + per, fours);
+    }
     float top = -INFINITY, sum = 0.f;
     unsigned int count = 0;
-    auto take = [&](float x) {
+    auto take = [&](float x) {             // NaN is -infinity, and there is one zero
+        x = x == x ? x + 0.f : -INFINITY;
         top = fmaxf(top, x);
-        if (fabsf(x) < INFINITY) {
-            sum += x;
-            ++count;
-        }
+        const bool finite = fabsf(x) < INFINITY;
+        sum += finite ? x : 0.f;
+        count += finite;
+        return x;
     };
-    constexpr int E = 16 / sizeof(T);
-    const int head = row.n > 0 ? min(row.n, (int)((16 - (reinterpret_cast<uintptr_t>(row.global) & 15)) & 15) / (int)sizeof(T)) : 0;
-    float* held = stretch + ((4 - head) & 3);          // where the aligned part starts on 16 bytes
-    row.held = held;
-    const int vectors = (row.n - head) / E, tail = head + vectors * E;
-    for (int i = threadIdx.x; i < vectors; i += kThreads) {
-        const uint4 raw = reinterpret_cast<const uint4*>(row.global + head)[i];
-        const T* p = reinterpret_cast<const T*>(&raw);
-        float x[E];
+    if constexpr (HELD) {
+        const int vectors = (lead + n + E - 1) / E;
+        constexpr int BATCH = 4;           // vectors of a thread under way
+        for (int v0 = threadIdx.x; v0 < vectors; v0 += BATCH * kThreads) {
+            uint4 raw[BATCH];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            x[e] = logit(p[e]);
-            take(x[e]);
+            for (int j = 0; j < BATCH; ++j) {
+                const int v = v0 + j * kThreads, i0 = v * E - lead;
+                if (v < vectors && i0 >= 0 && i0 + E <= n) raw[j] = *reinterpret_cast<const uint4*>(global + i0);
+            }
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int v = v0 + j * kThreads, i0 = v * E - lead;
+                if (v >= vectors) break;
+                T* p = reinterpret_cast<T*>(&raw[j]);
+                if (i0 < 0 || i0 + E > n)
+                    for (int e = 0; e < E; ++e) p[e] = i0 + e >= 0 && i0 + e < n ? global[i0 + e] : T(-INFINITY);
+#pragma unroll
+                for (int e = 0; e < E; e += 4)
+                    stretch[v * (E / 4) + e / 4] = make_float4(take(as_f32(p[e])), take(as_f32(p[e + 1])), take(as_f32(p[e + 2])), take(as_f32(p[e + 3])));
+            }
         }
-        if (HELD) {
-#pragma unroll
-            for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(held + head + i * E + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+    } else {
+        for (int v = row.from + lane; v < row.to; v += 32) {
+            const float4 x = row.get(v);
+            take(x.x); take(x.y); take(x.z); take(x.w);
         }
     }
-    for (int i = threadIdx.x; i < head + row.n - tail; i += kThreads) {
-        const int at = i < head ? i : tail + i - head;
-        const float x = logit(row.global[at]);
-        take(x);
-        if (HELD) held[at] = x;
-    }
-    for (int i = threadIdx.x; i < kTable; i += kThreads) sh.table[i] = exp2((double)i / kTable);
+    if (threadIdx.x < kTable) sh.table[threadIdx.x] = kPowers[threadIdx.x];
+    top = value_of(__reduce_max_sync(0xffffffffu, key_of(top)));
+    count = __reduce_add_sync(0xffffffffu, count);
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        count += __shfl_xor_sync(0xffffffffu, count, d);
-    }
-    if (lane == 0) { sh.warp_max[warp] = top; sh.warp_sum[warp] = sum; sh.warp_count[warp] = count; }
-    __syncthreads();
-    if ((int)threadIdx.x < ctas) {
-        float m = -INFINITY, s = 0.f;
-        unsigned int c = 0;
-        for (int w = 0; w < kWarps; ++w) { m = fmaxf(m, sh.warp_max[w]); s += sh.warp_sum[w]; c += sh.warp_count[w]; }
-        SampleShared* other = cluster.map_shared_rank(&sh, threadIdx.x);
-        other->peer_max[rank] = m;
-        other->peer_sum[rank] = s;
-        other->peer_count[rank] = c;
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane < ctas) {                     // of this warp, for every CTA
+        SampleShared* other = cluster.map_shared_rank(&sh, lane);
+        const int at = rank * kWarps + warp;
+        other->peer_max[at] = top;
+        other->peer_sum[at] = sum;
+        other->peer_count[at] = count;
     }
     cluster.sync();
-    top = -INFINITY;
-    sum = 0.f;
-    count = 0;
-    for (int c = 0; c < ctas; ++c) { top = fmaxf(top, sh.peer_max[c]); sum += sh.peer_sum[c]; count += sh.peer_count[c]; }
-    if (top == -INFINITY) {
+    {                                      // a lane takes four warps; every warp comes to the same
+        uint32_t most = 0;
+        sum = 0.f;
+        count = 0;
+#pragma unroll
+        for (int j = 0; j < kMostCtas * kWarps / 32; ++j) {
+            const int at = 32 * j + lane;
+            if (at >= ctas * kWarps) break;
+            most = max(most, key_of(sh.peer_max[at]));
+            sum += sh.peer_sum[at];
+            count += sh.peer_count[at];
+        }
+        top = value_of(__reduce_max_sync(0xffffffffu, most));
+        count = __reduce_add_sync(0xffffffffu, count);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    }
+    if (!valid || top == -INFINITY) {      // of the whole cluster
         if (rank == 0 && threadIdx.x == 0) {
             a.tokens[r] = -1;
             report(a.status, HOOK_ATTN_ERR_INVALID_ARG);
@@ -317,144 +512,154 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a)
     }
 
     // ---- what stays: larger keys than least_key, and the first `ties` tokens at it ----
-    const bool greedy = heat == 0.f;
     uint32_t least_key = greedy ? key_of(top) : 0;
     unsigned long long ties = greedy ? 1 : 0;
-    const double per_logit = greedy ? 0.0 : 1.4426950408889634 / (double)heat;
-    const float cutoff = least > 0.f && !greedy ? __double2float_ru((double)top + log2((double)least) / per_logit) : -INFINITY;
-    // next to an infinite logit everything else weighs nothing
-    auto weight = [&](float x) { return x == top ? (unsigned long long)kUnit : weight_of(((double)x - (double)top) * per_logit, sh.table); };
+    // what is in play: from here on
+    float floor = sh.below > -INFINITY ? fmaxf(__double2float_ru((double)top + sh.below), -kLargest) : -kLargest;
+    if (threadIdx.x == 0) sh.wide_top = (double)top;
+    __syncthreads();
     int level = 0;
-    auto in_play = [&](float x, uint32_t) { return x > -INFINITY && x >= cutoff; };
     const float spread = count > 0 ? top - sum / (float)count : 0.f;
-    if (!greedy && k > 0 && k < a.vocab) {
-        const float scale = spread > 0.f && spread < INFINITY ? (float)(kBins - 1) / spread : 0.f;
-        const Reached at = reach<false>(row, sh, cluster, level, (double)k, top, isfinite(scale) ? scale : 0.f, in_play, weight, 0, 0);
-        if (!at.all) {
-            least_key = at.key;
-            ties = k - at.above;
-        }
-    }
-    unsigned long long tie_weight = least_key ? weight(value_of(least_key)) : 0;
-    if (!greedy && share < 1.f) {
-        // beyond 2^-43 of the largest weight there is nothing
-        const float wide = fminf(spread, (float)(44.0 / per_logit));
-        const float scale = wide > 0.f && wide < INFINITY ? (float)(kBins - 1) / wide : 0.f;
-        const uint32_t bound = least_key;
-        const Reached at = reach<true>(row, sh, cluster, level, (double)share, top, isfinite(scale) ? scale : 0.f,
-                                       [&](float x, uint32_t key) { return key > bound && in_play(x, key); }, weight, bound, ties * tie_weight);
-        const double goal = (double)share * (double)at.total;
-        const unsigned long long each = at.key == least_key ? tie_weight : weight(value_of(at.key));
-        unsigned long long n = 1;          // those before which less than the goal lies
-        if (each > 0) {
-            const double more = (goal - (double)at.above) / (double)each;
-            n = more > 1.0 ? (unsigned long long)more : 1;
-            while ((double)(at.above + n * each) < goal) ++n;
-            while (n > 1 && (double)(at.above + (n - 1) * each) >= goal) --n;
-        }
-        ties = at.key == least_key ? min(ties, n) : n;
-        least_key = at.key;
-        tie_weight = each;
-    }
-
-    // ---- the draw: weights of stretches of the stretch, in the order of the indices ----
-    const int per = ((row.n + kWarps - 1) / kWarps + 31) / 32 * 32, from = min(warp * per, row.n), to = min(from + per, row.n);
-    unsigned long long mine = 0;
-    unsigned int tied = 0;
-    for (int i = from + lane; i < to; i += 32) {
-        const float x = row.at(i);
-        const uint32_t key = key_of(x);
-        if (key < least_key || !in_play(x, key)) continue;
-        if (least_key && key == least_key) ++tied;
-        else mine += weight(x);
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        mine += __shfl_xor_sync(0xffffffffu, mine, d);
-        tied += __shfl_xor_sync(0xffffffffu, tied, d);
-    }
-    if (lane < ctas) {
-        SampleShared* other = cluster.map_shared_rank(&sh, lane);
-        other->seg_sum[rank * kWarps + warp] = mine;
-        other->seg_ties[rank * kWarps + warp] = tied;
-    }
-    cluster.sync();
-    if (warp == 0) {                       // a lane takes a run of stretches
-        const int segs = ctas * kWarps, each = (segs + 31) / 32;
-        unsigned int t = 0;
-        for (int j = 0; j < each; ++j)
-            if (lane * each + j < segs) t += sh.seg_ties[lane * each + j];
-        unsigned int t_incl = t;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const unsigned int y = __shfl_up_sync(0xffffffffu, t_incl, d);
-            if (lane >= d) t_incl += y;
-        }
-        auto part = [&](int s, unsigned long long t_before) {
-            const unsigned long long left = ties > t_before ? ties - t_before : 0;
-            return sh.seg_sum[s] + min(left, (unsigned long long)sh.seg_ties[s]) * tie_weight;
-        };
-        unsigned long long w = 0, tb = t_incl - t;
-        for (int j = 0; j < each; ++j)
-            if (lane * each + j < segs) { w += part(lane * each + j, tb); tb += sh.seg_ties[lane * each + j]; }
-        unsigned long long w_incl = w;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const unsigned long long y = __shfl_up_sync(0xffffffffu, w_incl, d);
-            if (lane >= d) w_incl += y;
-        }
-        const unsigned long long total = __shfl_sync(0xffffffffu, w_incl, 31);
-        // the first weight that exceeds u of the total; rounded up to it, the last one
-        const double want = fmin((double)u * (double)total, (double)total - 1.0);
-        const unsigned int reached = __ballot_sync(0xffffffffu, (double)w_incl > want);
-        if (lane == __ffs(reached) - 1) {
-            unsigned long long before = w_incl - w;
-            tb = t_incl - t;
-            for (int j = 0; j < each; ++j) {
-                const int s = lane * each + j;
-                if (s >= segs) break;
-                const unsigned long long p = part(s, tb);
-                if ((double)(before + p) > want) {
-                    sh.found_seg = s;
-                    sh.found_before = before;
-                    sh.found_ties = (unsigned int)tb;
-                    sh.found_target = want;
-                    break;
-                }
-                before += p;
-                tb += sh.seg_ties[s];
+    auto scale_of = [&](float width) {
+        const float scale = width > 0.f && width < INFINITY ? (float)(kBins - 1) / width : 0.f;
+        return isfinite(scale) ? scale : 0.f;
+    };
+    unsigned long long tie_weight = (unsigned long long)kUnit;
+    // Top-k, then top-p among what it left: one loop, so that the code is there once (a small call waits for its instructions more than for anything else).
+#pragma unroll 1
+    for (int stage = 0; stage < 2; ++stage) {
+        const bool weighted = stage > 0;
+        if (greedy || !(weighted ? share < 1.f : k > 0 && k < a.vocab)) continue;
+        // beyond 2^-43 of the largest weight there is nothing; what follows infinity is a NaN, and nothing is from there on
+        const float width = weighted ? fminf(spread, 30.5f * heat) : spread, above = weighted && least_key ? value_of(least_key + 1) : floor;
+        const Reached at = reach(weighted, row, sh, level, weighted ? (double)share : (double)k, top, scale_of(width), floor, above, least_key,
+                                 weighted ? ties * tie_weight : 0);
+        if (at.all) continue;
+        unsigned long long n = k - at.above;
+        if (weighted) {                    // those before which less than the goal lies
+            const double goal = (double)share * (double)at.total;
+            n = 1;
+            const unsigned long long each = at.key == least_key ? tie_weight : weight_of(value_of(at.key), top, sh);
+            if (each > 0) {
+                const double more = (goal - (double)at.above) / (double)each;
+                n = more > 1.0 ? (unsigned long long)more : 1;
+                while ((double)(at.above + n * each) < goal) ++n;
+                while (n > 1 && (double)(at.above + (n - 1) * each) >= goal) --n;
             }
+            if (at.key == least_key) n = min(ties, n);
         }
+        ties = n;
+        least_key = at.key;
+        tie_weight = weight_of(value_of(least_key), top, sh);
+    }
+    if (least_key) floor = fmaxf(floor, value_of(least_key));
+
+    // ---- the draw, in the order of the indices: weights of the warps' stretches or lists, then of their parts ----
+    const float least_value = least_key ? value_of(least_key) : -INFINITY;
+    auto part_of = [&](int v, const Walk<T, HELD>& of, unsigned long long& w, unsigned long long& t) {     // weights above least_key, and how many are at it
+        const float4 x4 = of.get(v);
+        if (!(fmaxf(fmaxf(x4.x, x4.y), fmaxf(x4.z, x4.w)) >= floor)) return;
+        unsigned long long each[4];
+        weights_of(each, x4, top, sh);
+        const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool tie = x[e] == least_value && x[e] >= floor;
+            t += tie;
+            w += x[e] >= floor && !tie ? each[e] : 0;
+        }
+    };
+    unsigned long long part[2] = {0, 0};   // weight, ties
+#pragma unroll 2
+    for (int v = row.from + lane; v < row.to; v += 32) part_of(v, row, part[0], part[1]);
+    const unsigned long long lane_part[2] = {part[0], part[1]};
+    part[0] = sum_warp(part[0]);
+    part[1] = sum_warp(part[1]);
+    if (lane == 0) {
+        sh.draw[0][warp] = part[0];
+        sh.draw[1][warp] = part[1];
     }
     __syncthreads();
-    if (sh.found_seg != rank * kWarps + warp) return;
-    unsigned long long before = sh.found_before, t_before = sh.found_ties;
-    for (int i0 = from; i0 < to; i0 += 32) {
-        const int i = i0 + lane;
-        const float x = i < to ? row.at(i) : -INFINITY;
-        const uint32_t key = key_of(x);
-        const bool stays = key >= least_key && in_play(x, key), tie = stays && least_key && key == least_key;
-        const unsigned int all_ties = __ballot_sync(0xffffffffu, tie);
-        unsigned long long w = 0;
-        if (tie) w = t_before + __popc(all_ties & ((1u << lane) - 1)) < ties ? tie_weight : 0;
-        else if (stays) w = weight(x);
-        unsigned long long incl = w;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const unsigned long long y = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += y;
-        }
-        const unsigned int reached = __ballot_sync(0xffffffffu, w > 0 && (double)(before + incl) > sh.found_target);
-        if (reached) {
-            if (lane == __ffs(reached) - 1) a.tokens[r] = start + i;
-            return;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
-        t_before += __popc(all_ties);
+    // of the warps, in lanes
+    const unsigned long long each_warp = lane < kWarps ? sh.draw[0][lane] : 0, each_ties = lane < kWarps ? sh.draw[1][lane] : 0;
+    const unsigned long long cta_weight = sum_warp(each_warp), cta_ties = sum_warp(each_ties);
+    if ((int)threadIdx.x < ctas) {
+        SampleShared* other = cluster.map_shared_rank(&sh, threadIdx.x);
+        other->peer_weight[rank] = cta_weight;
+        other->peer_ties[rank] = cta_ties;
     }
+    cluster.sync();
+    // the first weight that exceeds u of the total; rounded up to it, the last one
+    auto of_ties = [&](unsigned long long before, unsigned long long n) { return min(ties > before ? ties - before : 0ull, n) * tie_weight; };
+    unsigned long long total = 0, seen = 0, before = 0, t_before = 0;
+    for (int c = 0; c < ctas; ++c) {
+        if (c == rank) { before = total; t_before = seen; }
+        total += sh.peer_weight[c] + of_ties(seen, sh.peer_ties[c]);
+        seen += sh.peer_ties[c];
+    }
+    const double want = fmin((double)u * (double)total, (double)total - 1.0);
+    if ((double)before > want || (double)(before + cta_weight + of_ties(t_before, cta_ties)) <= want) return;
+    // the warp: all know which
+    const unsigned long long warps[2] = {scan_warp(each_warp), scan_warp(each_ties)};
+    const unsigned int up_to = __ballot_sync(0xffffffffu, lane < kWarps && (double)(before + warps[0] + of_ties(t_before, warps[1])) > want);
+    const int chosen = __ffs(up_to) - 1;
+    if (chosen > 0) {
+        const unsigned long long w0 = __shfl_sync(0xffffffffu, warps[0], chosen - 1), t0 = __shfl_sync(0xffffffffu, warps[1], chosen - 1);
+        before += w0 + of_ties(t_before, t0);
+        t_before += t0;
+    }
+    // the element of vector i with which the wanted weight is exceeded, where it is one
+    auto pick = [&](int i) {
+        const float4 x4 = row.get(i);
+        unsigned long long each[4];
+        weights_of(each, x4, top, sh);
+        const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (x[e] < floor) continue;
+            if (x[e] == least_value) before += t_before++ < ties ? tie_weight : 0;
+            else before += each[e];
+            if ((double)before > want) {
+                a.tokens[r] = start - lead + (row.listed ? (int)sh.place[chosen][4 * i + e] : 4 * i + e);
+                return true;
+            }
+        }
+        return false;
+    };
+    if (warp == chosen && lane == 0) {     // its part of the stretch, or its list
+        sh.found_from = row.from;
+        sh.found_to = row.to;
+        sh.found_bin = row.listed;
+    }
+    const bool is_short = row.to - row.from <= 32;
+    if (warp == chosen && is_short) {      // a vector to a lane, whose parts are there
+        const unsigned long long w_up = scan_warp(lane_part[0]) - lane_part[0], t_up = scan_warp(lane_part[1]) - lane_part[1];
+        before += w_up + of_ties(t_before, t_up);
+        t_before += t_up;
+        if ((double)before <= want && (double)(before + lane_part[0] + of_ties(t_before, lane_part[1])) > want) pick(row.from + lane);
+    }
+    __syncthreads();
+    if (sh.found_to - sh.found_from <= 32) return;
+    row.from = sh.found_from;
+    row.to = sh.found_to;
+    row.listed = sh.found_bin != 0;
+    row.held = row.listed ? reinterpret_cast<const float4*>(sh.may_stay[chosen]) : stretch;
+    const int per = (row.to - row.from + kThreads - 1) / kThreads;
+    const int my_first = min(row.from + (int)threadIdx.x * per, row.to), my_end = min(my_first + per, row.to);
+    unsigned long long mine[2] = {0, 0}, all[2];
+#pragma unroll 1
+    for (int i = my_first; i < my_end; ++i) part_of(i, row, mine[0], mine[1]);
+    // of the threads before
+    const unsigned long long w_up = scan_cta(mine[0], all[0], sh.warp_scan[0]), t_up = scan_cta(mine[1], all[1], sh.warp_scan[1]);
+    before += w_up + of_ties(t_before, t_up);
+    t_before += t_up;
+    if ((double)before > want || (double)(before + mine[0] + of_ties(t_before, mine[1])) <= want) return;
+#pragma unroll 1
+    for (int i = my_first; i < my_end; ++i)
+        if (pick(i)) return;
 }
 
-constexpr int kMostHeld = 48 * 1024;       // tokens that a CTA keeps in shared memory; longer stretches are read again
+constexpr int kMostHeld = 192 * 1024;      // bytes that a CTA keeps in shared memory; longer stretches are read again
 
 template <typename T, bool HELD>
 cudaError_t issue(const SampleArgs& a, int ctas, cudaStream_t st)
@@ -466,7 +671,7 @@ cudaError_t issue(const SampleArgs& a, int ctas, cudaStream_t st)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.rows * ctas));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = HELD ? (size_t)(a.slice + 4) * 4 : 0;
+    cfg.dynamicSmemBytes = HELD ? (size_t)a.slice * 4 + 64 : 0;                // the stretch may begin and end inside a vector
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -479,14 +684,14 @@ cudaError_t launch(SampleArgs a, int num_sms, cudaStream_t st)
     int ctas = 1;
     while (ctas < kMostCtas && a.vocab > ctas * 4096) ctas *= 2;
     a.slice = ((a.vocab + ctas - 1) / ctas + 7) / 8 * 8;
-    return a.slice <= kMostHeld ? issue<T, true>(a, ctas, st) : issue<T, false>(a, ctas, st);
+    return (int64_t)a.slice * 4 + 64 <= kMostHeld ? issue<T, true>(a, ctas, st) : issue<T, false>(a, ctas, st);
 }
 
 }  // namespace
 
 cudaError_t configure_sample()
 {
-    const auto allow = [](auto* kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMostHeld + 4) * 4); };
+    const auto allow = [](auto* kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostHeld); };
     cudaError_t e = allow(sample_kernel<__nv_bfloat16, true>);
     if (e == cudaSuccess) e = allow(sample_kernel<__half, true>);
     if (e == cudaSuccess) e = allow(sample_kernel<float, true>);

@@ -22,7 +22,9 @@ long stream_parts_estimate(const KernelArgs& a, int ctas, int warps);
 
 namespace {
 
-constexpr int kQ4Stages = 4;          // slabs in flight or in use per warp
+constexpr int kQ4Pages = 2;           // pages that a warp takes at a time
+constexpr int kQ4Stages = 2;          // such pairs in flight or in use per warp
+constexpr int kQ4Keys = kQ4Pages * kPage;
 constexpr int kQ4CtasPerSM = 4;
 constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
 constexpr float kLeastLog = -80.f;    // steps below 2^-80 count as 2^-80 in the reference
@@ -56,19 +58,23 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// A warp that reduces runs of 4-bit pages.  Its stages and their barriers are its own; `turn` counts the pages it has taken, so stages and
-// phases go on from one run to the next.
+// A warp that reduces runs of 4-bit pages, two at a time.  Its stages and their barriers are its own; `turn` counts the pairs it has taken, so
+// stages and phases go on from one run to the next.
 template <int HD, int NG>
 struct Q4Walk {
     using Slab = Q4Slab<HD, NG>;
-    static constexpr int kBytes = kQ4Stages * Slab::kBytes;           // of one warp's stages
-    // of a CTA: the stages, where its warps' sums are folded in the end, then the barriers, which nothing else may touch
-    static constexpr int kCtaBytes = kDecWarps * (kBytes + kQ4Stages * 8);
+    static constexpr int kStage = kQ4Pages * Slab::kBytes;
+    static constexpr int kBytes = kQ4Stages * kStage;                 // of one warp's stages
+    static constexpr int kMass = kMaxSpans * 8 * 4;                   // of one warp's span sums
+    // of a CTA: the stages, where its warps' sums are folded in the end, the span sums, then the barriers, which nothing else may touch
+    static constexpr int kCtaBytes = kDecWarps * (kBytes + kMass + kQ4Stages * 8);
     static_assert(kDecWarps * 8 * (HD + 4) * 4 <= kDecWarps * kBytes, "the fold's buffer fits the stages");
     uint32_t base, bars, turn = 0;
+    float* mass;                                                      // [span][head]
 
     __device__ __forceinline__ Q4Walk(uint8_t* smem, int warp)
-        : base(smem_u32(smem) + warp * kBytes), bars(smem_u32(smem) + kDecWarps * kBytes + warp * kQ4Stages * 8)
+        : base(smem_u32(smem) + warp * kBytes), bars(smem_u32(smem) + kDecWarps * (kBytes + kMass) + warp * kQ4Stages * 8),
+          mass(reinterpret_cast<float*>(smem + kDecWarps * kBytes + warp * kMass))
     {
         if ((threadIdx.x & 31) == 0) {
 #pragma unroll
@@ -95,44 +101,70 @@ struct Q4Walk {
         if (seg <= 0) return;
 
         const int32_t* bt = a.block_table + (int64_t)s * a.max_blocks + pg;
-        const int key_base = pg * kPage;
+        const int key_base = pg * kPage, key_end = min(L, key_base + seg * kPage);
         const char* pages = reinterpret_cast<const char*>(a.k) + (int64_t)kvh * a.hs;     // strides in bytes
 
-        bool probe = false, broken = false;
-        if constexpr (NS > 0) {
-            for (int i = 0; i < G; ++i) probe |= (hc.slot[kvh * G + i] >= 0);
-            __syncwarp();
-            if (lane < 2 * NS) {
-                const int j = lane >> 1;
-                span[lane] = (probe && j < a.S) ? a.spans[((int64_t)s * a.S + j) * 2 + (lane & 1)] : 0;
+        // Spans cost nothing between their edges: `run` sums the probabilities since the last edge, for the spans in `inside`, and goes to their sums
+        // in shared memory at the next.
+        bool broken = false;
+        float run0 = 0.f, run1 = 0.f;
+        uint32_t inside = 0;
+        int edge = 0x7fffffff;
+        int my_a = 0, my_b = 0;                                       // lane j < S: span j
+        auto locate = [&](int key) {                                  // which spans hold the key, and where that next changes
+            inside = __ballot_sync(0xffffffffu, key >= my_a && key < my_b);
+            edge = __reduce_min_sync(0xffffffffu, my_a >= my_b ? 0x7fffffff : my_a > key ? my_a : my_b > key ? my_b : 0x7fffffff);
+        };
+        auto add_mass = [&](int j, float x0, float x1) {              // sums over the warp, to span j
+#pragma unroll
+            for (int d = 4; d <= 16; d <<= 1) {
+                x0 += __shfl_xor_sync(0xffffffffu, x0, d);
+                x1 += __shfl_xor_sync(0xffffffffu, x1, d);
             }
+            if (g == 0) {
+                mass[8 * j + 2 * tq] += x0;
+                mass[8 * j + 2 * tq + 1] += x1;
+            }
+        };
+        auto flush = [&]() {
+            if (inside)
+#pragma unroll 1
+                for (uint32_t left = inside; left; left &= left - 1) add_mass(__ffs(left) - 1, run0, run1);
+            run0 = run1 = 0.f;
+        };
+        if constexpr (NS > 0) {
+            bool probe = false;
+            for (int i = 0; i < G; ++i) probe |= (hc.slot[kvh * G + i] >= 0);
+            if (probe && lane < a.S) {
+                my_a = a.spans[((int64_t)s * a.S + lane) * 2];
+                my_b = a.spans[((int64_t)s * a.S + lane) * 2 + 1];
+            }
+            for (int i = lane; i < kMaxSpans * 8; i += 32) mass[i] = 0.f;
             __syncwarp();
+            locate(key_base);
         }
 
         // block ids of 32 consecutive pages, one per lane; the next 32 are fetched a window ahead
         int btw = 0, btw_next = (lane < seg) ? bt[lane] : 0;
-        auto issue = [&](int it) {
+        auto issue = [&](int it) {                                    // pages it and it + 1 by lanes 0 and 1
             if (it >= seg) return;
             if ((it & 31) == 0) {
                 btw = btw_next;
                 btw_next = (it + 32 + lane < seg) ? bt[it + 32 + lane] : 0;
             }
-            const int page = __shfl_sync(0xffffffffu, btw, it & 31);
-            const bool ok = page >= 0 && page < a.num_blocks;
-            broken |= !ok;
+            const int page = __shfl_sync(0xffffffffu, btw, (it + (lane & 1)) & 31);
+            const bool mine = lane < 2 && it + lane < seg, ok = mine && (uint32_t)page < (uint32_t)a.num_blocks;
+            const uint32_t good = __ballot_sync(0xffffffffu, ok), wanted = __ballot_sync(0xffffffffu, mine);
+            const uint32_t st = (turn + it / kQ4Pages) % kQ4Stages, bar = bars + 8 * st;
             if (lane == 0) {
-                const uint32_t st = (turn + it) % kQ4Stages, bar = bars + 8 * st;
-                if (ok) {
-                    mbar_expect_tx(bar, Slab::kBytes);
-                    bulk_load(base + st * Slab::kBytes, pages + (int64_t)page * a.bs, Slab::kBytes, bar);
-                } else {
-                    report(a.status, HOOK_ATTN_ERR_BOUNDS);
-                    mbar_arrive(bar);
-                }
+                mbar_expect_tx(bar, __popc(good) * Slab::kBytes);
+                if (good != wanted) report(a.status, HOOK_ATTN_ERR_BOUNDS);
             }
+            broken |= good != wanted;
+            __syncwarp();
+            if (ok) bulk_load(base + st * kStage + lane * Slab::kBytes, pages + (int64_t)page * a.bs, Slab::kBytes, bar);
         };
-#pragma unroll
-        for (int i = 0; i < kQ4Stages - 1; ++i) issue(i);
+        issue(0);
 
         // The queries of head g of the group as halves, times a power of two that brings the largest to [2^14, 2^15): what is below 2^-27 of
         // that loses bits.  In a word's pairs (element n, n + 4) the odd nibbles stand for 16 times their code.
@@ -193,69 +225,69 @@ struct Q4Walk {
         for (int j = 0; j < NG; ++j) zl[j][0] = zl[j][1] = 0.f;
 
         uint64_t limit_ns = 2000000000ull;
-        for (int it = 0; it < seg; ++it) {
-            issue(it + kQ4Stages - 1);
-            const uint32_t st = (turn + it) % kQ4Stages;
-            if (!__all_sync(0xffffffffu, mbar_wait(bars + 8 * st, ((turn + it) / kQ4Stages) & 1u, nullptr, limit_ns))) {
+#pragma unroll 1
+        for (int it = 0; it < seg; it += kQ4Pages) {
+            issue(it + kQ4Pages);
+            const uint32_t n = turn + it / kQ4Pages, st = n % kQ4Stages;
+            if (!__all_sync(0xffffffffu, mbar_wait(bars + 8 * st, (n / kQ4Stages) & 1u, nullptr, limit_ns))) {
                 if (lane == 0) report(a.status, HOOK_ATTN_ERR_TIMEOUT);
                 broken = true;
                 limit_ns = 1000000;                           // the others in flight are waited for, but not for long
             }
-            const uint32_t kt = base + st * Slab::kBytes, vt = kt + Slab::kCodes, kp = vt + Slab::kCodes, vp = kp + Slab::kParams;
+            const uint32_t stage = base + st * kStage;
             const int key0 = key_base + it * kPage;
+            const bool last = key0 + kQ4Keys > key_end;       // what lies behind the run may be anything
 
-            // ---- scores: keys g and g + 8 of the page for the heads 2 tq and 2 tq + 1 ----
-            float acc[NG][4];
-            {
-                uint32_t wa[W], wb[W];
+            // ---- scores: keys g and g + 8 of each page for the heads 2 tq and 2 tq + 1 ----
+            float x[kQ4Pages][4], top = 0.f;
+#pragma unroll
+            for (int u = 0; u < kQ4Pages; ++u) {
+                const uint32_t kt = stage + u * Slab::kBytes, kp = kt + 2 * Slab::kCodes + g * (NG * 4), vp = kp + Slab::kParams;
+                uint32_t wa[W], wb[W], pa[NG], pb[NG];
                 lds<W>(wa, kt + g * Slab::kRow + tq * (W * 4));
                 lds<W>(wb, kt + (g + 8) * Slab::kRow + tq * (W * 4));
+                lds<NG>(pa, kp);
+                lds<NG>(pb, kp + 8 * (NG * 4));
+                float w0 = 0.f, w1 = 0.f, w2 = 0.f, w3 = 0.f, y0 = 0.f, y1 = 0.f, y2 = 0.f, y3 = 0.f;
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
-                    acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int i = j * PER; i < (j + 1) * PER; ++i) {
-                        mma_f16_16816(acc[j], wa[i] & 0x000f000fu, wb[i] & 0x000f000fu, wa[i] & 0x00f000f0u, wb[i] & 0x00f000f0u, qb[2 * i][0], qb[2 * i][1]);
+                        mma_f16_16816(acc, wa[i] & 0x000f000fu, wb[i] & 0x000f000fu, wa[i] & 0x00f000f0u, wb[i] & 0x00f000f0u, qb[2 * i][0], qb[2 * i][1]);
                         const uint32_t ua = wa[i] >> 8, ub = wb[i] >> 8;
-                        mma_f16_16816(acc[j], ua & 0x000f000fu, ub & 0x000f000fu, ua & 0x00f000f0u, ub & 0x00f000f0u, qb[2 * i + 1][0], qb[2 * i + 1][1]);
+                        mma_f16_16816(acc, ua & 0x000f000fu, ub & 0x000f000fu, ua & 0x00f000f0u, ub & 0x00f000f0u, qb[2 * i + 1][0], qb[2 * i + 1][1]);
                     }
+                    const float sa = q4_step(pa[j]), sb = q4_step(pb[j]), la = q4_lowest(pa[j]), lb = q4_lowest(pb[j]);
+                    y0 += sa * acc[0]; y1 += sa * acc[1];
+                    y2 += sb * acc[2]; y3 += sb * acc[3];
+                    w0 += la * qsum[j][0]; w1 += la * qsum[j][1];
+                    w2 += lb * qsum[j][0]; w3 += lb * qsum[j][1];
                 }
+                x[u][0] = y0 * qs0 + w0; x[u][1] = y1 * qs1 + w1;
+                x[u][2] = y2 * qs0 + w2; x[u][3] = y3 * qs1 + w3;
+                lds<NG>(pa, vp);                              // steps of V
+                lds<NG>(pb, vp + 8 * (NG * 4));
+                const int t0 = key0 + u * kPage + g;
+                if (last && t0 >= key_end) {
+                    x[u][0] = x[u][1] = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) pa[j] = 0;
+                }
+                if (last && t0 + 8 >= key_end) {
+                    x[u][2] = x[u][3] = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) pb[j] = 0;
+                }
+#pragma unroll
+                for (int j = 0; j < NG; ++j) top = fmaxf(top, fmaxf(q4_step(pa[j]), q4_step(pb[j])));
             }
-            float x0 = 0.f, x1 = 0.f, x2 = 0.f, x3 = 0.f;
-            {
-                uint32_t pa[NG], pb[NG];
-                lds<NG>(pa, kp + g * (NG * 4));
-                lds<NG>(pb, kp + (g + 8) * (NG * 4));
-                float w0 = 0.f, w1 = 0.f, w2 = 0.f, w3 = 0.f;
+            float mx0 = x[0][0], mx1 = x[0][1];
 #pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    x0 += q4_step(pa[j]) * acc[j][0]; x1 += q4_step(pa[j]) * acc[j][1];
-                    x2 += q4_step(pb[j]) * acc[j][2]; x3 += q4_step(pb[j]) * acc[j][3];
-                    w0 += q4_lowest(pa[j]) * qsum[j][0]; w1 += q4_lowest(pa[j]) * qsum[j][1];
-                    w2 += q4_lowest(pb[j]) * qsum[j][0]; w3 += q4_lowest(pb[j]) * qsum[j][1];
-                }
-                x0 = x0 * qs0 + w0; x1 = x1 * qs1 + w1;
-                x2 = x2 * qs0 + w2; x3 = x3 * qs1 + w3;
+            for (int u = 0; u < kQ4Pages; ++u) {
+                mx0 = fmaxf(mx0, fmaxf(x[u][0], x[u][2]));
+                mx1 = fmaxf(mx1, fmaxf(x[u][1], x[u][3]));
             }
-            uint32_t va[NG], vb[NG];                          // steps and lowest values of V
-            lds<NG>(va, vp + g * (NG * 4));
-            lds<NG>(vb, vp + (g + 8) * (NG * 4));
-            const int t0 = key0 + g, t1 = t0 + 8;
-            if (key0 + kPage > L) {                           // what lies behind the sequence may be anything
-                if (t0 >= L) {
-                    x0 = x1 = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < NG; ++j) va[j] = 0;
-                }
-                if (t1 >= L) {
-                    x2 = x3 = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < NG; ++j) vb[j] = 0;
-                }
-            }
-            float mx0 = fmaxf(x0, x2), mx1 = fmaxf(x1, x3), top = 0.f;
-#pragma unroll
-            for (int j = 0; j < NG; ++j) top = fmaxf(top, fmaxf(q4_step(va[j]), q4_step(vb[j])));
             // ---- the reference: m = f - steps ----
             if (__any_sync(0xffffffffu, mx0 > f0 + (kDecRaise - steps) || mx1 > f1 + (kDecRaise - steps) || top > step_limit)) {
 #pragma unroll
@@ -275,56 +307,89 @@ struct Q4Walk {
                 for (int i = 0; i < KS; ++i) { o[i][0] *= c0; o[i][1] *= c1; o[i][2] *= c0; o[i][3] *= c1; }
 #pragma unroll
                 for (int j = 0; j < NG; ++j) { zl[j][0] *= c0; zl[j][1] *= c1; }
-                if (NS > 0) {
-#pragma unroll
-                    for (int j = 0; j < NSX; ++j) { sm[j][0] *= c0; sm[j][1] *= c1; }
+                if constexpr (NS > 0) {
+                    run0 *= c0;
+                    run1 *= c1;
+                    if (g == 0)
+#pragma unroll 1
+                        for (int j = 0; j < a.S; ++j) { mass[8 * j + 2 * tq] *= c0; mass[8 * j + 2 * tq + 1] *= c1; }
                 }
             }
-            const float p0 = fast_exp2(x0 - f0), p1 = fast_exp2(x1 - f1);
-            const float p2 = fast_exp2(x2 - f0), p3 = fast_exp2(x3 - f1);
-            l0 += p0 + p2;
-            l1 += p1 + p3;
-            if (NS > 0 && probe) {
+            float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-                for (int j = 0; j < NSX; ++j) {
-                    const int sa = span[2 * j], sb = span[2 * j + 1];
-                    if (sb > key0 && sa < key0 + kPage) {
-                        const bool in0 = (t0 >= sa) && (t0 < sb), in1 = (t1 >= sa) && (t1 < sb);
-                        sm[j][0] += (in0 ? p0 : 0.f) + (in1 ? p2 : 0.f);
-                        sm[j][1] += (in0 ? p1 : 0.f) + (in1 ? p3 : 0.f);
+            for (int u = 0; u < kQ4Pages; ++u) {
+                x[u][0] = fast_exp2(x[u][0] - f0); x[u][1] = fast_exp2(x[u][1] - f1);
+                x[u][2] = fast_exp2(x[u][2] - f0); x[u][3] = fast_exp2(x[u][3] - f1);
+                s0 += x[u][0] + x[u][2];
+                s1 += x[u][1] + x[u][3];
+            }
+            l0 += s0;
+            l1 += s1;
+            if constexpr (NS > 0) {
+                if (edge >= key0 + kQ4Keys) {
+                    run0 += s0;
+                    run1 += s1;
+                } else {                                      // an edge among these keys
+                    flush();
+#pragma unroll 1
+                    for (int j = 0; j < a.S; ++j) {
+                        const int sa = __shfl_sync(0xffffffffu, my_a, j), sb = __shfl_sync(0xffffffffu, my_b, j);
+                        float in0 = 0.f, in1 = 0.f;
+#pragma unroll
+                        for (int u = 0; u < kQ4Pages; ++u) {
+                            const int t0 = key0 + u * kPage + g, t1 = t0 + 8;
+                            if (t0 >= sa && t0 < sb) { in0 += x[u][0]; in1 += x[u][1]; }
+                            if (t1 >= sa && t1 < sb) { in0 += x[u][2]; in1 += x[u][3]; }
+                        }
+                        add_mass(j, in0, in1);
+                    }
+                    locate(key0 + kQ4Keys);
+                }
+            }
+            // ---- P V, page by page: for each group the probabilities times the steps, as the B operand (k = key, n = head) ----
+#pragma unroll
+            for (int u = 0; u < kQ4Pages; ++u) {
+                const uint32_t vt = stage + u * Slab::kBytes + Slab::kCodes, vp = vt + Slab::kCodes + Slab::kParams + g * (NG * 4);
+                uint32_t va[NG], vb[NG], pb[NG][2];
+                lds<NG>(va, vp);
+                lds<NG>(vb, vp + 8 * (NG * 4));
+                if (last) {
+                    const int t0 = key0 + u * kPage + g;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) {
+                        if (t0 >= key_end) va[j] = 0;
+                        if (t0 + 8 >= key_end) vb[j] = 0;
                     }
                 }
-            }
-            // ---- P V: for each group the probabilities times the steps, as the B operand (k = key, n = head) ----
-            uint32_t pb[NG][2];
 #pragma unroll
-            for (int j = 0; j < NG; ++j) {
-                const float sa = q4_step(va[j]), sb = q4_step(vb[j]);
-                pb[j][0] = movmatrix_trans(pack_f16(p0 * sa, p1 * sa));
-                pb[j][1] = movmatrix_trans(pack_f16(p2 * sb, p3 * sb));
-                zl[j][0] += p0 * q4_lowest(va[j]) + p2 * q4_lowest(vb[j]);
-                zl[j][1] += p1 * q4_lowest(va[j]) + p3 * q4_lowest(vb[j]);
-            }
-            constexpr int U = HD / 64;                        // words of a unit: keys 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9 of the page
-            uint32_t v0[U], v1[U], v2[U], v3[U];
-            const uint32_t unit = vt + tq * Slab::kRow + q4_unit<HD>(tq, g) * (U * 4);
-            lds<U>(v0, unit);
-            lds<U>(v1, unit + 4 * Slab::kRow);
-            lds<U>(v2, unit + 8 * Slab::kRow);
-            lds<U>(v3, unit + 12 * Slab::kRow);
+                for (int j = 0; j < NG; ++j) {
+                    const float sa = q4_step(va[j]), sb = q4_step(vb[j]), la = q4_lowest(va[j]), lb = q4_lowest(vb[j]);
+                    pb[j][0] = movmatrix_trans(pack_f16(x[u][0] * sa, x[u][1] * sa));
+                    pb[j][1] = movmatrix_trans(pack_f16(x[u][2] * sb, x[u][3] * sb));
+                    zl[j][0] += x[u][0] * la + x[u][2] * lb;
+                    zl[j][1] += x[u][1] * la + x[u][3] * lb;
+                }
+                constexpr int U = HD / 64;                    // words of a unit: keys 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9 of the page
+                uint32_t v0[U], v1[U], v2[U], v3[U];
+                const uint32_t unit = vt + tq * Slab::kRow + q4_unit<HD>(tq, g) * (U * 4);
+                lds<U>(v0, unit);
+                lds<U>(v1, unit + 4 * Slab::kRow);
+                lds<U>(v2, unit + 8 * Slab::kRow);
+                lds<U>(v3, unit + 12 * Slab::kRow);
 #pragma unroll
-            for (int j = 0; j < W; ++j) {                     // 32 elements: two blocks of 16 of the output
-                const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-                uint32_t lo = __byte_perm(v0[j / 2], v1[j / 2], sel), hi = __byte_perm(v2[j / 2], v3[j / 2], sel);
-                const int grp = j / PER;
-                mma_f16_16816(o[2 * j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, pb[grp][0], pb[grp][1]);
-                lo >>= 8;
-                hi >>= 8;
-                mma_f16_16816(o[2 * j + 1], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, pb[grp][0], pb[grp][1]);
+                for (int j = 0; j < W; ++j) {                 // 32 elements: two blocks of 16 of the output
+                    const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+                    uint32_t lo = __byte_perm(v0[j / 2], v1[j / 2], sel), hi = __byte_perm(v2[j / 2], v3[j / 2], sel);
+                    const int grp = j / PER;
+                    mma_f16_16816(o[2 * j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, pb[grp][0], pb[grp][1]);
+                    lo >>= 8;
+                    hi >>= 8;
+                    mma_f16_16816(o[2 * j + 1], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u, pb[grp][0], pb[grp][1]);
+                }
             }
             __syncwarp();                                     // the stage may be filled again
         }
-        turn += seg;
+        turn += (seg + kQ4Pages - 1) / kQ4Pages;
 
         // per-thread partial sums -> per-warp sums (lanes with the same tq hold the same heads)
 #pragma unroll
@@ -336,13 +401,16 @@ struct Q4Walk {
                 zl[j][0] += __shfl_xor_sync(0xffffffffu, zl[j][0], d);
                 zl[j][1] += __shfl_xor_sync(0xffffffffu, zl[j][1], d);
             }
-            if (NS > 0) {
+        }
+        if constexpr (NS > 0) {
+            flush();
+            __syncwarp();
 #pragma unroll
-                for (int j = 0; j < NS; ++j) {
-                    sm[j][0] += __shfl_xor_sync(0xffffffffu, sm[j][0], d);
-                    sm[j][1] += __shfl_xor_sync(0xffffffffu, sm[j][1], d);
-                }
+            for (int j = 0; j < NS; ++j) {
+                sm[j][0] = mass[8 * j + 2 * tq];
+                sm[j][1] = mass[8 * j + 2 * tq + 1];
             }
+            __syncwarp();
         }
         m0 = f0;
         m1 = f1;

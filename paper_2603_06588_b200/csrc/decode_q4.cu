@@ -11,6 +11,8 @@
 //
 // Halves reach from 2^-24 to 2^16, so the softmax's reference is that of p * step: it is raised when a score exceeds it by 2^8 or a step
 // exceeds 2^7 times the power of two that stands for the steps.  It cancels in o / l and s / l, as in decode.cu.
+#include <type_traits>
+
 #include "decode_device.cuh"
 #include "q4.cuh"
 
@@ -225,8 +227,9 @@ struct Q4Walk {
         for (int j = 0; j < NG; ++j) zl[j][0] = zl[j][1] = 0.f;
 
         uint64_t limit_ns = 2000000000ull;
-#pragma unroll 1
-        for (int it = 0; it < seg; it += kQ4Pages) {
+        // LAST: the run ends among these keys, and what lies behind it may be anything.
+        auto pair_of_pages = [&](auto LAST, int it) {
+            constexpr bool last = decltype(LAST)::value;
             issue(it + kQ4Pages);
             const uint32_t n = turn + it / kQ4Pages, st = n % kQ4Stages;
             if (!__all_sync(0xffffffffu, mbar_wait(bars + 8 * st, (n / kQ4Stages) & 1u, nullptr, limit_ns))) {
@@ -236,7 +239,6 @@ struct Q4Walk {
             }
             const uint32_t stage = base + st * kStage;
             const int key0 = key_base + it * kPage;
-            const bool last = key0 + kQ4Keys > key_end;       // what lies behind the run may be anything
 
             // ---- scores: keys g and g + 8 of each page for the heads 2 tq and 2 tq + 1 ----
             float x[kQ4Pages][4], top = 0.f;
@@ -388,7 +390,11 @@ struct Q4Walk {
                 }
             }
             __syncwarp();                                     // the stage may be filled again
-        }
+        };
+        int it = 0;
+#pragma unroll 1
+        for (; key_base + it * kPage + kQ4Keys <= key_end; it += kQ4Pages) pair_of_pages(std::false_type(), it);
+        if (it < seg) pair_of_pages(std::true_type(), it);
         turn += (seg + kQ4Pages - 1) / kQ4Pages;
 
         // per-thread partial sums -> per-warp sums (lanes with the same tq hold the same heads)

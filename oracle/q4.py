@@ -26,7 +26,7 @@ def quantise(x, group):
     codes, steps, lows = np.zeros(g.shape, dtype=np.int64), np.zeros(g.shape[:-1]), np.zeros(g.shape[:-1])
     for at in np.ndindex(*g.shape[:-1]):
         v = g[at].astype(np.float32)
-        low, high = v.min(), v.max()
+        low, high = v.min() + np.float32(0), v.max()                   # one zero
         with np.errstate(all="ignore"):
             step = float(bf16((high - low) / np.float32(15)))
         if not np.all(np.isfinite(v)) or not math.isfinite(step):

@@ -5,6 +5,8 @@
 //   lowest = min x,  step = (max x - min x) / 15 in bf16 (0 below 2^-100),  t = x - lowest in 32 bits,  c = t / step rounded to nearest,
 // halves to even, 0 .. 15 -- of the quotient itself and not of a rounded one, so that a code can be told from the inputs.  An element is off
 // by half a step at most (and by 15/512 of one more where the step was rounded down).
+#include <type_traits>
+
 #include "q4.cuh"
 #include "rope_device.cuh"
 
@@ -14,30 +16,57 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 8;             // rows per CTA at most: one warp looks each of them up
-constexpr int kAppendStage = 40 * 1024;    // bytes of keys and values of its rows that a CTA holds
+constexpr int kAppendStage = 40 * 1024;    // bytes of the keys of its rows that a CTA holds
 
-// c with |t - c step| at most half a step, halves to even.  t / step is estimated with the step's reciprocal (off by 2^-22 of it), and what is
-// left over is exact where it decides: t and c step lie within a step of one another.
-__device__ __forceinline__ uint32_t q4_code(float t, float step, float inv)
+// The smaller of two pairs of bf16, element by element; NaN where either is.
+__device__ __forceinline__ uint32_t min_pairs(uint32_t x, uint32_t y)
 {
-    float c = rintf(t * inv);
-    const float left = fmaf(-c, step, t), half = 0.5f * step;
-    const bool odd = ((int)c & 1) != 0;
-    if (left > half || (left == half && odd)) c += 1.f;
-    else if (left < -half || (left == -half && odd)) c -= 1.f;
-    return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
+    uint32_t m;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(x), "r"(y));
+    return m;
 }
 
-// A CTA takes a few rows.  Queries are turned and stored as in hook_rope_append; keys (turned) and values go to shared memory as bf16, then
-// a thread takes eight neighbouring elements of a head: the lanes of a group agree on its lowest and highest value, a thread's codes are a
-// word of K as they are, and four lanes exchange theirs for V.
+// The eight codes of four pairs of bf16 as a word: c with |t - c step| at most half a step, halves to even.  The quotient of t and the step's
+// reciprocal, corrected once by what it leaves over, is t / step to the nearest: a half where that is one, so that adding 1.5 * 2^23 rounds as asked,
+// and leaves the code in the low bits.  Only where a quotient next to a half became one can the code be a step off; that shows in what is left
+// over, which is exact (t and c step lie within a step of one another).  The sum of the words so shifted holds all eight codes.
+__device__ __forceinline__ uint32_t q4_codes(const uint32_t (&w)[4], float lo, float step)
+{
+    if (!(step > 0.f)) return 0;
+    constexpr float kRound = 12582912.f;
+    const float inv = 1.f / step, half = 0.5f * step;
+    uint32_t codes = 0;
+    bool off = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) - lo;
+        const float q = t * inv, rounded = fmaf(fmaf(-q, step, t), inv, q) + kRound;
+        off |= fabsf(fmaf(kRound - rounded, step, t)) > half;
+        codes += __float_as_uint(rounded) << (4 * e);
+    }
+    if (off) {
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t word = e < 4 ? (e < 2 ? w[0] : w[1]) : (e < 6 ? w[2] : w[3]);
+            const float t = __uint_as_float(e & 1 ? word & 0xffff0000u : word << 16) - lo;
+            const float q = t * inv, rounded = fmaf(fmaf(-q, step, t), inv, q) + kRound, left = fmaf(kRound - rounded, step, t);
+            if (left > half) codes += 1u << (4 * e);
+            if (left < -half) codes -= 1u << (4 * e);
+        }
+    }
+    return codes - (0x4b400000u + 0xb4000000u + 0x40000000u);     // the constant's own bits: shifted three times they are gone
+}
+
+// A CTA takes a few rows.  Queries are turned and stored as in hook_rope_append; keys, turned, go to shared memory as bf16.  Then a thread takes
+// eight neighbouring elements of a head of keys or values: the lanes of a group agree on its lowest and highest value, a thread's codes are
+// a word of K as they are, and four lanes exchange theirs for V.
 template <typename T, int V, int HD, int NG>
 __global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __grid_constant__ RopeArgs a)
 {
     using Slab = Q4Slab<HD, NG>;
     __shared__ __align__(16) float2 turn[kAppendRows][kMaxPairs];
     __shared__ RowPlace places[kAppendRows];
-    extern __shared__ __align__(16) __nv_bfloat16 held[];            // [rows][K, V][Hkv][HD]
+    extern __shared__ __align__(16) __nv_bfloat16 held[];            // [rows][Hkv][HD]
     const int row0 = blockIdx.x * a.rows_per_cta, warp = threadIdx.x >> 5;
     if (warp < a.rows_per_cta) {
         const RowPlace r = find_row(a, row0 + warp);
@@ -54,34 +83,35 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __
     }
     __syncthreads();
 
-    constexpr int PER_HEAD = HD / (2 * V);
-    const int heads = a.Hq + 2 * a.Hkv, turning = a.pairs / V, total = a.rows_per_cta * heads * PER_HEAD;
-    for (int i = threadIdx.x; i < total; i += kAppendThreads) {
-        const int j = i % PER_HEAD, rh = i / PER_HEAD, r = rh / heads;
-        int h = rh - r * heads;
+    // A thread keeps its place j in a head, and goes through heads and rows in steps.
+    constexpr int PER_HEAD = HD / (2 * V), STEP = kAppendThreads / PER_HEAD;
+    const int heads = a.Hq + a.Hkv, j = threadIdx.x % PER_HEAD;
+    const bool turns = j < a.pairs / V;
+    int e0 = j * 2 * V, e1 = e0 + V;
+    if (a.halves && turns) {
+        e0 = j * V;
+        e1 = a.pairs + j * V;
+    }
+    const int row_step = STEP / heads, head_step = STEP % heads;
+    int r = threadIdx.x / PER_HEAD / heads, at = threadIdx.x / PER_HEAD % heads;
+    for (; r < a.rows_per_cta; r += row_step, at += head_step) {
+        if (at >= heads) {
+            at -= heads;
+            if (++r >= a.rows_per_cta) break;
+        }
+        int h = at;
         const int state = places[r].state;
         if (state == kBehind || (state == kBroken && h >= a.Hq)) continue;
         const int64_t row = row0 + r;
         const T* src;
         __nv_bfloat16* dst;
-        bool turns = j < turning;
         if (h < a.Hq) {
             src = static_cast<const T*>(a.q) + row * a.q_row + h * a.q_head;
             dst = a.q_out + (row * a.Hq + h) * HD;
         } else {
             h -= a.Hq;
-            dst = held + (r * 2 * a.Hkv + h) * HD;
-            if (h < a.Hkv) {
-                src = static_cast<const T*>(a.k) + row * a.k_row + h * a.k_head;
-            } else {
-                src = static_cast<const T*>(a.v) + row * a.v_row + (h - a.Hkv) * a.v_head;
-                turns = false;
-            }
-        }
-        int e0 = j * 2 * V, e1 = e0 + V;
-        if (a.halves && j < turning) {             // v takes the same runs as k: which they are is of no account there
-            e0 = j * V;
-            e1 = a.pairs + j * V;
+            src = static_cast<const T*>(a.k) + row * a.k_row + h * a.k_head;
+            dst = held + (r * a.Hkv + h) * HD;
         }
         float x[V], y[V];
         load(x, src + e0);
@@ -96,48 +126,58 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __
     }
     __syncthreads();
 
-    constexpr int CHUNKS = HD / 8, LANES = CHUNKS / NG;              // threads to a head and to a group
-    const int work = a.rows_per_cta * 2 * a.Hkv * CHUNKS, rounded = (work + kAppendThreads - 1) / kAppendThreads * kAppendThreads;
-    for (int i = threadIdx.x; i < rounded; i += kAppendThreads) {    // all lanes of a warp stay: they exchange values
-        const int c = i % CHUNKS, rh = i / CHUNKS, r = rh / (2 * a.Hkv);
-        int h = rh - r * 2 * a.Hkv;
-        const bool live = i < work && places[r].state == kGood;
-        uint4 raw = make_uint4(0, 0, 0, 0);
-        if (live) raw = *reinterpret_cast<const uint4*>(held + (size_t)rh * HD + 8 * c);
-        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-        float x[8], bad = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = q4_step(w[e]);              // a bf16 in the low half, and one in the high half
-            x[2 * e + 1] = q4_lowest(w[e]);
+    constexpr int CHUNKS = HD / 8, LANES = CHUNKS / NG, UNITS = kAppendThreads / CHUNKS;     // threads to a head and to a group; heads at a time
+    const int both = 2 * a.Hkv, c = threadIdx.x % CHUNKS, next_row = UNITS / both, next_head = UNITS % both;
+    const int turns_of_all = (a.rows_per_cta * both + UNITS - 1) / UNITS;
+    r = threadIdx.x / CHUNKS / both;
+    at = threadIdx.x / CHUNKS % both;
+    for (int n = 0; n < turns_of_all; ++n, r += next_row, at += next_head) {     // all lanes of a warp stay: they exchange values
+        if (at >= both) {
+            at -= both;
+            ++r;
         }
-        float lo = x[0], hi = x[0];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            lo = fminf(lo, x[e]);
-            hi = fmaxf(hi, x[e]);
-            bad = fmaf(x[e], 0.f, bad);            // NaN when an element is not finite
-        }
-#pragma unroll
-        for (int d = 1; d < LANES; d <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-            bad += __shfl_xor_sync(0xffffffffu, bad, d);
-        }
-        float step = __bfloat162float(__float2bfloat16((hi - lo) / 15.f));
-        if (step < 7.88860905e-31f) step = 0.f;    // 2^-100
-        if (bad != 0.f || !(step <= 3.3895314e38f)) step = __int_as_float(0x7fc00000);
-        const float inv = step > 0.f ? 1.f / step : 0.f;
-        uint32_t codes = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (step > 0.f) codes |= q4_code(x[e] - lo, step, inv) << (4 * e);
+        int h = at;
+        const bool live = r < a.rows_per_cta && places[r].state == kGood;
         const bool value = h >= a.Hkv;
+        if (value) h -= a.Hkv;
+        uint32_t w[4] = {};
+        if (live && !value) {
+            const uint4 raw = *reinterpret_cast<const uint4*>(held + (r * a.Hkv + h) * HD + 8 * c);
+            w[0] = raw.x; w[1] = raw.y; w[2] = raw.z; w[3] = raw.w;
+        } else if (live) {
+            const T* src = static_cast<const T*>(a.v) + (row0 + r) * a.v_row + h * a.v_head + 8 * c;
+            if constexpr (std::is_same<T, __nv_bfloat16>::value && V == 8) {
+                const uint4 raw = *reinterpret_cast<const uint4*>(src);
+                w[0] = raw.x; w[1] = raw.y; w[2] = raw.z; w[3] = raw.w;
+            } else {
+                float x[8];
+#pragma unroll
+                for (int p = 0; p < 8 / V; ++p) {
+                    float y[V];
+                    load(y, src + p * V);
+#pragma unroll
+                    for (int m = 0; m < V; ++m) x[p * V + m] = y[m];
+                }
+#pragma unroll
+                for (int p = 0; p < 4; ++p) w[p] = pack_bf16(x[2 * p], x[2 * p + 1]);
+            }
+        }
+        // lowest, and the lowest of the negated ones, as a pair: a NaN stays in it, and an infinity leaves no finite range
+        const uint32_t low = min_pairs(min_pairs(w[0], w[1]), min_pairs(w[2], w[3]));
+        const uint32_t high = min_pairs(min_pairs(w[0] ^ 0x80008000u, w[1] ^ 0x80008000u), min_pairs(w[2] ^ 0x80008000u, w[3] ^ 0x80008000u));
+        uint32_t range = min_pairs(__byte_perm(low, high, 0x5410), __byte_perm(low, high, 0x7632));
+#pragma unroll
+        for (int d = 1; d < LANES; d <<= 1) range = min_pairs(range, __shfl_xor_sync(0xffffffffu, range, d));
+        const float lo = q4_step(range) + 0.f, width = -q4_lowest(range) - lo;    // one zero
+        const float fifteenth = width * (1.f / 15.f);                             // corrected once: width / 15 to the nearest
+        float step = __bfloat162float(__float2bfloat16(fmaf(fmaf(-fifteenth, 15.f, width), 1.f / 15.f, fifteenth)));
+        if (step < 7.88860905e-31f) step = 0.f;                                   // 2^-100
+        if (!(step <= 3.3895314e38f)) step = __int_as_float(0x7fc00000);
+        const uint32_t codes = q4_codes(w, lo, step);
         uint32_t others[4];                        // of the four chunks of 32 elements, in their order
 #pragma unroll
         for (int k = 0; k < 4; ++k) others[k] = __shfl_sync(0xffffffffu, codes, (threadIdx.x & 28) + k);
         if (!live) continue;
-        if (value) h -= a.Hkv;
         const int t = places[r].pos % kPage;
         uint8_t* slab = reinterpret_cast<uint8_t*>(a.k_cache) + places[r].slot + h * a.hs;
         if (!value) {
@@ -166,7 +206,7 @@ template <typename T, int V, int HD, int NG>
 cudaError_t issue(RopeArgs& a, int num_sms, cudaStream_t st)
 {
     // as many rows per CTA as let all CTAs be resident at once, within the shared memory that holds their keys and values
-    const int row_bytes = 2 * a.Hkv * HD * 2, resident = num_sms * 4;
+    const int row_bytes = a.Hkv * HD * 2, resident = num_sms * 4;
     int rows = (a.total_q + resident - 1) / resident;
     if (rows > kAppendRows) rows = kAppendRows;
     if (rows > kAppendStage / row_bytes) rows = kAppendStage / row_bytes > 0 ? kAppendStage / row_bytes : 1;
@@ -191,6 +231,7 @@ cudaError_t launch(RopeArgs& a, int group, int num_sms, cudaStream_t st)
     const int64_t strides = a.q_row | a.q_head | a.k_row | a.k_head | a.v_row | a.v_head | a.pairs;
     const uintptr_t from = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v);
     if (((strides & 7) == 0) && (from & 15) == 0) return for_group<T, 8>(a, group, num_sms, st);
+    if (((strides | (int64_t)(from / sizeof(T))) & 3) == 0) return for_group<T, 4>(a, group, num_sms, st);
     if (((strides | (int64_t)(from / sizeof(T))) & 1) == 0) return for_group<T, 2>(a, group, num_sms, st);
     return for_group<T, 1>(a, group, num_sms, st);
 }

@@ -83,36 +83,38 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __
     }
     __syncthreads();
 
-    // A thread keeps its place j in a head, and goes through heads and rows in steps.
-    constexpr int PER_HEAD = HD / (2 * V), STEP = kAppendThreads / PER_HEAD;
-    const int heads = a.Hq + a.Hkv, j = threadIdx.x % PER_HEAD;
+    // `per` threads to a head: a thread keeps its place in a head, and goes through the heads of a row, or of as many rows as the CTA has threads
+    // for, in steps that are powers of two.
+    auto each_head = [&](int heads, int per, auto body) {
+        int lanes = kAppendThreads;
+        while (lanes / 2 >= heads * per) lanes /= 2;
+        for (int r = threadIdx.x / lanes; r < a.rows_per_cta; r += kAppendThreads / lanes)
+            for (int h = threadIdx.x % lanes / per; h < heads; h += lanes / per) body(r, h);
+    };
+    constexpr int PER_HEAD = HD / (2 * V);
+    const int j = threadIdx.x % PER_HEAD;
     const bool turns = j < a.pairs / V;
     int e0 = j * 2 * V, e1 = e0 + V;
     if (a.halves && turns) {
         e0 = j * V;
         e1 = a.pairs + j * V;
     }
-    const int row_step = STEP / heads, head_step = STEP % heads;
-    int r = threadIdx.x / PER_HEAD / heads, at = threadIdx.x / PER_HEAD % heads;
-    for (; r < a.rows_per_cta; r += row_step, at += head_step) {
-        if (at >= heads) {
-            at -= heads;
-            if (++r >= a.rows_per_cta) break;
-        }
-        int h = at;
+    each_head(a.Hkv, PER_HEAD, [&](int r, int h) {
+        if (places[r].state != kGood) return;
+        const T* src = static_cast<const T*>(a.k) + (int64_t)(row0 + r) * a.k_row + h * a.k_head;
+        float x[V], y[V];
+        load(x, src + e0);
+        load(y, src + e1);
+        if (turns) turn_item<V>(x, y, &turn[r][j * V], a.halves);
+        store(held + (r * a.Hkv + h) * HD + e0, x);
+        store(held + (r * a.Hkv + h) * HD + e1, y);
+    });
+    each_head(a.Hq, PER_HEAD, [&](int r, int h) {
         const int state = places[r].state;
-        if (state == kBehind || (state == kBroken && h >= a.Hq)) continue;
+        if (state == kBehind) return;
         const int64_t row = row0 + r;
-        const T* src;
-        __nv_bfloat16* dst;
-        if (h < a.Hq) {
-            src = static_cast<const T*>(a.q) + row * a.q_row + h * a.q_head;
-            dst = a.q_out + (row * a.Hq + h) * HD;
-        } else {
-            h -= a.Hq;
-            src = static_cast<const T*>(a.k) + row * a.k_row + h * a.k_head;
-            dst = held + (r * a.Hkv + h) * HD;
-        }
+        const T* src = static_cast<const T*>(a.q) + row * a.q_row + h * a.q_head;
+        __nv_bfloat16* dst = a.q_out + (row * a.Hq + h) * HD;
         float x[V], y[V];
         load(x, src + e0);
         load(y, src + e1);
@@ -123,29 +125,22 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __
         }
         store(dst + e0, x);
         store(dst + e1, y);
-    }
+    });
     __syncthreads();
 
-    constexpr int CHUNKS = HD / 8, LANES = CHUNKS / NG, UNITS = kAppendThreads / CHUNKS;     // threads to a head and to a group; heads at a time
-    const int both = 2 * a.Hkv, c = threadIdx.x % CHUNKS, next_row = UNITS / both, next_head = UNITS % both;
-    const int turns_of_all = (a.rows_per_cta * both + UNITS - 1) / UNITS;
-    r = threadIdx.x / CHUNKS / both;
-    at = threadIdx.x / CHUNKS % both;
-    for (int n = 0; n < turns_of_all; ++n, r += next_row, at += next_head) {     // all lanes of a warp stay: they exchange values
-        if (at >= both) {
-            at -= both;
-            ++r;
-        }
-        int h = at;
-        const bool live = r < a.rows_per_cta && places[r].state == kGood;
-        const bool value = h >= a.Hkv;
-        if (value) h -= a.Hkv;
+    constexpr int CHUNKS = HD / 8, LANES = CHUNKS / NG;              // threads to a head and to a group
+    const int c = threadIdx.x % CHUNKS;
+    const uint32_t head_lanes = ((1u << CHUNKS) - 1) << (threadIdx.x & (32 - CHUNKS) & 31);
+    each_head(2 * a.Hkv, CHUNKS, [&](int r, int kv) {
+        if (places[r].state != kGood) return;
+        const bool value = kv >= a.Hkv;
+        const int h = value ? kv - a.Hkv : kv;
         uint32_t w[4] = {};
-        if (live && !value) {
+        if (!value) {
             const uint4 raw = *reinterpret_cast<const uint4*>(held + (r * a.Hkv + h) * HD + 8 * c);
             w[0] = raw.x; w[1] = raw.y; w[2] = raw.z; w[3] = raw.w;
-        } else if (live) {
-            const T* src = static_cast<const T*>(a.v) + (row0 + r) * a.v_row + h * a.v_head + 8 * c;
+        } else {
+            const T* src = static_cast<const T*>(a.v) + (int64_t)(row0 + r) * a.v_row + h * a.v_head + 8 * c;
             if constexpr (std::is_same<T, __nv_bfloat16>::value && V == 8) {
                 const uint4 raw = *reinterpret_cast<const uint4*>(src);
                 w[0] = raw.x; w[1] = raw.y; w[2] = raw.z; w[3] = raw.w;
@@ -167,22 +162,21 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __
         const uint32_t high = min_pairs(min_pairs(w[0] ^ 0x80008000u, w[1] ^ 0x80008000u), min_pairs(w[2] ^ 0x80008000u, w[3] ^ 0x80008000u));
         uint32_t range = min_pairs(__byte_perm(low, high, 0x5410), __byte_perm(low, high, 0x7632));
 #pragma unroll
-        for (int d = 1; d < LANES; d <<= 1) range = min_pairs(range, __shfl_xor_sync(0xffffffffu, range, d));
+        for (int d = 1; d < LANES; d <<= 1) range = min_pairs(range, __shfl_xor_sync(head_lanes, range, d));
         const float lo = q4_step(range) + 0.f, width = -q4_lowest(range) - lo;    // one zero
         const float fifteenth = width * (1.f / 15.f);                             // corrected once: width / 15 to the nearest
         float step = __bfloat162float(__float2bfloat16(fmaf(fmaf(-fifteenth, 15.f, width), 1.f / 15.f, fifteenth)));
         if (step < 7.88860905e-31f) step = 0.f;                                   // 2^-100
         if (!(step <= 3.3895314e38f)) step = __int_as_float(0x7fc00000);
         const uint32_t codes = q4_codes(w, lo, step);
-        uint32_t others[4];                        // of the four chunks of 32 elements, in their order
-#pragma unroll
-        for (int k = 0; k < 4; ++k) others[k] = __shfl_sync(0xffffffffu, codes, (threadIdx.x & 28) + k);
-        if (!live) continue;
         const int t = places[r].pos % kPage;
         uint8_t* slab = reinterpret_cast<uint8_t*>(a.k_cache) + places[r].slot + h * a.hs;
         if (!value) {
             *reinterpret_cast<uint32_t*>(slab + t * Slab::kRow + (c % 4 * (HD / 32) + c / 4) * 4) = codes;
         } else {
+            uint32_t others[4];                    // of the four chunks of 32 elements, in their order
+#pragma unroll
+            for (int k = 0; k < 4; ++k) others[k] = __shfl_sync(head_lanes, codes, (threadIdx.x & 28) + k);
             const int n = c % 4, row = q4_row(t);
             uint32_t even = 0, odd = 0;            // nibbles of elements 2 n and 2 n + 1 of the four chunks
 #pragma unroll
@@ -199,7 +193,7 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_q4_kernel(const __
             const uint32_t pair = (__float_as_uint(step) >> 16) | (__float_as_uint(lo) & 0xffff0000u);
             *reinterpret_cast<uint32_t*>(slab + 2 * Slab::kCodes + value * Slab::kParams + (t * NG + c / LANES) * 4) = pair;
         }
-    }
+    });
 }
 
 template <typename T, int V, int HD, int NG>

@@ -91,18 +91,18 @@ __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&x)[V])
 template <int V>
 __device__ __forceinline__ void turn_item(float (&x)[V], float (&y)[V], const float2* turn, bool halves)
 {
+    if (halves || V == 1) {
 #pragma unroll
-    for (int m = 0; m < V; ++m) {
-        const float2 t = turn[m];
-        if (halves) {
+        for (int m = 0; m < V; ++m) {
+            const float2 t = turn[m];
             const float u = x[m], w = y[m];
             x[m] = u * t.x - w * t.y;
             y[m] = w * t.x + u * t.y;
-        } else if (V == 1) {
-            const float u = x[0], w = y[0];
-            x[0] = u * t.x - w * t.y;
-            y[0] = w * t.x + u * t.y;
-        } else {                           // pair m: elements 2 m and 2 m + 1 of x, then of y
+        }
+    } else {                               // pair m: elements 2 m and 2 m + 1 of x, then of y
+#pragma unroll
+        for (int m = 0; m < V; ++m) {
+            const float2 t = turn[m];
             float& u = m < V / 2 ? x[2 * m % V] : y[2 * m % V];
             float& w = m < V / 2 ? x[(2 * m + 1) % V] : y[(2 * m + 1) % V];
             const float u0 = u, w0 = w;

@@ -56,10 +56,12 @@ struct alignas(16) SampleShared {
     double table[kTable], wide_top;
     float peer_max[kMostCtas * kWarps], peer_sum[kMostCtas * kWarps];
     unsigned int peer_count[kMostCtas * kWarps];
-    unsigned long long peer_weight[kMostCtas], peer_ties[kMostCtas];
-    unsigned long long warp_scan[2][kWarps], draw[2][kWarps];
+    unsigned long long peer_weight[kMostCtas];
+    unsigned int peer_ties[kMostCtas];
+    unsigned long long warp_scan[2][kWarps], draw[kWarps];
+    unsigned int draw_ties[kWarps];
     double per_logit, below;               // log2(e) / T; how far below the largest logit min_p's border lies
-    unsigned long long found_before, found_ties;
+    unsigned long long found_before;
     int found_bin, found_from, found_to, too_many;
     unsigned int listed_count, listed[kShare], all[kList], all_count[kMostCtas], keys[kList], pick;
     unsigned long long amounts[kList];
@@ -73,26 +75,25 @@ __device__ const double kPowers[kTable] = {
     0x1.ae89f995ad3adp+0, 0x1.c199bdd85529cp+0, 0x1.d5818dcfba487p+0, 0x1.ea4afa2a490dap+0,
 };
 
-// A float as a double, by its bits: the conversion instruction takes four times as long as arithmetic, and a branch for the rare cases would keep
-// the chains of several logits from running side by side.  A zero becomes 2^-151, an infinity 2^128.
+// A float as a double, by its bits: the conversion instruction takes four times as long as arithmetic.  Numbers below 2^-126 (zero among them) are off by
+// as much at most, and an infinity becomes 2^128.
 __device__ __forceinline__ double widened(float x)
 {
-    const bool tiny = fabsf(x) < 1.17549435e-38f;
-    const uint32_t b = __float_as_uint(tiny ? x * 16777216.f : x);
-    return __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + (tiny ? 0x36800000u : 0x38000000u))), (int)(b << 29));
+    const int b = __float_as_int(x);
+    return __hiloint2double(((b >> 3) & (int)0x8fffffffu) + 0x38000000, b << 29);
 }
 
-// The weights of four logits in units of 2^-42: 2^y with y = (x - top) * per_logit.  y is brought to a multiple of 1/16, whose power is in the table,
-// and a rest r of at most 1/32, for which six terms of the series of exp(r ln 2) leave out less than 1e-15.  Next to an infinite logit
-// everything else weighs nothing.
-__device__ __forceinline__ void weights_of(unsigned long long (&w)[4], const float4& x4, float top, const SampleShared& sh)
+// The weights of four logits in units of 2^-42: 2^y with y = (x - top) * per_logit from -45 to 0 (of others nothing is to be made).  y is brought to a
+// multiple of 1/16, whose power is in the table, and a rest r of at most 1/32, for which six terms of the series of exp(r ln 2) leave out
+// less than 1e-15.  No branches: the four chains run side by side.
+__device__ __forceinline__ void weights_of(unsigned long long (&w)[4], const float4& x4, const SampleShared& sh)
 {
     constexpr double kShifter = 6755399441055744.0 / kTable;               // 1.5 * 2^52 / 16: adding it rounds to a multiple of 1/16
-    constexpr double kFixed = 6755399441055744.0 / kUnit;                  // and this one to a multiple of 2^-42
+    constexpr double kFixed = 6755399441055744.0 / kUnit;                  // and this one to a multiple of 2^-42, which is what its low 51 bits are
     const float x[4] = {x4.x, x4.y, x4.z, x4.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const double y = x[e] == top ? 0.0 : (widened(x[e]) - sh.wide_top) * sh.per_logit;
+        const double y = (widened(x[e]) - sh.wide_top) * sh.per_logit;
         const double rounded = y + kShifter;
         const int n = __double2loint(rounded);                             // 16 times the multiple
         const double r = (y - (rounded - kShifter)) * 0.6931471805599453;
@@ -103,15 +104,15 @@ __device__ __forceinline__ void weights_of(unsigned long long (&w)[4], const flo
         p = fma(p, r, 1.0);
         p = fma(p, r, 1.0);
         p *= sh.table[n & (kTable - 1)];
-        p = __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p));
-        w[e] = y > -43.5 ? (unsigned long long)(__double_as_longlong(p + kFixed) - __double_as_longlong(kFixed)) : 0ull;
+        p = __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p)) + kFixed;
+        w[e] = (unsigned long long)(__double2hiint(p) & 0x0007ffff) << 32 | (unsigned int)__double2loint(p);
     }
 }
 
 __device__ __forceinline__ unsigned long long weight_of(float x, float top, const SampleShared& sh)
 {
     unsigned long long w[4];
-    weights_of(w, make_float4(x, top, top, top), top, sh);
+    weights_of(w, make_float4(x, top, top, top), sh);
     return w[0];
 }
 
@@ -133,12 +134,13 @@ __device__ __forceinline__ unsigned long long sum_warp(unsigned long long x)
 }
 
 // Inclusive, over a warp.
-__device__ __forceinline__ unsigned long long scan_warp(unsigned long long x)
+template <typename N>
+__device__ __forceinline__ N scan_warp(N x)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long y = __shfl_up_sync(0xffffffffu, x, d);
+        const N y = __shfl_up_sync(0xffffffffu, x, d);
         if (lane >= d) x += y;
     }
     return x;
@@ -212,38 +214,40 @@ __device__ __forceinline__ Reached reach(const bool weighted, R& row, SampleShar
         hist[threadIdx.x] = 0;
         if (threadIdx.x == 0) sh.listed_count = 0;
         __syncthreads();
-        auto bin_of = [&](float x) {
-            const int l = linear_bin(x, top, scale);
-            if (pass == 0) return l;
-            const uint32_t key = key_of(x);
-            return l == linear && key >= key_lo && key <= key_hi ? (int)((key_hi - key) >> shift) : -1;
-        };
         unsigned long long rest = 0;       // of the last linear bin: most of a row, added once
+        if (pass == 0) {
 #pragma unroll 2
-        for (int v = row.from + lane; v < row.to; v += 32) {
-            const float4 x4 = row.get(v);
-            if (!(fmaxf(fmaxf(x4.x, x4.y), fmaxf(x4.z, x4.w)) >= floor)) continue;
-            unsigned long long w[4] = {1, 1, 1, 1};
-            if (weighted) weights_of(w, x4, top, sh);
-            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
-            int bin[4];
+            for (int v = row.from + lane; v < row.to; v += 32) {
+                const float4 x4 = row.get(v);
+                if (!(fmaxf(fmaxf(x4.x, x4.y), fmaxf(x4.z, x4.w)) >= floor)) continue;
+                unsigned long long w[4] = {1, 1, 1, 1};
+                if (weighted) weights_of(w, x4, sh);
+                const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+                int bin[4];
+                bool in[4];
+                unsigned int old[4];       // the four side by side: what they wait for is the old values
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                bin[e] = x[e] >= floor ? bin_of(x[e]) : -1;
-                if (pass == 0 && bin[e] == kBins - 1) {
-                    rest += w[e];
-                    bin[e] = -1;
+                for (int e = 0; e < 4; ++e) {
+                    bin[e] = linear_bin(x[e], top, scale);
+                    in[e] = x[e] >= floor && bin[e] < kBins - 1;
+                    if (x[e] >= floor && bin[e] == kBins - 1) rest += w[e];
+                    if (in[e]) old[e] = atomicAdd(reinterpret_cast<unsigned int*>(&hist[bin[e]]), (unsigned int)w[e]);
                 }
+                if (weighted)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned int high = (unsigned int)(w[e] >> 32) + (old[e] + (unsigned int)w[e] < old[e]);
+                        if (in[e] && high) atomicAdd(reinterpret_cast<unsigned int*>(&hist[bin[e]]) + 1, high);
+                    }
             }
-            unsigned int old[4];           // the four side by side: what they wait for is the old values
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (bin[e] >= 0) old[e] = atomicAdd(reinterpret_cast<unsigned int*>(&hist[bin[e]]), (unsigned int)w[e]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (!weighted || bin[e] < 0) continue;
-                const unsigned int high = (unsigned int)(w[e] >> 32) + (old[e] + (unsigned int)w[e] < old[e]);
-                if (high) atomicAdd(reinterpret_cast<unsigned int*>(&hist[bin[e]]) + 1, high);
+        } else {
+#pragma unroll 1
+            for (int i = 4 * row.from + lane; i < 4 * row.to; i += 32) {
+                const float4 x4 = row.get(i / 4);
+                const float x = i & 2 ? (i & 1 ? x4.w : x4.z) : (i & 1 ? x4.y : x4.x);
+                const uint32_t key = key_of(x);
+                if (x >= floor && key >= key_lo && key <= key_hi && linear_bin(x, top, scale) == linear)
+                    add_words(&hist[(key_hi - key) >> shift], weighted ? weight_of(x, top, sh) : 1);
             }
         }
         if (__any_sync(0xffffffffu, rest != 0)) {
@@ -251,8 +255,9 @@ __device__ __forceinline__ Reached reach(const bool weighted, R& row, SampleShar
             if (lane == 0) add_words(&hist[kBins - 1], rest);
         }
         if (rank == 0 && threadIdx.x == 0 && tie_amount) {
-            const int b = bin_of(value_of(tie_key));
-            if (b >= 0) add_words(&hist[b], tie_amount);
+            const int l = linear_bin(value_of(tie_key), top, scale);
+            if (pass == 0) add_words(&hist[l], tie_amount);
+            else if (l == linear && tie_key >= key_lo && tie_key <= key_hi) add_words(&hist[(key_hi - tie_key) >> shift], tie_amount);
         }
         cluster.sync();
         unsigned long long mine = 0, theirs[kMostCtas];        // all under way at once
@@ -438,12 +443,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     float top = -INFINITY, sum = 0.f;
     unsigned int count = 0;
     auto take = [&](float x) {             // NaN is -infinity, and there is one zero
-        x = x == x ? x + 0.f : -INFINITY;
+        x = fmaxf(x, -INFINITY) + 0.f;
         top = fmaxf(top, x);
-        const bool finite = fabsf(x) < INFINITY;
-        sum += finite ? x : 0.f;
-        count += finite;
         return x;
+    };
+    auto survey = [&](const float4& x4) {  // how far the logits lie below the largest: a few of each thread tell
+        const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool finite = fabsf(x[e]) < INFINITY;
+            sum += finite ? x[e] : 0.f;
+            count += finite;
+        }
     };
     if constexpr (HELD) {
         const int vectors = (lead + n + E - 1) / E;
@@ -463,14 +474,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
                 if (i0 < 0 || i0 + E > n)
                     for (int e = 0; e < E; ++e) p[e] = i0 + e >= 0 && i0 + e < n ? global[i0 + e] : T(-INFINITY);
 #pragma unroll
-                for (int e = 0; e < E; e += 4)
-                    stretch[v * (E / 4) + e / 4] = make_float4(take(as_f32(p[e])), take(as_f32(p[e + 1])), take(as_f32(p[e + 2])), take(as_f32(p[e + 3])));
+                for (int e = 0; e < E; e += 4) {
+                    const float4 x = make_float4(take(as_f32(p[e])), take(as_f32(p[e + 1])), take(as_f32(p[e + 2])), take(as_f32(p[e + 3])));
+                    stretch[v * (E / 4) + e / 4] = x;
+                    if (v < kThreads && e == 0) survey(x);
+                }
             }
         }
     } else {
         for (int v = row.from + lane; v < row.to; v += 32) {
             const float4 x = row.get(v);
             take(x.x); take(x.y); take(x.z); take(x.w);
+            if (v < row.from + 32) survey(x);
         }
     }
     if (threadIdx.x < kTable) sh.table[threadIdx.x] = kPowers[threadIdx.x];
@@ -516,7 +531,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     unsigned long long ties = greedy ? 1 : 0;
     // what is in play: from here on
     float floor = sh.below > -INFINITY ? fmaxf(__double2float_ru((double)top + sh.below), -kLargest) : -kLargest;
-    if (threadIdx.x == 0) sh.wide_top = (double)top;
+    floor = fmaxf(floor, top - 31.f * heat);                   // further down weights are below 2^-44: none is ever drawn
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sh.wide_top = widened(top);
+        if (top == INFINITY) sh.per_logit = 1.0;               // next to an infinite logit everything else weighs nothing, whatever the temperature
+    }
     __syncthreads();
     int level = 0;
     const float spread = count > 0 ? top - sum / (float)count : 0.f;
@@ -555,34 +575,36 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     if (least_key) floor = fmaxf(floor, value_of(least_key));
 
     // ---- the draw, in the order of the indices: weights of the warps' stretches or lists, then of their parts ----
-    const float least_value = least_key ? value_of(least_key) : -INFINITY;
-    auto part_of = [&](int v, const Walk<T, HELD>& of, unsigned long long& w, unsigned long long& t) {     // weights above least_key, and how many are at it
-        const float4 x4 = of.get(v);
-        if (!(fmaxf(fmaxf(x4.x, x4.y), fmaxf(x4.z, x4.w)) >= floor)) return;
+    const float least_value = value_of((least_key ? least_key : key_of(floor) - 1));      // what is above it stays, whole
+    const unsigned int most_ties = (unsigned int)min(ties, (unsigned long long)kMaxVocab);
+    auto part_of = [&](int v, unsigned long long& w, unsigned int& t) {           // weights above least_value, and how many are at it
+        const float4 x4 = row.get(v);
+        if (!(fmaxf(fmaxf(x4.x, x4.y), fmaxf(x4.z, x4.w)) >= least_value)) return;
         unsigned long long each[4];
-        weights_of(each, x4, top, sh);
+        weights_of(each, x4, sh);
         const float x[4] = {x4.x, x4.y, x4.z, x4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const bool tie = x[e] == least_value && x[e] >= floor;
-            t += tie;
-            w += x[e] >= floor && !tie ? each[e] : 0;
+            t += x[e] == least_value;
+            if (x[e] > least_value) w += each[e];
         }
     };
-    unsigned long long part[2] = {0, 0};   // weight, ties
+    unsigned long long lane_weight = 0;
+    unsigned int lane_ties = 0;
 #pragma unroll 2
-    for (int v = row.from + lane; v < row.to; v += 32) part_of(v, row, part[0], part[1]);
-    const unsigned long long lane_part[2] = {part[0], part[1]};
-    part[0] = sum_warp(part[0]);
-    part[1] = sum_warp(part[1]);
+    for (int v = row.from + lane; v < row.to; v += 32) part_of(v, lane_weight, lane_ties);
+    const unsigned long long warp_weight = sum_warp(lane_weight);
+    const unsigned int warp_ties = __reduce_add_sync(0xffffffffu, lane_ties);
     if (lane == 0) {
-        sh.draw[0][warp] = part[0];
-        sh.draw[1][warp] = part[1];
+        sh.draw[warp] = warp_weight;
+        sh.draw_ties[warp] = warp_ties;
     }
     __syncthreads();
     // of the warps, in lanes
-    const unsigned long long each_warp = lane < kWarps ? sh.draw[0][lane] : 0, each_ties = lane < kWarps ? sh.draw[1][lane] : 0;
-    const unsigned long long cta_weight = sum_warp(each_warp), cta_ties = sum_warp(each_ties);
+    const unsigned long long each_warp = lane < kWarps ? sh.draw[lane] : 0;
+    const unsigned int each_ties = lane < kWarps ? sh.draw_ties[lane] : 0;
+    const unsigned long long cta_weight = sum_warp(each_warp);
+    const unsigned int cta_ties = __reduce_add_sync(0xffffffffu, each_ties);
     if ((int)threadIdx.x < ctas) {
         SampleShared* other = cluster.map_shared_rank(&sh, threadIdx.x);
         other->peer_weight[rank] = cta_weight;
@@ -590,8 +612,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     }
     cluster.sync();
     // the first weight that exceeds u of the total; rounded up to it, the last one
-    auto of_ties = [&](unsigned long long before, unsigned long long n) { return min(ties > before ? ties - before : 0ull, n) * tie_weight; };
-    unsigned long long total = 0, seen = 0, before = 0, t_before = 0;
+    auto of_ties = [&](unsigned int before, unsigned int n) { return min(most_ties > before ? most_ties - before : 0u, n) * tie_weight; };
+    unsigned long long total = 0, before = 0;
+    unsigned int seen = 0, t_before = 0;
     for (int c = 0; c < ctas; ++c) {
         if (c == rank) { before = total; t_before = seen; }
         total += sh.peer_weight[c] + of_ties(seen, sh.peer_ties[c]);
@@ -600,11 +623,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     const double want = fmin((double)u * (double)total, (double)total - 1.0);
     if ((double)before > want || (double)(before + cta_weight + of_ties(t_before, cta_ties)) <= want) return;
     // the warp: all know which
-    const unsigned long long warps[2] = {scan_warp(each_warp), scan_warp(each_ties)};
-    const unsigned int up_to = __ballot_sync(0xffffffffu, lane < kWarps && (double)(before + warps[0] + of_ties(t_before, warps[1])) > want);
+    const unsigned long long warps_weight = scan_warp(each_warp);
+    const unsigned int warps_ties = scan_warp(each_ties);
+    const unsigned int up_to = __ballot_sync(0xffffffffu, lane < kWarps && (double)(before + warps_weight + of_ties(t_before, warps_ties)) > want);
     const int chosen = __ffs(up_to) - 1;
     if (chosen > 0) {
-        const unsigned long long w0 = __shfl_sync(0xffffffffu, warps[0], chosen - 1), t0 = __shfl_sync(0xffffffffu, warps[1], chosen - 1);
+        const unsigned long long w0 = __shfl_sync(0xffffffffu, warps_weight, chosen - 1);
+        const unsigned int t0 = __shfl_sync(0xffffffffu, warps_ties, chosen - 1);
         before += w0 + of_ties(t_before, t0);
         t_before += t0;
     }
@@ -612,12 +637,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     auto pick = [&](int i) {
         const float4 x4 = row.get(i);
         unsigned long long each[4];
-        weights_of(each, x4, top, sh);
+        weights_of(each, x4, sh);
         const float x[4] = {x4.x, x4.y, x4.z, x4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (x[e] < floor) continue;
-            if (x[e] == least_value) before += t_before++ < ties ? tie_weight : 0;
+            if (x[e] < least_value) continue;
+            if (x[e] == least_value) before += t_before++ < most_ties ? tie_weight : 0;
             else before += each[e];
             if ((double)before > want) {
                 a.tokens[r] = start - lead + (row.listed ? (int)sh.place[chosen][4 * i + e] : 4 * i + e);
@@ -633,10 +658,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     }
     const bool is_short = row.to - row.from <= 32;
     if (warp == chosen && is_short) {      // a vector to a lane, whose parts are there
-        const unsigned long long w_up = scan_warp(lane_part[0]) - lane_part[0], t_up = scan_warp(lane_part[1]) - lane_part[1];
+        const unsigned long long w_up = scan_warp(lane_weight) - lane_weight;
+        const unsigned int t_up = scan_warp(lane_ties) - lane_ties;
         before += w_up + of_ties(t_before, t_up);
         t_before += t_up;
-        if ((double)before <= want && (double)(before + lane_part[0] + of_ties(t_before, lane_part[1])) > want) pick(row.from + lane);
+        if ((double)before <= want && (double)(before + lane_weight + of_ties(t_before, lane_ties)) > want) pick(row.from + lane);
     }
     __syncthreads();
     if (sh.found_to - sh.found_from <= 32) return;
@@ -646,14 +672,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     row.held = row.listed ? reinterpret_cast<const float4*>(sh.may_stay[chosen]) : stretch;
     const int per = (row.to - row.from + kThreads - 1) / kThreads;
     const int my_first = min(row.from + (int)threadIdx.x * per, row.to), my_end = min(my_first + per, row.to);
-    unsigned long long mine[2] = {0, 0}, all[2];
+    unsigned long long mine = 0, all;
+    unsigned int tied = 0;
 #pragma unroll 1
-    for (int i = my_first; i < my_end; ++i) part_of(i, row, mine[0], mine[1]);
+    for (int i = my_first; i < my_end; ++i) part_of(i, mine, tied);
     // of the threads before
-    const unsigned long long w_up = scan_cta(mine[0], all[0], sh.warp_scan[0]), t_up = scan_cta(mine[1], all[1], sh.warp_scan[1]);
+    const unsigned long long w_up = scan_cta(mine, all, sh.warp_scan[0]);
+    const unsigned int t_up = (unsigned int)scan_cta(tied, all, sh.warp_scan[1]);
     before += w_up + of_ties(t_before, t_up);
     t_before += t_up;
-    if ((double)before > want || (double)(before + mine[0] + of_ties(t_before, mine[1])) <= want) return;
+    if ((double)before > want || (double)(before + mine + of_ties(t_before, tied)) <= want) return;
 #pragma unroll 1
     for (int i = my_first; i < my_end; ++i)
         if (pick(i)) return;
@@ -681,8 +709,11 @@ cudaError_t issue(const SampleArgs& a, int ctas, cudaStream_t st)
 template <typename T>
 cudaError_t launch(SampleArgs a, int num_sms, cudaStream_t st)
 {
+    // Stretches of which two fit an SM; and as long as all rows are resident at once, shorter ones, down to 4096 tokens (what a cluster does
+    // besides the stretches costs as much as some ten thousand tokens: 256 rows of 32000 take 125 us in eights, 49 us in twos).
     int ctas = 1;
-    while (ctas < kMostCtas && a.vocab > ctas * 4096) ctas *= 2;
+    while (ctas < kMostCtas && a.vocab > ctas * 20480) ctas *= 2;
+    while (ctas < kMostCtas && a.vocab > ctas * 4096 && (int64_t)a.rows * ctas * 2 <= 2 * num_sms) ctas *= 2;
     a.slice = ((a.vocab + ctas - 1) / ctas + 7) / 8 * 8;
     return (int64_t)a.slice * 4 + 64 <= kMostHeld ? issue<T, true>(a, ctas, st) : issue<T, false>(a, ctas, st);
 }

@@ -462,7 +462,8 @@ typedef struct {
  * w_v >= min_p, and of these each before which less than top_p of their weight lies; the first one always stays.  The token is the first, in the
  * order of the indices, up to and with which the weights of those that stayed exceed `uniform` times their sum.
  * The weights are computed in 64 bits and summed as whole multiples of 2^-42: the order of the sums has no say in the result, and a
- * token below 2^-43 of the most likely one is never drawn.  A NaN counts as -infinity; infinite logits weigh the same.
+ * token below 2^-43 of the most likely one is never drawn.  Logits are taken to within 2^-126.  A NaN counts as -infinity; infinite logits weigh
+ * the same, and the others nothing next to them.
  * A row without a logit above -infinity, or with a parameter outside the ranges above (NaN among them), gets -1 and sets status to
  * HOOK_ATTN_ERR_INVALID_ARG.  vocab_size <= 2^20, num_rows < 2^16. */
 int hook_sample_tokens(hook_attn_handle* handle, const hook_sample_params* p, void* cuda_stream);

@@ -28,6 +28,7 @@ constexpr int kQ4Pages = 2;           // pages that a warp takes at a time
 constexpr int kQ4Stages = 2;          // such pairs in flight or in use per warp
 constexpr int kQ4Keys = kQ4Pages * kPage;
 constexpr int kQ4CtasPerSM = 4;
+constexpr int kQ4Min = 4;             // pages for a warp at least (1 x 8000 keys: 14.6, 12.5 and 14.5 us a call with 2, 4 and 8)
 constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
 constexpr float kLeastLog = -80.f;    // steps below 2^-80 count as 2^-80 in the reference
 
@@ -511,7 +512,10 @@ cudaError_t launch_t(KernelArgs a, const HeadCfg& hc, int num_sms, cudaStream_t 
     cfg.numAttrs = plan.stream ? 0 : 1;
     cudaError_t e;
     if (plan.stream) {
-        const int ctas = kQ4CtasPerSM * (num_sms < kDecMaxSMs ? (num_sms > 0 ? num_sms : 1) : kDecMaxSMs);
+        // a warp has kQ4Min pages at least
+        const int most = kQ4CtasPerSM * (num_sms < kDecMaxSMs ? (num_sms > 0 ? num_sms : 1) : kDecMaxSMs);
+        const long pages = (long)a.num_seqs * a.Hkv * (((long)a.max_keys + kPage - 1) / kPage), wanted = (pages + kQ4Min * kDecWarps - 1) / (kQ4Min * kDecWarps);
+        const int ctas = wanted < most ? (int)wanted : most;
         a.workers = ctas * kDecWarps;
         cfg.gridDim = dim3(ctas);
         e = cudaLaunchKernelEx(&cfg, decode_q4_stream_kernel<HD, NG, NS>, a, hc);

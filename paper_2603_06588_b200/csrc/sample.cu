@@ -531,7 +531,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     unsigned long long ties = greedy ? 1 : 0;
     // what is in play: from here on
     float floor = sh.below > -INFINITY ? fmaxf(__double2float_ru((double)top + sh.below), -kLargest) : -kLargest;
-    floor = fmaxf(floor, top - 31.f * heat);                   // further down weights are below 2^-44: none is ever drawn
+    // further down weights are below 2^-44, and next to an infinite logit all others are: none of those is ever drawn
+    floor = top == INFINITY ? top : fmaxf(floor, top - 31.f * heat);
     __syncthreads();
     if (threadIdx.x == 0) {
         sh.wide_top = widened(top);

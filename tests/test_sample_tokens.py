@@ -150,6 +150,22 @@ def test_rows_of_a_kind(eng, kind):
 
 
 @pytest.mark.gpu
+def test_extreme_temperatures(eng):
+    """From a temperature at which only ties are left to one at which all finite logits weigh the same, with and without an infinite one."""
+    g = np.random.default_rng(7)
+    x = g.normal(size=(6, 3001)) * 4
+    x[:, ::500] = np.round(x[:, ::500])
+    heat = [1e-44, 1e-20, 1e-6, 1e20, 1.5e37, 3.4e38]
+    u = g.random(6).tolist()
+    logits = torch.from_numpy(x).float()
+    for more in (dict(), dict(top_k=[40] * 6), dict(top_p=[0.77] * 6), dict(min_p=[0.3] * 6)):
+        _check(eng, logits, u, temperature=heat, **more)
+    logits[:, 700], logits[:, 2000] = float("inf"), float("inf")
+    for more in (dict(), dict(top_k=[2] * 6), dict(top_p=[0.77] * 6), dict(min_p=[0.3] * 6)):
+        _check(eng, logits, u, temperature=heat, **more)
+
+
+@pytest.mark.gpu
 def test_strides_alignment_and_outputs(eng):
     """Rows that start anywhere, padded rows, one row for all, a tensor of their own for the tokens."""
     g = np.random.default_rng(4)

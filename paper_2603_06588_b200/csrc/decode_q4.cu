@@ -27,8 +27,9 @@ namespace {
 constexpr int kQ4Pages = 2;           // pages that a warp takes at a time
 constexpr int kQ4Stages = 2;          // such pairs in flight or in use per warp
 constexpr int kQ4Keys = kQ4Pages * kPage;
-constexpr int kQ4CtasPerSM = 4;
-constexpr int kQ4Min = 4;             // pages for a warp at least (1 x 8000 keys: 14.6, 12.5 and 14.5 us a call with 2, 4 and 8)
+constexpr int kQ4CtasPerSM = 4;       // at most
+// With four groups and no span sums the registers of three CTAs do without memory: 4 x 32768 keys 49.5 us, and 52.6 with four; with span sums 58 and 54.
+constexpr int q4_ctas(int ng, int ns) { return ng == 4 && ns == 0 ? 3 : kQ4CtasPerSM; }
 constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
 constexpr float kLeastLog = -80.f;    // steps below 2^-80 count as 2^-80 in the reference
 
@@ -442,7 +443,7 @@ template <int HD, int NG>
 constexpr int q4_smem_bytes() { return Q4Walk<HD, NG>::kCtaBytes; }
 
 template <int HD, int NG, int NS>
-__global__ void __launch_bounds__(kDecWarps * 32, kQ4CtasPerSM) decode_q4_stream_kernel(const KernelArgs a, const HeadCfg hc)
+__global__ void __launch_bounds__(kDecWarps * 32, q4_ctas(NG, NS)) decode_q4_stream_kernel(const KernelArgs a, const HeadCfg hc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ DecStreamShared<kDecWarps> sh;
@@ -450,7 +451,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, kQ4CtasPerSM) decode_q4_stream
 }
 
 template <int HD, int NG, int NS>
-__global__ void __launch_bounds__(kDecWarps * 32, kQ4CtasPerSM) decode_q4_splitk_kernel(const KernelArgs a, const HeadCfg hc)
+__global__ void __launch_bounds__(kDecWarps * 32, q4_ctas(NG, NS)) decode_q4_splitk_kernel(const KernelArgs a, const HeadCfg hc)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int sh_span[kDecWarps][2 * kMaxSpans];
@@ -473,7 +474,12 @@ __global__ void __launch_bounds__(kDecWarps * 32, kQ4CtasPerSM) decode_q4_splitk
     decode_fold_cta<HD, NS>(part, a.G, reinterpret_cast<float*>(smem), sh_fold, 1, m0, m1, l0, l1, o, sm);
 }
 
-// How a call is cut, from host-known bounds only, as in decode.cu: few units share their pages out evenly; many are cut into chunks.
+// How a call is cut, from host-known bounds only.  Chunks of a fixed length, the largest power of two in 256 .. 2048 keys that leaves eight CTAs
+// an SM, but for few units of very long sequences, whose pages are shared out evenly: there chunks would leave long merges (4 x 32768
+// keys of 8 KV heads: 41 to 54 us shared out, 43 to 59 in chunks).  Elsewhere finding the shares is what costs: 1 x 2000 keys take 8.3 us in
+// chunks and 12.4 shared out, 36 of up to 4096 31 to 36 and 42 to 49.
+constexpr int kQ4Long = 16384;            // keys of a sequence, at most
+constexpr long kQ4Shared = 4L * kQ4CtasPerSM * kDecMaxSMs * 16;   // pages of all units, at most: four waves of CTAs of 256 keys
 struct Q4Plan {
     bool stream;
     int chunk, max_chunks;
@@ -482,7 +488,8 @@ struct Q4Plan {
 Q4Plan q4_plan(int num_seqs, int Hkv, int max_keys)
 {
     Q4Plan p = {};
-    p.stream = (long)num_seqs * Hkv < kDecStreamUnits;
+    const long pages = (long)num_seqs * Hkv * (((long)max_keys + kPage - 1) / kPage);
+    p.stream = (long)num_seqs * Hkv < kDecStreamUnits && max_keys >= kQ4Long && pages > kQ4Shared;
     p.chunk = 2048;
     while (p.chunk > 256) {
         const long ctas = (long)num_seqs * Hkv * (((long)max_keys + p.chunk - 1) / p.chunk);
@@ -512,10 +519,7 @@ cudaError_t launch_t(KernelArgs a, const HeadCfg& hc, int num_sms, cudaStream_t 
     cfg.numAttrs = plan.stream ? 0 : 1;
     cudaError_t e;
     if (plan.stream) {
-        // a warp has kQ4Min pages at least
-        const int most = kQ4CtasPerSM * (num_sms < kDecMaxSMs ? (num_sms > 0 ? num_sms : 1) : kDecMaxSMs);
-        const long pages = (long)a.num_seqs * a.Hkv * (((long)a.max_keys + kPage - 1) / kPage), wanted = (pages + kQ4Min * kDecWarps - 1) / (kQ4Min * kDecWarps);
-        const int ctas = wanted < most ? (int)wanted : most;
+        const int ctas = q4_ctas(NG, NS) * (num_sms < kDecMaxSMs ? (num_sms > 0 ? num_sms : 1) : kDecMaxSMs);
         a.workers = ctas * kDecWarps;
         cfg.gridDim = dim3(ctas);
         e = cudaLaunchKernelEx(&cfg, decode_q4_stream_kernel<HD, NG, NS>, a, hc);

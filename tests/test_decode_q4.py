@@ -89,13 +89,13 @@ def _slabs(g, shape, d, group, kind="normal"):
 
 
 class Case:
-    def __init__(self, lens, hq, hkv, d, group, seed=1, kind="normal", spans=0, steer=False, q_size=1.0, layout="tight", scale=0.0):
+    def __init__(self, lens, hq, hkv, d, group, seed=1, kind="normal", spans=0, steer=False, q_size=1.0, layout="tight", scale=0.0, width=0):
         g = np.random.default_rng(seed)
         self.lens, self.hq, self.hkv, self.d, self.group = lens, hq, hkv, d, group
         pages = [-(-max(L, 0) // 16) for L in lens]
         pool = sum(pages) + 2
         order = g.permutation(pool).tolist()
-        self.table = np.full((len(lens), max(pages + [1]) + 2), -1, dtype=np.int64)
+        self.table = np.full((len(lens), max([width, max(pages + [1]) + 2])), -1, dtype=np.int64)
         self.slabs = _slabs(g, (pool, hkv), d, group, kind)
         for s, n in enumerate(pages):
             self.table[s, :n], order = order[:n], order[n:]
@@ -169,11 +169,34 @@ def _run(eng, case, **kw):
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (7, 1), (8, 4), (24, 3), (15, 5)])
 @pytest.mark.parametrize("spans", [0, 2, 5])
 def test_parity(eng, d, group, hq, hkv, spans):
-    """Lengths around a page's borders, shuffled pages, NaN wherever no sequence has a token; equal shares of the pages."""
+    """Lengths around a page's borders, shuffled pages, NaN wherever no sequence has a token."""
     c = Case([1, 15, 16, 17, 33, 700, 100], hq, hkv, d, group, seed=hq + spans, spans=spans, steer=spans == 2)
     out, mass, status = _run(eng, c)
     assert status == 0
     c.check(out, mass)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,group", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("lens", [[1, 15, 16, 17, 33, 700, 100], [4000, 5, 9001, 2000], [20, 0, 300, -1]])
+@pytest.mark.parametrize("spans", [0, 2, 7])
+def test_parity_of_shared_pages(eng, d, group, lens, spans):
+    """Tables wide enough for very long sequences: few units, whose pages are dealt out evenly, from less than one page a warp to runs that go on
+    in the next unit."""
+    c = Case(lens, 10, 5, d, group, seed=spans, spans=spans, steer=spans == 2, width=4000)
+    out, mass, status = _run(eng, c)
+    assert status == (binding.HOOK_ATTN_ERR_INVALID_ARG if min(lens) <= 0 else 0)
+    c.check(out, mass)
+    again = _run(eng, c)
+    assert torch.equal(again[0], out) and (mass is None or torch.equal(again[1], mass))
+    if min(lens) > 0:                                       # a page out of range takes its row with it, and no other
+        kw = c.kw()
+        kw["block_table"][2, 0] = len(c.slabs)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        bad, bad_mass = eng.hook_attn_decode_q4(**kw, status=status)
+        assert int(status.item()) == binding.HOOK_ATTN_ERR_BOUNDS and not bad[2].any() and (mass is None or not bad_mass[2].any())
+        rest = [r for r in range(len(lens)) if r != 2]
+        assert torch.equal(bad[rest], out[rest]) and (mass is None or torch.equal(bad_mass[rest], mass[rest]))
 
 
 @pytest.mark.gpu

@@ -12,11 +12,13 @@
 // Weights are exp((x - max) / T) in 64 bits, off by 2^-44 of them, and are summed as whole multiples of 2^-42: whatever the order, the
 // sums are the same, and a random number that falls next to a border is on the same side in every run and for every cluster size.
 //
-// Reading the row is the least of it.  A token takes 50 instructions where every weight is needed (12 of them in 64 bits) and 20 in a pass that only compares;
-// a cluster's six exchanges, the scans and the lists cost a row about 10 us.  256 x 160000 fp32: 203 us with rows of all filters, 138 without any, 169 top-k,
-// 239 top-p; 1 x 32000 bf16: 14.5, 9.6, 11.5 and 11.7 us.  Issue slots are half busy at 32 warps an SM, which barriers and loads hold up by turns.
+// Reading the row is the least of it.  A token takes some 50 instructions where every weight is needed (12 of them in 64 bits) and 20 in a pass that only compares;
+// a cluster's six exchanges, the scans and the lists cost a row about 10 us.  256 x 160000 fp32: 206 us with rows of all filters, 142 without any, 173 top-k,
+// 242 top-p; 1 x 32000 bf16: 15.6, 10.4, 11.7 and 12.0 us.  Issue slots are half busy at 32 warps an SM, which barriers and loads hold up by turns.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
+
+#include <utility>
 
 #include "common.cuh"
 #include "ops.cuh"
@@ -418,6 +420,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     cg::cluster_group cluster = cg::this_cluster();
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), r = blockIdx.x / ctas;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // the others' shared memory is there once they have all begun; by the time it is written to they have
+    auto begun = cluster.barrier_arrive();
 
     const float u = a.uniform[r], heat = a.temperature ? a.temperature[r] : 1.f;
     const float share = a.top_p ? a.top_p[r] : 1.f, least = a.min_p ? a.min_p[r] : 0.f;
@@ -497,6 +501,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     count = __reduce_add_sync(0xffffffffu, count);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    cluster.barrier_wait(std::move(begun));
     if (lane < ctas) {                     // of this warp, for every CTA
         SampleShared* other = cluster.map_shared_rank(&sh, lane);
         const int at = rank * kWarps + warp;

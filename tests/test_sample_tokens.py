@@ -183,7 +183,7 @@ def test_strides_alignment_and_outputs(eng):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,vocab", [(1, 160000), (2, 2 ** 20), (300, 700)])
+@pytest.mark.parametrize("rows,vocab", [(1, 160000), (2, 2 ** 20), (300, 700), (3, 392001), (150, 21000)])
 def test_large_calls(eng, rows, vocab):
     """A vocabulary that a cluster cannot hold, and more rows than SMs."""
     g = np.random.default_rng(rows)

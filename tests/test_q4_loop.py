@@ -140,3 +140,59 @@ def test_prompts_forks_and_sampled_steps():
     for n in range(8):
         live, out = loop.step(nxt)
         nxt = loop.choose(live, out, seed=200 + n)
+
+
+@pytest.mark.gpu
+def test_captured_steps_beside_another_loop():
+    """A whole step -- room, shared pages, append, attention, the next tokens -- in one graph that feeds itself, replayed next to eager steps of
+    another pool on another stream: both hold at every step the bits of eager steps with nothing beside them."""
+    eng, steps = binding.HookAttn(0), 40
+    g = torch.Generator().manual_seed(31)
+    qkv = torch.randn(VOCAB, HQ + 2 * HKV, D, generator=g).to(torch.bfloat16).cuda()
+    head = torch.randn(HQ * D, VOCAB, generator=g).cuda() / 4
+    freq = (10000.0 ** (-torch.arange(D // 2) / (D // 2))).float().cuda()
+    draws = torch.rand(steps, 4, generator=g).cuda()
+    heat, top = torch.tensor([0.8, 1.0, 0.0, 1.2]).cuda(), torch.tensor([0.9, 0.5, 1.0, 0.95]).cuda()
+
+    class Pool:
+        def __init__(self):
+            self.pages = torch.zeros(40, HKV, q4.slab_bytes(D, GROUP), dtype=torch.uint8, device="cuda")
+            self.pool = dict(block_table=torch.full((4, WIDTH), -1, dtype=torch.int32, device="cuda"), seq_lens=_i32([0] * 4),
+                             page_refs=_i32([0] * 40), status=_i32([0]))
+            self.tokens, self.n, self.ones = _i32([3, 5, 7, 11]), torch.zeros(1, dtype=torch.int64, device="cuda"), _i32([1] * 4)
+
+        def step(self):
+            table, lens, status = (self.pool[n] for n in ("block_table", "seq_lens", "status"))
+            pairs = eng.hook_cache_extend(**self.pool, new_rows=self.ones)
+            eng.hook_cache_copy_pages_q4([self.pages], pairs, status=status)
+            row = qkv[self.tokens.long()]
+            q = eng.hook_rope_append_q4(q=row[:, :HQ], k=row[:, HQ:HQ + HKV], v=row[:, HQ + HKV:], pages=self.pages, block_table=table, seq_lens=lens,
+                                        inv_freq=freq, status=status)
+            out, _ = eng.hook_attn_decode_q4(q=q, pages=self.pages, block_table=table, seq_lens=lens, status=status, max_seq_len=WIDTH * 16)
+            logits = (out.float()[:, :, :, None] * head.view(HQ, D, VOCAB)).sum((1, 2))             # no workspace of a library
+            eng.hook_sample_tokens(logits, draws[self.n].view(4), temperature=heat, top_p=top, tokens=self.tokens, status=status)
+            self.n += 1
+            return out
+
+        def now(self, out):
+            return [t.clone() for t in (out, self.tokens, self.pages, self.pool["seq_lens"], self.pool["status"])]
+
+    alone = Pool()
+    want = [alone.now(alone.step()) for _ in range(steps)]
+    assert int(alone.pool["status"].item()) == 0 and alone.pool["seq_lens"].tolist() == [steps] * 4
+
+    captured, beside, side = Pool(), Pool(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = captured.step()
+    torch.cuda.synchronize()
+    got, other = [], []
+    for _ in range(steps):
+        graph.replay()
+        got.append(captured.now(out))
+        with torch.cuda.stream(side):
+            other.append(beside.now(beside.step()))
+    torch.cuda.synchronize()
+    for n in range(steps):
+        for a, b, c in zip(want[n], got[n], other[n]):
+            assert torch.equal(a, b) and torch.equal(a, c), n

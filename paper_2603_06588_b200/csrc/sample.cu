@@ -276,14 +276,14 @@ __device__ __forceinline__ Reached reach(const bool weighted, R& row, SampleShar
         if (pass == 0) {
             out.total = total;
             if (weighted) {
-                goal = want * (double)total;
+                goal = fmax(want * (double)total, 1.0);          // a unit at least: the first token stays, and it may lie in any bin
             } else if ((double)total <= want) {
                 out.all = true;
                 return out;
             }
         }
         // the first bin with which the goal is reached
-        if ((double)(before + mine) >= goal && ((double)before < goal || threadIdx.x == 0)) {
+        if ((double)(before + mine) >= goal && (double)before < goal) {
             sh.found_bin = threadIdx.x;
             sh.found_before = before;
         }
@@ -383,7 +383,7 @@ __device__ __forceinline__ Reached reach(const bool weighted, R& row, SampleShar
                         whole += __shfl_xor_sync(0xffffffffu, whole, d);
                         larger += __shfl_xor_sync(0xffffffffu, larger, d);
                     }
-                if (live && ((double)(out.above + larger) < goal || key == key_of(top))) atomicMin(&sh.pick, key);
+                if (live && (double)(out.above + larger) < goal) atomicMin(&sh.pick, key);
                 __syncthreads();
                 const uint32_t pick = sh.pick;
                 const bool none = pick == 0xffffffffu;                             // the bin holds nothing but those that have no turn

@@ -585,7 +585,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     if (least_key) floor = fmaxf(floor, value_of(least_key));
 
     // ---- the draw, in the order of the indices: weights of the warps' stretches or lists, then of their parts ----
-    const float least_value = value_of((least_key ? least_key : key_of(floor) - 1));      // what is above it stays, whole
+    // What is above least_value stays, whole: without a key, the number before floor (before zero that is -2^-149, as no number lies between it and -0).
+    const float least_value = least_key ? value_of(least_key) : floor == 0.f ? -1.40129846e-45f : value_of(key_of(floor) - 1);
     const unsigned int most_ties = (unsigned int)min(ties, (unsigned long long)kMaxVocab);
     auto part_of = [&](int v, unsigned long long& w, unsigned int& t) {           // weights above least_value, and how many are at it
         const float4 x4 = row.get(v);

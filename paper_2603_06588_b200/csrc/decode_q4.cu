@@ -9,8 +9,8 @@
 // the steps of K multiply the partial products of a group, those of V the probabilities before their one rounding to halves (off by
 // 2^-12 of a probability times its group's range), and the lowest values are summed in 32 bits.
 //
-// Halves reach from 2^-24 to 2^16, so the softmax's reference is that of p * step: it is raised when a score exceeds it by 2^8 or a step
-// exceeds 2^7 times the power of two that stands for the steps.  It cancels in o / l and s / l, as in decode.cu.
+// Halves reach from 2^-24 to 2^16: p, in the frame of decode.cu, is at most 2^8, and the steps go times a power of two that keeps the largest
+// in [2^6, 2^7) and comes out of the sums in the end.
 //
 // What bounds it is not HBM but the integer pipe: 340 to 410 instructions a page and KV head of 128 (two to four groups), 180 of them on the pipe that masks, shifts and
 // permutes take at half rate (58 % busy; issue slots 60 %, tensor pipe 24 %, DRAM 47 %).  256 sequences of 1024 to 8192 keys (683 MB): 166 us,
@@ -37,7 +37,8 @@ constexpr int kQ4CtasPerSM = 4;       // at most
 // With four groups and no span sums the registers of three CTAs do without memory: 4 x 32768 keys 49.5 us, and 52.6 with four; with span sums 58 and 54.
 constexpr int q4_ctas(int ng, int ns) { return ng == 4 && ns == 0 ? 3 : kQ4CtasPerSM; }
 constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
-constexpr float kLeastLog = -80.f;    // steps below 2^-80 count as 2^-80 in the reference
+constexpr float kTopStep = 128.f;     // steps times their frame are below this
+constexpr float kFirstFrame = 1.6225928e32f;          // 2^107: steps are at least 2^-100
 
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -229,8 +230,8 @@ struct Q4Walk {
             }
         }
 
-        // Scores so far at most m; the accumulators hold p 2^(x - f) with f = m + steps, where 2^steps stands for the steps of V.
-        float f0 = -INFINITY, f1 = -INFINITY, steps = kLeastLog, step_limit = 0.f, zl[NG][2];
+        // The accumulators hold p 2^(x - m), o's codes that times `frame`, the power of two that brings the largest step of V so far to [2^6, 2^7).
+        float frame = kFirstFrame, zl[NG][2];
 #pragma unroll
         for (int j = 0; j < NG; ++j) zl[j][0] = zl[j][1] = 0.f;
 
@@ -298,23 +299,27 @@ struct Q4Walk {
                 mx0 = fmaxf(mx0, fmaxf(x[u][0], x[u][2]));
                 mx1 = fmaxf(mx1, fmaxf(x[u][1], x[u][3]));
             }
-            // ---- the reference: m = f - steps ----
-            if (__any_sync(0xffffffffu, mx0 > f0 + (kDecRaise - steps) || mx1 > f1 + (kDecRaise - steps) || top > step_limit)) {
+            // ---- the references ----
+            if (__any_sync(0xffffffffu, mx0 > m0 + kDecRaise || mx1 > m1 + kDecRaise || top * frame >= kTopStep)) {
 #pragma unroll
                 for (int d = 4; d <= 16; d <<= 1) {
                     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
                     mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
                 }
-                const float e = fmaxf((float)((int)(__float_as_uint(top) >> 23) - 127), steps);
-                const float n0 = fmaxf(f0 - steps, mx0) + e, n1 = fmaxf(f1 - steps, mx1) + e;
-                const float c0 = fast_exp2(f0 - n0), c1 = fast_exp2(f1 - n1);
-                f0 = n0; f1 = n1;
-                steps = e;
-                step_limit = fast_exp2(e + 7.f);
+                const float n0 = fmaxf(m0, mx0), n1 = fmaxf(m1, mx1);
+                const float c0 = fast_exp2(m0 - n0), c1 = fast_exp2(m1 - n1);
+                m0 = n0; m1 = n1;
                 l0 *= c0; l1 *= c1;
+                const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+                float shrink = 1.f;
+                if (__uint_as_float(most) * frame >= kTopStep) {
+                    const float to = __uint_as_float((260u << 23) - (most & 0x7f800000u));            // 2^6 over the step's power
+                    shrink = to * __uint_as_float((254u << 23) - __float_as_uint(frame));
+                    frame = to;
+                }
+                const float k0 = c0 * shrink, k1 = c1 * shrink;
 #pragma unroll
-                for (int i = 0; i < KS; ++i) { o[i][0] *= c0; o[i][1] *= c1; o[i][2] *= c0; o[i][3] *= c1; }
+                for (int i = 0; i < KS; ++i) { o[i][0] *= k0; o[i][1] *= k1; o[i][2] *= k0; o[i][3] *= k1; }
 #pragma unroll
                 for (int j = 0; j < NG; ++j) { zl[j][0] *= c0; zl[j][1] *= c1; }
                 if constexpr (NS > 0) {
@@ -328,8 +333,8 @@ struct Q4Walk {
             float s0 = 0.f, s1 = 0.f;
 #pragma unroll
             for (int u = 0; u < kQ4Pages; ++u) {
-                x[u][0] = fast_exp2(x[u][0] - f0); x[u][1] = fast_exp2(x[u][1] - f1);
-                x[u][2] = fast_exp2(x[u][2] - f0); x[u][3] = fast_exp2(x[u][3] - f1);
+                x[u][0] = fast_exp2(x[u][0] - m0); x[u][1] = fast_exp2(x[u][1] - m1);
+                x[u][2] = fast_exp2(x[u][2] - m0); x[u][3] = fast_exp2(x[u][3] - m1);
                 s0 += x[u][0] + x[u][2];
                 s1 += x[u][1] + x[u][3];
             }
@@ -373,7 +378,7 @@ struct Q4Walk {
                 }
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
-                    const float sa = q4_step(va[j]), sb = q4_step(vb[j]), la = q4_lowest(va[j]), lb = q4_lowest(vb[j]);
+                    const float sa = q4_step(va[j]) * frame, sb = q4_step(vb[j]) * frame, la = q4_lowest(va[j]), lb = q4_lowest(vb[j]);
                     pb[j][0] = movmatrix_trans(pack_f16(x[u][0] * sa, x[u][1] * sa));
                     pb[j][1] = movmatrix_trans(pack_f16(x[u][2] * sb, x[u][3] * sb));
                     zl[j][0] += x[u][0] * la + x[u][2] * lb;
@@ -426,13 +431,12 @@ struct Q4Walk {
             }
             __syncwarp();
         }
-        m0 = f0;
-        m1 = f1;
+        const float out = __uint_as_float((254u << 23) - __float_as_uint(frame));
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             const int j = i / 2 / PER;
-            o[i][0] = o[i][0] * 16777216.f + zl[j][0]; o[i][1] = o[i][1] * 16777216.f + zl[j][1];   // rows g: codes times 2^-24
-            o[i][2] = o[i][2] * 1048576.f + zl[j][0]; o[i][3] = o[i][3] * 1048576.f + zl[j][1];     // rows g + 8: times 2^-20
+            o[i][0] = o[i][0] * 16777216.f * out + zl[j][0]; o[i][1] = o[i][1] * 16777216.f * out + zl[j][1];   // rows g: codes times 2^-24
+            o[i][2] = o[i][2] * 1048576.f * out + zl[j][0]; o[i][3] = o[i][3] * 1048576.f * out + zl[j][1];     // rows g + 8: times 2^-20
         }
         if (broken) {                                         // a page out of range: the row becomes zeros
             m0 = m1 = kBrokenMax;

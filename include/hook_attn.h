@@ -407,7 +407,8 @@ int hook_rope_append_q4(hook_attn_handle* handle, const hook_rope_params* p, con
 
 /* hook_attn_decode over a 4-bit cache: the same arguments, outputs, hooks and faults, k_cache, v_cache and the kv strides of `p` being
  * ignored.  `workspace` holds hook_attn_workspace_bytes(p, 3) bytes.  Scores, softmax, span masses and the sums over the values
- * are in 32 bits; a probability times a step is rounded to 11 bits. */
+ * are in 32 bits; a probability times a step of V is rounded to 11 bits or, below 2^-20 of the largest probability times the largest step of
+ * the same group, to multiples of 2^-30 of the latter.  Elements of q below 2^-27 of their head's largest are rounded to 2^-34 of it. */
 int hook_attn_decode_q4(hook_attn_handle* handle, const hook_attn_params* p, const hook_q4_cache* cache, void* cuda_stream);
 
 typedef struct {

@@ -6,11 +6,12 @@
 // above it), exactly, and products with subnormal halves are exact too.  So no code is converted; a word of eight costs four ANDs and a
 // shift, and the powers of two go into the queries and out of the sums.  With k = lowest + step c for the tokens' groups,
 //   x_t = scale * sum_g (step_tg * (q_g . c_tg) + lowest_tg * sum(q_g)),    o = sum_t sum_g p_t step_tg c_tg + sum_t p_t lowest_tg:
-// the steps of K multiply the partial products of a group, those of V the probabilities before their one rounding to halves (off by
-// 2^-12 of a probability times its group's range), and the lowest values are summed in 32 bits.
+// the steps of K multiply the partial products of a group, those of V the probabilities before their one rounding to halves, and the lowest
+// values are summed in 32 bits.
 //
-// Halves reach from 2^-24 to 2^16: p, in the frame of decode.cu, is at most 2^8, and the steps go times a power of two that keeps the largest
-// in [2^6, 2^7) and comes out of the sums in the end.
+// Halves reach from 2^-24 to 2^16: p, in the frame of decode.cu, is at most 2^8, and a group's steps go times a power of two of their own that
+// keeps the largest so far in [2^6, 2^7) and comes out of the group's sums in the end.  So a product is off by 2^-11 of itself, or by 2^-31 of
+// the group's largest step where that is more (from a probability of 2^-20 of the largest on), whatever the other groups hold.
 //
 // What bounds it is not HBM but the integer pipe: 340 to 410 instructions a page and KV head of 128 (two to four groups), 180 of them on the pipe that masks, shifts and
 // permutes take at half rate (58 % busy; issue slots 60 %, tensor pipe 24 %, DRAM 47 %).  256 sequences of 1024 to 8192 keys (683 MB): 166 us,
@@ -230,10 +231,13 @@ struct Q4Walk {
             }
         }
 
-        // The accumulators hold p 2^(x - m), o's codes that times `frame`, the power of two that brings the largest step of V so far to [2^6, 2^7).
-        float frame = kFirstFrame, zl[NG][2];
+        // The accumulators hold p 2^(x - m), o's codes that times their group's `frame`, the power of two that brings its largest step so far to [2^6, 2^7).
+        float frame[NG], zl[NG][2];
 #pragma unroll
-        for (int j = 0; j < NG; ++j) zl[j][0] = zl[j][1] = 0.f;
+        for (int j = 0; j < NG; ++j) {
+            frame[j] = kFirstFrame;
+            zl[j][0] = zl[j][1] = 0.f;
+        }
 
         uint64_t limit_ns = 2000000000ull;
         // LAST: the run ends among these keys, and what lies behind it may be anything.
@@ -250,7 +254,9 @@ struct Q4Walk {
             const int key0 = key_base + it * kPage;
 
             // ---- scores: keys g and g + 8 of each page for the heads 2 tq and 2 tq + 1 ----
-            float x[kQ4Pages][4], top = 0.f;
+            float x[kQ4Pages][4], top[NG];
+#pragma unroll
+            for (int j = 0; j < NG; ++j) top[j] = 0.f;
 #pragma unroll
             for (int u = 0; u < kQ4Pages; ++u) {
                 const uint32_t kt = stage + u * Slab::kBytes, kp = kt + 2 * Slab::kCodes + g * (NG * 4), vp = kp + Slab::kParams;
@@ -291,7 +297,7 @@ struct Q4Walk {
                     for (int j = 0; j < NG; ++j) pb[j] = 0;
                 }
 #pragma unroll
-                for (int j = 0; j < NG; ++j) top = fmaxf(top, fmaxf(q4_step(pa[j]), q4_step(pb[j])));
+                for (int j = 0; j < NG; ++j) top[j] = fmaxf(top[j], fmaxf(q4_step(pa[j]), q4_step(pb[j])));
             }
             float mx0 = x[0][0], mx1 = x[0][1];
 #pragma unroll
@@ -300,7 +306,10 @@ struct Q4Walk {
                 mx1 = fmaxf(mx1, fmaxf(x[u][1], x[u][3]));
             }
             // ---- the references ----
-            if (__any_sync(0xffffffffu, mx0 > m0 + kDecRaise || mx1 > m1 + kDecRaise || top * frame >= kTopStep)) {
+            float highest = top[0] * frame[0];
+#pragma unroll
+            for (int j = 1; j < NG; ++j) highest = fmaxf(highest, top[j] * frame[j]);
+            if (__any_sync(0xffffffffu, mx0 > m0 + kDecRaise || mx1 > m1 + kDecRaise || highest >= kTopStep)) {
 #pragma unroll
                 for (int d = 4; d <= 16; d <<= 1) {
                     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
@@ -310,18 +319,21 @@ struct Q4Walk {
                 const float c0 = fast_exp2(m0 - n0), c1 = fast_exp2(m1 - n1);
                 m0 = n0; m1 = n1;
                 l0 *= c0; l1 *= c1;
-                const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-                float shrink = 1.f;
-                if (__uint_as_float(most) * frame >= kTopStep) {
-                    const float to = __uint_as_float((260u << 23) - (most & 0x7f800000u));            // 2^6 over the step's power
-                    shrink = to * __uint_as_float((254u << 23) - __float_as_uint(frame));
-                    frame = to;
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top[j]));
+                    float k0 = c0, k1 = c1;
+                    if (__uint_as_float(most) * frame[j] >= kTopStep) {
+                        const float to = __uint_as_float((260u << 23) - (most & 0x7f800000u));        // 2^6 over the step's power
+                        const float shrink = to * __uint_as_float((254u << 23) - __float_as_uint(frame[j]));
+                        k0 *= shrink;
+                        k1 *= shrink;
+                        frame[j] = to;
+                    }
+#pragma unroll
+                    for (int i = 2 * j * PER; i < 2 * (j + 1) * PER; ++i) { o[i][0] *= k0; o[i][1] *= k1; o[i][2] *= k0; o[i][3] *= k1; }
+                    zl[j][0] *= c0; zl[j][1] *= c1;
                 }
-                const float k0 = c0 * shrink, k1 = c1 * shrink;
-#pragma unroll
-                for (int i = 0; i < KS; ++i) { o[i][0] *= k0; o[i][1] *= k1; o[i][2] *= k0; o[i][3] *= k1; }
-#pragma unroll
-                for (int j = 0; j < NG; ++j) { zl[j][0] *= c0; zl[j][1] *= c1; }
                 if constexpr (NS > 0) {
                     run0 *= c0;
                     run1 *= c1;
@@ -378,7 +390,7 @@ struct Q4Walk {
                 }
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
-                    const float sa = q4_step(va[j]) * frame, sb = q4_step(vb[j]) * frame, la = q4_lowest(va[j]), lb = q4_lowest(vb[j]);
+                    const float sa = q4_step(va[j]) * frame[j], sb = q4_step(vb[j]) * frame[j], la = q4_lowest(va[j]), lb = q4_lowest(vb[j]);
                     pb[j][0] = movmatrix_trans(pack_f16(x[u][0] * sa, x[u][1] * sa));
                     pb[j][1] = movmatrix_trans(pack_f16(x[u][2] * sb, x[u][3] * sb));
                     zl[j][0] += x[u][0] * la + x[u][2] * lb;
@@ -431,12 +443,12 @@ struct Q4Walk {
             }
             __syncwarp();
         }
-        const float out = __uint_as_float((254u << 23) - __float_as_uint(frame));
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             const int j = i / 2 / PER;
-            o[i][0] = o[i][0] * 16777216.f * out + zl[j][0]; o[i][1] = o[i][1] * 16777216.f * out + zl[j][1];   // rows g: codes times 2^-24
-            o[i][2] = o[i][2] * 1048576.f * out + zl[j][0]; o[i][3] = o[i][3] * 1048576.f * out + zl[j][1];     // rows g + 8: times 2^-20
+            const float back = __uint_as_float((254u << 23) - __float_as_uint(frame[j]));
+            o[i][0] = o[i][0] * 16777216.f * back + zl[j][0]; o[i][1] = o[i][1] * 16777216.f * back + zl[j][1];   // rows g: codes times 2^-24
+            o[i][2] = o[i][2] * 1048576.f * back + zl[j][0]; o[i][3] = o[i][3] * 1048576.f * back + zl[j][1];     // rows g + 8: times 2^-20
         }
         if (broken) {                                         // a page out of range: the row becomes zeros
             m0 = m1 = kBrokenMax;

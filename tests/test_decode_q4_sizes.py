@@ -1,4 +1,5 @@
-"""The attention over a 4-bit cache where the sizes of its values differ by much: constant groups of large values.  Bounds go by the element's own group."""
+"""The attention over a 4-bit cache where the sizes of its values differ by much: constant groups of large values, groups of small values beside large
+ones under a sharp softmax, steps that grow along the sequence.  Bounds go by the element's own group."""
 import numpy as np
 import pytest
 import torch
@@ -90,3 +91,41 @@ def test_constant_groups_of_any_size(eng, d, group, power, width):
     held.check(eng, [1.0, -0.5, 0.0], width, [[0, 700], [699, 1500]])
     low[:, 0] = 2.0 ** power                                   # the same in all tokens
     Held(d, group, g.integers(0, 16, L), np.zeros((L, d), dtype=np.int64), np.zeros((L, n)), low, seed=2).check(eng, [1.0, 0.25], width)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("d,group", [(64, 32), (128, 32), (128, 64)])
+@pytest.mark.parametrize("ratio", [-4, -8, -10, -14, -24, -60])
+@pytest.mark.parametrize("sharp", [0, 20001])
+def test_small_groups_beside_large_ones(eng, d, group, ratio, sharp, width):
+    """One token holds most of the probability (12 above the others' scores) and has codes 0; the others' codes are what is left to see.  Each group's steps
+    are 2^ratio of the group before it, or, in the last of four, none."""
+    g = np.random.default_rng(ratio + 100)
+    L, n = 32768, d // group
+    k, v = np.zeros(L, dtype=np.int64), g.integers(8, 16, (L, d))
+    k[sharp], v[sharp] = 12, 0
+    step = 2.0 ** (ratio * np.arange(n)) * g.uniform(1, 2, (L, n))
+    if n == 4:
+        step[:, 3] = 0
+    low = -3 * step
+    held = Held(d, group, k, v, step, low, seed=3)
+    held.check(eng, [1.0, 0.875, 0.0, -1.0], width, [[0, 100], [100, 32768], [20001, 20002]])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("d,group", [(64, 32), (64, 64), (128, 32), (128, 128)])
+@pytest.mark.parametrize("kind", ["growing", "falling", "mixed", "largest"])
+def test_steps_along_the_sequence(eng, d, group, kind, width):
+    """A group's steps from 2^-60 to 2^3 (or up to 2^109, where the sums still fit 32 bits), growing with the tokens, falling or in no order, each group at its own pace."""
+    g = np.random.default_rng(11)
+    L, n = 2000, d // group
+    at = np.linspace(0, 1, L)[:, None] * np.ones(n) if kind != "mixed" else g.random((L, n))
+    if kind == "falling":
+        at = at[::-1]
+    power = 3 - 63 * (1 - at) / (1 + np.arange(n)) if kind != "largest" else 108 - 40 * at * np.arange(n)
+    step = 2.0 ** np.round(power) * g.uniform(1, 2, (L, n)) * (g.random((L, n)) < 0.9)
+    low = -8 * step
+    held = Held(d, group, g.integers(0, 4, L), g.integers(0, 16, (L, d)), step, low, seed=4)
+    held.check(eng, [1.0, 0.5, 0.0, 2.0, -1.0], width, [[0, 16], [31, 33], [1000, 5000]])

@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kMergeMaxWarps * 32) decode_merge_kernel(const
         val = Mg == kBrokenMax ? 0.f : val * inv + steer_d;
         orow[d] = __float2bfloat16(val);
     }
-    if (mrow && d < a.S) mrow[d] = mm * inv;
+    if (mrow && d < a.S) mrow[d] = Mg == kBrokenMax ? 0.f : mm * inv;     // whatever the rest of the row holds
 }
 
 // ------------------------------------------------------------------------------------------

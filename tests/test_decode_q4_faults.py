@@ -1,0 +1,34 @@
+"""The rows of a page out of range over a 4-bit cache, beside pages that read as NaN."""
+import pytest
+import torch
+
+from paper_2603_06588_b200 import binding
+
+from .test_decode_q4 import Case
+
+
+@pytest.fixture(scope="module")
+def eng():
+    return binding.HookAttn(0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width", [0, 40000])
+@pytest.mark.parametrize("kind", ["keys", "values"])
+@pytest.mark.parametrize("bad,odd", [(6, 1), (1, 6), (20, 3), (3, 20), (40, 41), (43, 0)])
+def test_nothing_is_left_of_a_broken_row(eng, bad, odd, kind, width):
+    """A page out of range and one whose keys or values are NaN, in one warp's run, in two of a chunk, in two
+    chunks: outputs and span masses of that row are zeros, and the other rows are as they were."""
+    c = Case([700, 700], 8, 2, 128, 128, spans=3, steer=True, width=width)
+    c.mask[:] = 1
+    good = eng.hook_attn_decode_q4(**c.kw())
+    kw = c.kw()
+    pages, kw["block_table"] = c.pages.clone(), kw["block_table"].clone()
+    at = 16 * 128 + (16 * 4 if kind == "values" else 0)
+    pages[int(c.table[0, odd]), :, at:at + 16 * 4] = 0xFF
+    kw["block_table"][0, bad] = len(c.slabs)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, mass = eng.hook_attn_decode_q4(**{**kw, "pages": pages, "status": status})
+    assert int(status.item()) == binding.HOOK_ATTN_ERR_BOUNDS
+    assert torch.equal(out[0], torch.zeros_like(out[0])) and torch.equal(mass[0], torch.zeros_like(mass[0]))
+    assert torch.equal(out[1], good[0][1]) and torch.equal(mass[1], good[1][1])

@@ -38,6 +38,7 @@ constexpr int kQ4CtasPerSM = 4;       // at most
 // With four groups and no span sums the registers of three CTAs do without memory: 4 x 32768 keys 49.5 us, and 52.6 with four; with span sums 58 and 54.
 constexpr int q4_ctas(int ng, int ns) { return ng == 4 && ns == 0 ? 3 : kQ4CtasPerSM; }
 constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
+constexpr float kLargestMax = 3.40282326e38f;         // infinite scores count as this in the reference, below kBrokenMax; their probabilities are infinite
 constexpr float kTopStep = 128.f;     // steps times their frame are below this
 constexpr float kFirstFrame = 1.6225928e32f;          // 2^107: steps are at least 2^-100
 
@@ -315,7 +316,7 @@ struct Q4Walk {
                     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
                     mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
                 }
-                const float n0 = fmaxf(m0, mx0), n1 = fmaxf(m1, mx1);
+                const float n0 = fminf(fmaxf(m0, mx0), kLargestMax), n1 = fminf(fmaxf(m1, mx1), kLargestMax);
                 const float c0 = fast_exp2(m0 - n0), c1 = fast_exp2(m1 - n1);
                 m0 = n0; m1 = n1;
                 l0 *= c0; l1 *= c1;

@@ -1,4 +1,4 @@
-"""The rows of a page out of range over a 4-bit cache, beside pages that read as NaN."""
+"""The rows of a page out of range over a 4-bit cache, beside pages that read as NaN or whose scores are infinite."""
 import pytest
 import torch
 
@@ -14,18 +14,19 @@ def eng():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("width", [0, 40000])
-@pytest.mark.parametrize("kind", ["keys", "values"])
+@pytest.mark.parametrize("kind", ["keys", "values", "scores"])
 @pytest.mark.parametrize("bad,odd", [(6, 1), (1, 6), (20, 3), (3, 20), (40, 41), (43, 0)])
 def test_nothing_is_left_of_a_broken_row(eng, bad, odd, kind, width):
-    """A page out of range and one whose keys or values are NaN, in one warp's run, in two of a chunk, in two
-    chunks: outputs and span masses of that row are zeros, and the other rows are as they were."""
-    c = Case([700, 700], 8, 2, 128, 128, spans=3, steer=True, width=width)
+    """A page out of range and one whose keys or values are NaN, or whose keys are so large that scores overflow, in one warp's run, in two of a chunk,
+    in two chunks: outputs and span masses of that row are zeros, and the other rows are as they were."""
+    c = Case([700, 700], 8, 2, 128, 128, spans=3, steer=True, width=width, q_size=64.0 if kind == "scores" else 1.0)
     c.mask[:] = 1
     good = eng.hook_attn_decode_q4(**c.kw())
     kw = c.kw()
     pages, kw["block_table"] = c.pages.clone(), kw["block_table"].clone()
     at = 16 * 128 + (16 * 4 if kind == "values" else 0)
-    pages[int(c.table[0, odd]), :, at:at + 16 * 4] = 0xFF
+    pair = [0, 0, 0x7F, 0x7F] if kind == "scores" else [0xFF] * 4                 # lowest 3.4e38; NaN
+    pages[int(c.table[0, odd]), :, at:at + 16 * 4] = torch.tensor(pair * 16, dtype=torch.uint8, device="cuda")
     kw["block_table"][0, bad] = len(c.slabs)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     out, mass = eng.hook_attn_decode_q4(**{**kw, "pages": pages, "status": status})

@@ -38,7 +38,7 @@ constexpr int kQ4CtasPerSM = 4;       // at most
 // With four groups and no span sums the registers of three CTAs do without memory: 4 x 32768 keys 49.5 us, and 52.6 with four; with span sums 58 and 54.
 constexpr int q4_ctas(int ng, int ns) { return ng == 4 && ns == 0 ? 3 : kQ4CtasPerSM; }
 constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
-constexpr float kLargestMax = 3.40282326e38f;         // infinite scores count as this in the reference, below kBrokenMax; their probabilities are infinite
+constexpr float kLargestMax = 3.40282326e38f;         // the references stay within it, below kBrokenMax; the probability of an infinite score is infinite
 constexpr float kTopStep = 128.f;     // steps times their frame are below this
 constexpr float kFirstFrame = 1.6225928e32f;          // 2^107: steps are at least 2^-100
 
@@ -112,6 +112,7 @@ struct Q4Walk {
 #pragma unroll
         for (int j = 0; j < NSX; ++j) sm[j][0] = sm[j][1] = 0.f;
         if (seg <= 0) return;
+        m0 = m1 = -kLargestMax;                                       // finite, so that keys whose scores are all -infinity weigh nothing
 
         const int32_t* bt = a.block_table + (int64_t)s * a.max_blocks + pg;
         const int key_base = pg * kPage, key_end = min(L, key_base + seg * kPage);

@@ -379,7 +379,8 @@ int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params
  * Where the cache and not the model bounds the number of sequences: keys and values of 16 tokens in 2.1 to 2.5 KB a
  * head of 128 instead of 8 KB.  Block tables, lengths and the pool calls above are as for a bf16 cache; the pages are
  * written by hook_rope_append_q4, read by hook_attn_decode_q4, and read back to bf16 pages for whatever else reads a
- * cache (hook_attn_prefill of a prompt's next chunk, hook_capture_qk) by hook_cache_read_q4.
+ * cache (hook_attn_prefill of a prompt's next chunk, hook_capture_qk) by hook_cache_read_q4.  A sequence has at most 2^31 - 4096 tokens; a longer
+ * one is a fault, like one that is longer than its table.
  *
  * A head's elements share a step and a lowest value in groups of `group` neighbours.  Of the group's elements, rounded
  * to bf16 (what a bf16 cache holds), lowest is the least, step = (greatest - lowest) / 15 rounded to bf16 (0 if that is below

@@ -243,7 +243,7 @@ size_t hook_attn_workspace_bytes(const hook_attn_params* p, int is_decode)
     if (validate_common(p, is_decode != 0) != HOOK_ATTN_OK) return 0;
     if (!is_decode) return 0;
     const int G = p->num_q_heads / p->num_kv_heads;
-    if (is_decode == 3) return decode_q4_workspace_bytes(p->num_seqs, p->num_kv_heads, G, p->head_dim, max_keys_of(p));
+    if (is_decode == 3) return decode_q4_workspace_bytes(p->num_seqs, p->num_kv_heads, G, p->head_dim, (int)min64(max_keys_of(p), kQ4MostKeys));
     const size_t alone = decode_workspace_bytes(p->num_seqs, p->num_kv_heads, G, p->head_dim, max_keys_of(p));
     if (is_decode != 2) return alone;
     // the decode half of hook_attn_mixed: the one-launch path cuts by page shares whatever the unit count,
@@ -490,7 +490,7 @@ static int prepare_rope(const hook_attn_handle* handle, const hook_rope_params* 
     a.status = p->status;
     a.num_seqs = p->num_seqs; a.total_q = p->total_q; a.Hq = p->num_q_heads; a.Hkv = p->num_kv_heads;
     a.head_dim = p->head_dim; a.pairs = pairs; a.num_blocks = p->num_blocks; a.max_blocks = p->max_blocks_per_seq;
-    a.max_keys = (int32_t)min64((int64_t)p->max_blocks_per_seq * kPage, INT32_MAX);
+    a.max_keys = (int32_t)min64((int64_t)p->max_blocks_per_seq * kPage, q4 ? kQ4MostKeys : INT32_MAX);
     a.factor = p->factor == 0.f ? 1.f : p->factor;
     a.halves = p->pairing == HOOK_ROPE_PAIR_HALVES;
     for (int pair = 0, axis = 0; pair < pairs; ++pair) {
@@ -665,6 +665,7 @@ int hook_attn_decode_q4(hook_attn_handle* handle, const hook_attn_params* p, con
     HeadCfg hc;
     if ((rc = prepare(&q, true, a, hc)) != HOOK_ATTN_OK) return rc;
     if (p->num_seqs > 0 && p->max_blocks_per_seq == 0) return HOOK_ATTN_ERR_INVALID_ARG;
+    a.max_keys = (int)min64(a.max_keys, kQ4MostKeys);
     if (p->num_seqs > 0) {
         const size_t need = decode_q4_workspace_bytes(p->num_seqs, p->num_kv_heads, a.G, p->head_dim, a.max_keys);
         if (!p->workspace || p->workspace_bytes < need || (reinterpret_cast<uintptr_t>(p->workspace) & 255u)) return HOOK_ATTN_ERR_WORKSPACE;
@@ -703,7 +704,7 @@ int hook_cache_read_q4(hook_attn_handle* handle, const hook_q4_read_params* p, c
     a.num_blocks = p->num_blocks; a.max_blocks = p->max_blocks_per_seq;
     a.to_num_blocks = p->to_num_blocks; a.to_max_blocks = p->to_max_blocks_per_seq;
     const int64_t shorter = min64(p->max_blocks_per_seq, p->to_max_blocks_per_seq);
-    a.max_keys = (int32_t)min64(shorter * kPage, INT32_MAX);
+    a.max_keys = (int32_t)min64(shorter * kPage, kQ4MostKeys);
     cudaError_t e = launch_q4_read(a, p->head_dim, cache->group, handle->num_sms, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? HOOK_ATTN_OK : HOOK_ATTN_ERR_CUDA;
 }

@@ -15,6 +15,9 @@
 
 namespace hook_attn {
 
+// Tokens of a sequence at most: far enough from 2^31 that the end of a chunk or of a few pages behind any token is an int.
+constexpr int kQ4MostKeys = 0x7fffffff - 4095;
+
 template <int HD, int NG>
 struct Q4Slab {
     static constexpr int kRow = HD / 2;                       // bytes of a token's codes

@@ -383,10 +383,10 @@ int hook_cache_copy_pages(hook_attn_handle* handle, const hook_cache_copy_params
  * one is a fault, like one that is longer than its table.
  *
  * A head's elements share a step and a lowest value in groups of `group` neighbours.  Of the group's elements, rounded
- * to bf16 (what a bf16 cache holds), lowest is the least, step = (greatest - lowest) / 15 rounded to bf16 (0 if that is below
- * 2^-100), and an element x has the code nearest to (x - lowest) / step, 0 .. 15, x - lowest rounded to 32 bits and halves to
- * even (0 where the step is 0).  It reads as lowest + step * code.  A group that holds an infinity or a NaN, or whose step
- * overflows, reads as NaN.
+ * to bf16 (what a bf16 cache holds), lowest is the least, step = (greatest - lowest) / 15, both in 32 bits, rounded to bf16 (0 if
+ * that is below 2^-100), and an element x has the code nearest to (x - lowest) / step, 0 .. 15, x - lowest rounded to 32 bits and halves
+ * to even (0 where the step is 0).  It reads as lowest + step * code.  A group that holds an infinity or a NaN, or whose greatest - lowest
+ * overflows 32 bits, reads as NaN.
  *
  * A page's part for one KV head is a slab of hook_q4_slab_bytes(head_dim, group) bytes: 16 head_dim / 2 bytes of K codes, as
  * many of V codes, then for K and for V the pairs (step, lowest) of bf16 [16][head_dim / group].  The codes of token t, element e:
@@ -409,7 +409,7 @@ int hook_rope_append_q4(hook_attn_handle* handle, const hook_rope_params* p, con
 /* hook_attn_decode over a 4-bit cache: the same arguments, outputs, hooks and faults, k_cache, v_cache and the kv strides of `p` being
  * ignored.  `workspace` holds hook_attn_workspace_bytes(p, 3) bytes.  Scores, softmax, span masses and the sums over the values
  * are in 32 bits; a probability times a step of V is rounded to 11 bits or, below 2^-20 of the largest probability times the largest step of
- * the same group, to multiples of 2^-30 of the latter.  Elements of q below 2^-27 of their head's largest are rounded to 2^-34 of it. */
+ * the same group, to within 2^-31 of the latter.  Elements of q below 2^-27 of their head's largest are rounded to within 2^-35 of it. */
 int hook_attn_decode_q4(hook_attn_handle* handle, const hook_attn_params* p, const hook_q4_cache* cache, void* cuda_stream);
 
 typedef struct {

@@ -13,9 +13,10 @@
 // keeps the largest so far in [2^6, 2^7) and comes out of the group's sums in the end.  So a product is off by 2^-11 of itself, or by 2^-31 of
 // the group's largest step where that is more (from a probability of 2^-20 of the largest on), whatever the other groups hold.
 //
-// What bounds it is not HBM but the integer pipe: 340 to 410 instructions a page and KV head of 128 (two to four groups), 180 of them on the pipe that masks, shifts and
-// permutes take at half rate (58 % busy; issue slots 60 %, tensor pipe 24 %, DRAM 47 %).  256 sequences of 1024 to 8192 keys (683 MB): 166 us,
-// 4.1 TB/s; 4 x 32768 keys of 8 heads in four groups, eight spans (168 MB): 54 us, 3.1 TB/s; 128 x 4096 in one, two and four groups 111, 119 and 140 us.
+// What bounds it is not HBM but instructions: 345 to 425 a page and KV head of 128 (two to four groups), 180 of them on the pipe that masks, shifts and
+// permutes take at half rate (58 % busy; issue slots 62 %, tensor pipe 24 %, DRAM 46 %), and the waits for their fixed latencies.  256 sequences of 1024 to
+// 8192 keys (683 MB): 165 to 176 us by box, 3.9 to 4.1 TB/s; 4 x 32768 keys of 8 heads in four groups, eight spans (168 MB): 56 us, 3.0 TB/s; 128 x 4096 in
+// one, two and four groups 112, 121 and 145 us.  One power of two for the steps of all groups took 55 us in four groups and lost small ones.
 // A page at a time with the spans tested on each took 188 and 68 us; five CTAs an SM (96 registers) 192 us, three 167; the shifts by
 // multiplication on the other pipe 182 us.
 #include <type_traits>
@@ -35,7 +36,7 @@ constexpr int kQ4Pages = 2;           // pages that a warp takes at a time
 constexpr int kQ4Stages = 2;          // such pairs in flight or in use per warp
 constexpr int kQ4Keys = kQ4Pages * kPage;
 constexpr int kQ4CtasPerSM = 4;       // at most
-// With four groups and no span sums the registers of three CTAs do without memory: 4 x 32768 keys 49.5 us, and 52.6 with four; with span sums 58 and 54.
+// With four groups and no span sums the registers of three CTAs do without memory: 4 x 32768 keys 51 us, and 54 with four; with span sums 59 and 56.
 constexpr int q4_ctas(int ng, int ns) { return ng == 4 && ns == 0 ? 3 : kQ4CtasPerSM; }
 constexpr int kQ4MaxWorkers = kQ4CtasPerSM * kDecMaxSMs * kDecWarps;
 constexpr float kLargestMax = 3.40282326e38f;         // the references stay within it, below kBrokenMax; the probability of an infinite score is infinite

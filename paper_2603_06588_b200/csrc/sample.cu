@@ -13,8 +13,13 @@
 // sums are the same, and a random number that falls next to a border is on the same side in every run and for every cluster size.
 //
 // Reading the row is the least of it.  A token takes some 50 instructions where every weight is needed (12 of them in 64 bits) and 20 in a pass that only compares;
-// a cluster's six exchanges, the scans and the lists cost a row about 10 us.  256 x 160000 fp32: 206 us with rows of all filters, 142 without any, 173 top-k,
-// 242 top-p; 1 x 32000 bf16: 15.6, 10.4, 11.7 and 12.0 us.  Issue slots are half busy at 32 warps an SM, which barriers and loads hold up by turns.
+// a cluster's six exchanges, the scans and the lists cost a row about 10 us.  256 x 160000 fp32: 203 us with rows of all filters, 141 without any, 171 top-k,
+// 240 top-p; 1 x 32000 bf16: 15.1, 10.3, 11.7 and 11.7 us.  Issue slots are half busy at 32 warps an SM, which barriers and loads hold up by turns.
+//
+// Those are steep rows.  Where a CTA has more than 64 tokens in the boundary's bin (flat rows, many ties, a border among the thousandth tokens), the passes
+// by the keys' bits follow, a token at a time, and those of one key are added in shared memory one after the other: 256 x 160000 with top-p 0.9 takes 0.32 ms with
+// logits of deviation 3, 0.84 with 0.05 or evenly spread ones, 1.4 with two values and 2.1 with one; top-k 50 0.19, 0.19 to 0.33, 0.6 and 1.2;
+// 1 x 32000 bf16 with top-p 15, 32, 39 and 49 us.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
@@ -68,7 +73,7 @@ struct alignas(16) SampleShared {
     unsigned int draw_ties[kWarps];
     double per_logit, below;               // log2(e) / T; how far below the largest logit min_p's border lies
     unsigned long long found_before;
-    int found_bin, found_from, found_to, too_many;
+    int found_bin, found_from, found_to;
     unsigned int listed_count, listed[kShare], all[kList], all_count[kMostCtas], keys[kList], pick;
     unsigned long long amounts[kList];
 };
